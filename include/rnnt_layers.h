@@ -1,0 +1,121 @@
+/*
+ * rnnt_layers.h - C ABI of the layers beside the transducer loss of rnnt_joint_loss.h (same library, same conventions, statuses
+ * and dtypes): what the encoders in front of the joint network are made of, and the other loss of its output layer.
+ *
+ *   rnnt_linear_*    y = residual + dropout(act(x W + b)) and its gradients.  The dropout mask is a function of a seed, an offset and an entry's
+ *                    place and is never stored.
+ *   rnnt_ce_loss_*   cross entropy of softmax(x W + b) with one label per row, and its gradients, without the [R, V] scores.
+ *
+ * Conventions beyond those of rnnt_joint_loss.h: every array is dense; device pointers are 16-byte aligned (RNNT_ERR_UNSUPPORTED otherwise),
+ * workspaces 256-byte aligned.  Every call can be recorded into a HIP graph: all it needs is in its arguments and in device memory, it allocates
+ * nothing and copies nothing from the host.  Workspaces hold nothing between calls; calls that share one must be ordered (two graphs that may run
+ * side by side need two).  With RNNT_BF16 results are summed in a fixed order (equal bits from run to run); with RNNT_F32 the
+ * weight gradients are added to with float atomics and can differ in the last bits.
+ */
+#ifndef RNNT_LAYERS_H
+#define RNNT_LAYERS_H
+
+#include "rnnt_joint_loss.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+typedef enum {
+    RNNT_ACT_NONE = 0,
+    RNNT_ACT_RELU = 1,
+    RNNT_ACT_SILU = 2, /* z sigmoid(z)                              */
+    RNNT_ACT_GELU = 3, /* z Phi(z), Phi the normal distribution's   */
+    RNNT_ACT_TANH = 4
+} rnnt_activation;
+
+typedef struct {
+    int64_t M;          /* rows, 0..2^30                                                                    */
+    int32_t K;          /* inputs, 1..2^20                                                                  */
+    int32_t N;          /* outputs, 1..2^20                                                                 */
+    int32_t dtype;      /* rnnt_dtype of x, W, residual, y, their gradients                                 */
+    int32_t activation; /* rnnt_activation                                                                  */
+    float dropout;      /* probability p of an entry to be dropped, 0 <= p < 1; taken as cut / 65536 with the integer cut nearest to 65536 p (at most
+                           65535)                                                                                                       */
+    int32_t accumulate_params; /* backward: 0: dW, db are overwritten; 1: added to (they are float then)    */
+    int32_t param_grads_bf16;  /* backward, RNNT_BF16 only: bit 0: dW is bfloat16, bit 1: db is bfloat16; else float.  */
+} rnnt_linear_desc;
+
+/*
+ * z = x W + b,  a = act(z),  y = residual + a m / (1 - p)
+ *
+ * m: entry (r, n) is kept where its 16 random bits are at least cut.  They come from Philox4x32-10 with the key {low, high word of the seed} on the
+ * counter {n / 8, r, low, high word of the offset}: entry n takes half n % 2 (0: the low one) of word (n % 8) / 2.  The same seed and offset give the
+ * same mask, whatever the sizes of the call; calls that shall have different ones (layers, steps) take different offsets or seeds.
+ *
+ * x        dev [M, K]   desc->dtype
+ * W        dev [K, N]   desc->dtype (the transpose of a torch Linear's weight)
+ * b        dev [N]      float, or NULL
+ * residual dev [M, N]   desc->dtype, or NULL
+ * rng      dev [2]      {seed, offset}, read by the kernels when they run (a replayed graph takes what is there then); NULL allowed with p = 0
+ * y        dev [M, N]   desc->dtype, out
+ * saved    dev [M, N]   out, or NULL: z for the backward pass, two bytes per entry with RNNT_BF16 (fp16), four with RNNT_F32.  The backward
+ *                       pass of RNNT_ACT_NONE does without.
+ * RNNT_BF16: the product runs on bf16 MFMA with fp32 accumulation, everything behind it in fp32, one rounding at the end.
+ * workspace_bytes >= rnnt_linear_workspace_bytes(desc, 0); with 0 bytes workspace may be NULL.
+ */
+size_t rnnt_linear_workspace_bytes(const rnnt_linear_desc* desc, int32_t backward);
+rnnt_status rnnt_linear_fwd(const rnnt_linear_desc* desc, const void* x, const void* W, const float* b, const void* residual,
+                            const uint64_t* rng, void* y, void* saved, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Gradients for an incoming dy = d/dy: with dz = dy act'(z) m / (1 - p)
+ *   dx = dz W^T,  dW = x^T dz,  db = column sums of dz   (and dy itself is the residual's)
+ * RNNT_BF16: dz is rounded to bfloat16 as the operand of both products (db: before that rounding).
+ *
+ * x, W, rng as in the forward call, with the same values; saved: what it left (NULL allowed with RNNT_ACT_NONE)
+ * dy dev [M, N] desc->dtype;  dx dev [M, K] desc->dtype, out;  dW dev [K, N], db dev [N], out.  Each of dx, dW, db may be NULL: not wanted.
+ * workspace_bytes >= rnnt_linear_workspace_bytes(desc, 1).
+ */
+rnnt_status rnnt_linear_bwd(const rnnt_linear_desc* desc, const void* x, const void* W, const void* saved, const uint64_t* rng, const void* dy,
+                            void* dx, void* dW, void* db, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+typedef struct {
+    int64_t R;            /* rows, 0..2^30                                                                  */
+    int32_t D;            /* width of x, 1..2^20                                                            */
+    int32_t V;            /* vocabulary, 1..2^20                                                            */
+    int32_t dtype;        /* rnnt_dtype of x, W and their gradients                                         */
+    int32_t ignore_label; /* rows with this label are padding                                               */
+    int32_t accumulate_params; /* 0: dW, db are overwritten; 1: added to (they are float then)              */
+    int32_t param_grads_bf16;  /* RNNT_BF16 only: bit 0: dW is bfloat16, bit 1: db is bfloat16; else float  */
+} rnnt_ce_desc;
+
+/*
+ * h = x W + b,  loss[r] = ln sum_v e^{h[r, v]} - h[r, label[r]]      (natural log)
+ * and, for L = sum_r row_weight[r] loss[r] (dh = row_weight (softmax(h) - onehot)),  dx = dh W^T,  dW = x^T dh,  db = column sums of dh.
+ *
+ * The rows that are no padding are put together and go through in chunks: a chunk's exponentials (RNNT_BF16: fp16 relative to
+ * maxima over parts of the vocabulary; RNNT_F32: its scores) are kept in the workspace until its score gradients have replaced them.  Three
+ * products per row, as many as the gradients need.
+ *
+ * x          dev [R, D]  desc->dtype; padding rows may hold anything and are never used
+ * W          dev [D, V]  desc->dtype (W_out of rnnt_joint_loss_fwd_bwd)
+ * b          dev [V]     float, or NULL; -inf takes an entry out of the vocabulary
+ * label      dev [R]     int32
+ * row_weight dev [R]     float, any sign, or NULL (ones); read by the kernels
+ * loss       dev [R]     float, out; 0 in padding rows; +inf where the label is outside [0, V) (its gradient then is row_weight softmax(h)) or no entry
+ *                        of the vocabulary is possible (all scores -inf: its gradient is that of the label alone)
+ * dx         dev [R, D]  desc->dtype, out; zeros in padding rows
+ * dW dev [D, V], db dev [V] (NULL: not wanted), out
+ * RNNT_BF16: the three products run on bf16 MFMA with fp32 accumulation, the softmax in fp32; dh is rounded to bfloat16 as their operand.
+ *
+ * workspace bytes: grads = 0 for rnnt_ce_loss_fwd, 1 for rnnt_ce_loss_fwd_bwd.  budget_bytes = 0: the library's default (chunk buffers of at most
+ * 1 GiB); otherwise chunks as large as fit the budget, and if even the smallest (256 rows) exceed it, their size.  A workspace larger than that of the
+ * default is used for larger chunks.
+ */
+size_t rnnt_ce_loss_workspace_bytes(const rnnt_ce_desc* desc, int32_t grads, size_t budget_bytes);
+rnnt_status rnnt_ce_loss_fwd(const rnnt_ce_desc* desc, const void* x, const void* W, const float* b, const int32_t* label, float* loss,
+                             void* workspace, size_t workspace_bytes, void* hip_stream);
+rnnt_status rnnt_ce_loss_fwd_bwd(const rnnt_ce_desc* desc, const void* x, const void* W, const float* b, const int32_t* label,
+                                 const float* row_weight, float* loss, void* dx, void* dW, void* db, void* workspace, size_t workspace_bytes,
+                                 void* hip_stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* RNNT_LAYERS_H */

@@ -68,3 +68,98 @@ def rnnt_joint_loss(enc, pred, W_out, b_out, labels, T_len, U_len, blank: int = 
     (bfloat16 only): the descriptor field of that name, scores kept in a larger workspace instead of computed twice."""
     return _RnntJointLoss.apply(enc, pred, W_out, b_out, labels, T_len, U_len, blank, sample_weight, workspace,
                                 keep_scores)
+
+
+class _RnntLinear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, W, b, activation, residual, dropout, rng_state):
+        # the state as the kernels see it now: the caller may advance it before the backward pass
+        rng = rng_state.clone() if rng_state is not None and dropout > 0.0 else None
+        need = any(ctx.needs_input_grad[:3])
+        out = Bd.run_linear_fwd(x, W, None if b is None else b.float(), activation, residual, dropout, rng, save=need)
+        ctx.save_for_backward(x, W, out["saved"], rng)
+        ctx.activation, ctx.dropout, ctx.b_dtype = activation, dropout, None if b is None else b.dtype
+        return out["y"]
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, W, saved, rng = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        want = tuple(k for k, n in zip(("dx", "dW", "db"), need) if n)
+        g = dict(dx=None, dW=None, db=None)
+        dy = dy.contiguous()
+        if want:
+            bf16 = 0 if W.dtype == torch.float32 else 1 | (2 if ctx.b_dtype == torch.bfloat16 else 0)
+            g = Bd.run_linear_bwd(x, W, dy, ctx.activation, saved, ctx.dropout, rng, param_grads_bf16=bf16, want=want)
+        db = g["db"]
+        return g["dx"], g["dW"], db if db is None else db.to(ctx.b_dtype), None, dy if need[4] else None, None, None
+
+
+def rnnt_linear(x, W, b=None, activation="none", residual=None, dropout: float = 0.0, rng_state=None):
+    """residual + dropout(act(x W + b)) with gradients for x, W, b and residual.
+
+    x [..., K], W [K, N] (float32 or bfloat16, CUDA, contiguous), b [N] (float32 or bfloat16) or None, residual [..., N] or None; activation: none,
+    relu, silu, gelu, tanh.  dropout in [0, 1) needs rng_state, an int64 tensor [2] on the device with {seed, offset}: the mask is a function of them
+    and of an entry's place, so advance the offset between calls that shall have different masks (in place, also inside a captured graph)."""
+    return _RnntLinear.apply(x, W, b, activation, residual, float(dropout), rng_state)
+
+
+class _RnntCeSum(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, W, b, labels, row_weight, ignore_label, budget_bytes):
+        if not any(ctx.needs_input_grad[:3]):
+            loss = Bd.run_ce_fwd(x, W, None if b is None else b.float(), labels, ignore_label, budget_bytes=budget_bytes)["loss"]
+        else:
+            bf16 = 0 if W.dtype == torch.float32 else 1 | (2 if b is not None and b.dtype == torch.bfloat16 else 0)
+            out = Bd.run_ce_fwd_bwd(x, W, None if b is None else b.float(), labels, row_weight, ignore_label, param_grads_bf16=bf16,
+                                    budget_bytes=budget_bytes)
+            loss = out["loss"]
+            ctx.save_for_backward(out["dx"], out["dW"], out["db"])
+            ctx.b_dtype = None if b is None else b.dtype
+        # (a row of weight 0 counts for nothing, whatever its loss is)
+        return loss.sum() if row_weight is None else torch.where(row_weight == 0, 0.0, loss * row_weight).sum()
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, g):
+        dx, dW, db = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        return ((dx * g).to(dx.dtype) if need[0] else None, (dW * g).to(dW.dtype) if need[1] else None,
+                (db * g).to(ctx.b_dtype) if need[2] else None, None, None, None, None)
+
+
+class _RnntCeRows(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, W, b, labels, ignore_label, budget_bytes):
+        ctx.save_for_backward(x, W, b, labels)
+        ctx.opts = ignore_label, budget_bytes
+        return Bd.run_ce_fwd(x, W, None if b is None else b.float(), labels, ignore_label, budget_bytes=budget_bytes)["loss"]
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, g):
+        x, W, b, labels = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        bf16 = 0 if W.dtype == torch.float32 else 1 | (2 if b is not None and b.dtype == torch.bfloat16 else 0)
+        out = Bd.run_ce_fwd_bwd(x, W, None if b is None else b.float(), labels, g.contiguous().float(), ctx.opts[0], param_grads_bf16=bf16,
+                                budget_bytes=ctx.opts[1])
+        return (out["dx"] if need[0] else None, out["dW"] if need[1] else None, out["db"].to(b.dtype) if b is not None and need[2] else None,
+                None, None, None)
+
+
+def rnnt_ce_loss(x, W, b, labels, row_weight=None, ignore_label: int = -1, reduction: str = "sum", budget_bytes: int = 0):
+    """Cross entropy of softmax(x W + b) with gradients for x, W and b, without the [rows, V] scores.
+
+    x [..., D], W [D, V] (float32 or bfloat16, CUDA, contiguous), b [V] (float32 or bfloat16) or None, labels [...] int32 (rows with ignore_label are
+    padding: loss and gradients 0, x never used).
+    reduction "sum": sum of row_weight * loss over the rows (row_weight [...] float32 on the device, None: ones; 1 / count for a mean), a scalar.  The
+    forward call computes the gradients too (three products per row); backward scales them.
+    reduction "none": the loss of each row; the gradients are computed in backward, with the incoming gradient as the rows' weights (four products)."""
+    if reduction == "sum":
+        return _RnntCeSum.apply(x, W, b, labels, row_weight, ignore_label, budget_bytes)
+    if reduction != "none":
+        raise ValueError(f"reduction must be 'sum' or 'none', got {reduction!r}")
+    if row_weight is not None:
+        raise ValueError("row_weight goes with reduction='sum'; with 'none' weight the returned losses")
+    return _RnntCeRows.apply(x, W, b, labels, ignore_label, budget_bytes)

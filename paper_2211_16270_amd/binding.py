@@ -25,6 +25,10 @@ EXPORTS = ["rnnt_status_string", "rnnt_last_hip_error", "rnnt_joint_loss_workspa
            "rnnt_joint_proj_workspace_bytes", "rnnt_joint_proj_loss_fwd_bwd", "rnnt_joint_loss_fwd_bwd_weighted",
            "rnnt_joint_loss_fwd_bwd_static", "rnnt_plan_create", "rnnt_plan_workspace_bytes", "rnnt_plan_describe",
            "rnnt_plan_destroy", "rnnt_joint_loss_fwd_bwd_planned", "rnnt_debug_read_active_tiles"]
+# include/rnnt_layers.h
+LAYER_EXPORTS = ["rnnt_linear_workspace_bytes", "rnnt_linear_fwd", "rnnt_linear_bwd", "rnnt_ce_loss_workspace_bytes", "rnnt_ce_loss_fwd",
+                 "rnnt_ce_loss_fwd_bwd"]
+ACTIVATIONS = ["none", "relu", "silu", "gelu", "tanh"]          # rnnt_activation
 RNNT_STATIC_SCRATCH_BYTES = 128 << 20
 
 
@@ -42,6 +46,17 @@ class RnntPlanInfo(ctypes.Structure):
                 ("n_chunks", ctypes.c_int32), ("group_rows_cap", ctypes.c_int64),
                 ("chunk_rows", ctypes.c_int64), ("workspace_bytes", ctypes.c_size_t),
                 ("lattice_bytes", ctypes.c_size_t), ("chunk_bytes", ctypes.c_size_t)]
+
+
+class RnntLinearDesc(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int64), ("K", ctypes.c_int32), ("N", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("activation", ctypes.c_int32), ("dropout", ctypes.c_float), ("accumulate_params", ctypes.c_int32),
+                ("param_grads_bf16", ctypes.c_int32)]
+
+
+class RnntCeDesc(ctypes.Structure):
+    _fields_ = [("R", ctypes.c_int64), ("D", ctypes.c_int32), ("V", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("ignore_label", ctypes.c_int32), ("accumulate_params", ctypes.c_int32), ("param_grads_bf16", ctypes.c_int32)]
 
 
 class RnntError(RuntimeError):
@@ -134,6 +149,19 @@ def lib() -> ctypes.CDLL:
     L.rnnt_profile_kernel_name.argtypes = [ctypes.c_int32]
     L.rnnt_profile_read.restype = ctypes.c_int
     L.rnnt_profile_read.argtypes = [ctypes.c_int32, ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_double)]
+    lp, cp = ctypes.POINTER(RnntLinearDesc), ctypes.POINTER(RnntCeDesc)
+    L.rnnt_linear_workspace_bytes.restype = ctypes.c_size_t
+    L.rnnt_linear_workspace_bytes.argtypes = [lp, ctypes.c_int32]
+    L.rnnt_linear_fwd.restype = ctypes.c_int
+    L.rnnt_linear_fwd.argtypes = [lp] + [vp] * 8 + [ctypes.c_size_t, vp]
+    L.rnnt_linear_bwd.restype = ctypes.c_int
+    L.rnnt_linear_bwd.argtypes = [lp] + [vp] * 9 + [ctypes.c_size_t, vp]
+    L.rnnt_ce_loss_workspace_bytes.restype = ctypes.c_size_t
+    L.rnnt_ce_loss_workspace_bytes.argtypes = [cp, ctypes.c_int32, ctypes.c_size_t]
+    L.rnnt_ce_loss_fwd.restype = ctypes.c_int
+    L.rnnt_ce_loss_fwd.argtypes = [cp] + [vp] * 6 + [ctypes.c_size_t, vp]
+    L.rnnt_ce_loss_fwd_bwd.restype = ctypes.c_int
+    L.rnnt_ce_loss_fwd_bwd.argtypes = [cp] + [vp] * 10 + [ctypes.c_size_t, vp]
     _lib = L
     return L
 
@@ -476,3 +504,219 @@ def run_proj_fwd_bwd(dev: dict, devp: dict, B, T_max, U_max, H, V, blank, dtype,
         raise RnntError(st, "rnnt_joint_proj_loss_fwd_bwd")
     out.update(workspace=workspace, desc=desc)
     return out
+
+
+# ---- include/rnnt_layers.h: the linear layer with its epilogue, the output layer's cross entropy ---------------------------------
+
+def _nbytes(t) -> int:
+    return 0 if t is None else int(t.numel() * t.element_size())
+
+
+def rnnt_linear_workspace_bytes(desc: RnntLinearDesc, backward: bool) -> int:
+    return int(lib().rnnt_linear_workspace_bytes(ctypes.byref(desc), int(backward)))
+
+
+def rnnt_linear_fwd(desc: RnntLinearDesc, x, W, b, residual, rng, y, saved, workspace=None, stream=None) -> int:
+    """Raw call: torch CUDA tensors (or None) of the layouts the header states.  Returns the status code; enqueues on `stream` (default: torch's
+    current stream) without synchronising."""
+    return int(lib().rnnt_linear_fwd(ctypes.byref(desc), _ptr(x), _ptr(W), _ptr(b), _ptr(residual), _ptr(rng), _ptr(y), _ptr(saved),
+                                     _ptr(workspace), _nbytes(workspace), _stream_handle(stream)))
+
+
+def rnnt_linear_bwd(desc: RnntLinearDesc, x, W, saved, rng, dy, dx, dW, db, workspace=None, stream=None) -> int:
+    return int(lib().rnnt_linear_bwd(ctypes.byref(desc), _ptr(x), _ptr(W), _ptr(saved), _ptr(rng), _ptr(dy), _ptr(dx), _ptr(dW), _ptr(db),
+                                     _ptr(workspace), _nbytes(workspace), _stream_handle(stream)))
+
+
+def rnnt_ce_loss_workspace_bytes(desc: RnntCeDesc, grads: bool, budget_bytes: int = 0) -> int:
+    return int(lib().rnnt_ce_loss_workspace_bytes(ctypes.byref(desc), int(grads), int(budget_bytes)))
+
+
+def rnnt_ce_loss_fwd(desc: RnntCeDesc, x, W, b, label, loss, workspace=None, stream=None) -> int:
+    return int(lib().rnnt_ce_loss_fwd(ctypes.byref(desc), _ptr(x), _ptr(W), _ptr(b), _ptr(label), _ptr(loss), _ptr(workspace),
+                                      _nbytes(workspace), _stream_handle(stream)))
+
+
+def rnnt_ce_loss_fwd_bwd(desc: RnntCeDesc, x, W, b, label, row_weight, loss, dx, dW, db, workspace=None, stream=None) -> int:
+    return int(lib().rnnt_ce_loss_fwd_bwd(ctypes.byref(desc), _ptr(x), _ptr(W), _ptr(b), _ptr(label), _ptr(row_weight), _ptr(loss), _ptr(dx),
+                                          _ptr(dW), _ptr(db), _ptr(workspace), _nbytes(workspace), _stream_handle(stream)))
+
+
+def _check_tensor(name, t, dtype, device, shape=None):
+    if t.device != device or t.dtype != dtype or not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor on {device}"
+                         + ("" if shape is None else f" of shape {tuple(shape)}")
+                         + f", got {t.dtype} {tuple(t.shape)} on {t.device}" + ("" if t.is_contiguous() else ", not contiguous"))
+
+
+def _aligned(t):
+    # (a view that starts inside a 16-byte piece is copied: the kernels move such pieces)
+    return t if t is None or t.data_ptr() % 16 == 0 else t.clone()
+
+
+class _CallOn:
+    """The device of the tensors made current, and `stream` (None: that device's current one), for allocations and launches."""
+
+    def __init__(self, device, stream):
+        import torch
+        self.contexts = []
+        if stream is not None:
+            if stream.device != device:
+                raise ValueError(f"stream on {stream.device}, tensors on {device}")
+            self.contexts.append(torch.cuda.stream(stream))
+        elif torch.cuda.current_device() != device.index:
+            self.contexts.append(torch.cuda.device(device))
+
+    def __enter__(self):
+        for c in self.contexts:
+            c.__enter__()
+
+    def __exit__(self, *exc):
+        for c in reversed(self.contexts):
+            c.__exit__(*exc)
+
+
+def _layer_dtype(x):
+    import torch
+    if not x.is_cuda:
+        raise ValueError("x must be a CUDA tensor")
+    if x.dtype == torch.bfloat16:
+        return RNNT_BF16
+    if x.dtype == torch.float32:
+        return RNNT_F32
+    raise ValueError(f"x must be bfloat16 or float32, got {x.dtype}")
+
+
+def _layer_workspace(workspace, nbytes, device):
+    import torch
+    if workspace is not None:
+        return workspace.buf
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+def _check_linear(x, W, activation, dropout, rng_state, accumulate, param_grads_bf16):
+    import torch
+    code = _layer_dtype(x)
+    if x.dim() < 1 or W.dim() != 2 or x.shape[-1] != W.shape[0]:
+        raise ValueError(f"x [..., K] and W [K, N] do not fit: {tuple(x.shape)}, {tuple(W.shape)}")
+    _check_tensor("x", x, x.dtype, x.device)
+    _check_tensor("W", W, x.dtype, x.device)
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {ACTIVATIONS}, got {activation!r}")
+    if not 0.0 <= dropout < 1.0:
+        raise ValueError(f"dropout must be in [0, 1), got {dropout}")
+    if dropout > 0.0 and rng_state is None:
+        raise ValueError("dropout needs rng_state, an int64 tensor [2] on the device: {seed, offset}")
+    if rng_state is not None:
+        _check_tensor("rng_state", rng_state, torch.int64, x.device, (2,))
+    K, N = W.shape
+    return RnntLinearDesc(x.numel() // K if K else 0, K, N, code, ACTIVATIONS.index(activation), float(dropout), int(accumulate),
+                          int(param_grads_bf16))
+
+
+def run_linear_fwd(x, W, b=None, activation="none", residual=None, dropout=0.0, rng_state=None, save=False,
+                   workspace: Optional[Workspace] = None, stream=None):
+    """y = residual + dropout(act(x W + b)): checks the tensors, allocates the outputs (and a workspace unless given), calls rnnt_linear_fwd, raises
+    on a non-zero status.  x [..., K], W [K, N] (bfloat16 or float32), b [N] float32 or None, residual [..., N] or None, rng_state int64 [2] on the
+    device {seed, offset}.  save: also keep what run_linear_bwd needs of an activation.  Returns dict(y, saved)."""
+    import torch
+    desc = _check_linear(x, W, activation, dropout, rng_state, 0, 0)
+    shape = x.shape[:-1] + (desc.N,)
+    if b is not None:
+        _check_tensor("b", b, torch.float32, x.device, (desc.N,))
+    if residual is not None:
+        _check_tensor("residual", residual, x.dtype, x.device, shape)
+    with _CallOn(x.device, stream):
+        y = torch.empty(shape, dtype=x.dtype, device=x.device)
+        saved = torch.empty(shape, dtype=torch.float16 if desc.dtype == RNNT_BF16 else torch.float32, device=x.device) \
+            if save and desc.activation != 0 else None
+        ws = _layer_workspace(workspace, rnnt_linear_workspace_bytes(desc, False), x.device)
+        st = rnnt_linear_fwd(desc, _aligned(x), _aligned(W), _aligned(b), _aligned(residual), rng_state, y, saved, ws)
+    if st != 0:
+        raise RnntError(st, "rnnt_linear_fwd")
+    return dict(y=y, saved=saved)
+
+
+def run_linear_bwd(x, W, dy, activation="none", saved=None, dropout=0.0, rng_state=None, accumulate_into=None, param_grads_bf16=0,
+                   want=("dx", "dW", "db"), workspace: Optional[Workspace] = None, stream=None):
+    """Gradients of run_linear_fwd for an incoming dy [..., N]; rng_state must hold what the forward call read.  accumulate_into: (dW, db) float32
+    to add to; param_grads_bf16: the descriptor's field; want: which of dx, dW, db.  Returns dict(dx, dW, db) (None: not wanted)."""
+    import torch
+    desc = _check_linear(x, W, activation, dropout, rng_state, accumulate_into is not None, param_grads_bf16)
+    shape = x.shape[:-1] + (desc.N,)
+    _check_tensor("dy", dy, x.dtype, x.device, shape)
+    if desc.activation != 0:
+        if saved is None:
+            raise ValueError(f"the backward pass of {activation} needs what the forward call saved")
+        _check_tensor("saved", saved, torch.float16 if desc.dtype == RNNT_BF16 else torch.float32, x.device, shape)
+    with _CallOn(x.device, stream):
+        dx = torch.empty_like(x) if "dx" in want else None
+        if accumulate_into is not None:
+            dW, db = accumulate_into
+            for name, t, s in (("dW", dW, (desc.K, desc.N)), ("db", db, (desc.N,))):
+                if t is not None:
+                    _check_tensor(name, t, torch.float32, x.device, s)
+        else:
+            kind = [torch.bfloat16 if desc.param_grads_bf16 >> bit & 1 else torch.float32 for bit in (0, 1)]
+            dW = torch.empty(desc.K, desc.N, dtype=kind[0], device=x.device) if "dW" in want else None
+            db = torch.empty(desc.N, dtype=kind[1], device=x.device) if "db" in want else None
+        ws = _layer_workspace(workspace, rnnt_linear_workspace_bytes(desc, True), x.device)
+        st = rnnt_linear_bwd(desc, _aligned(x), _aligned(W), _aligned(saved), rng_state, _aligned(dy), dx, dW, db, ws)
+    if st != 0:
+        raise RnntError(st, "rnnt_linear_bwd")
+    return dict(dx=dx, dW=dW, db=db)
+
+
+def _check_ce(x, W, b, labels, ignore_label, accumulate, param_grads_bf16):
+    import torch
+    code = _layer_dtype(x)
+    if x.dim() < 1 or W.dim() != 2 or x.shape[-1] != W.shape[0]:
+        raise ValueError(f"x [..., D] and W [D, V] do not fit: {tuple(x.shape)}, {tuple(W.shape)}")
+    _check_tensor("x", x, x.dtype, x.device)
+    _check_tensor("W", W, x.dtype, x.device)
+    D, V = W.shape
+    if b is not None:
+        _check_tensor("b", b, torch.float32, x.device, (V,))
+    _check_tensor("labels", labels, torch.int32, x.device, x.shape[:-1])
+    return RnntCeDesc(labels.numel(), D, V, code, int(ignore_label), int(accumulate), int(param_grads_bf16))
+
+
+def run_ce_fwd(x, W, b, labels, ignore_label=-1, workspace: Optional[Workspace] = None, budget_bytes: int = 0, stream=None):
+    """Cross entropy of softmax(x W + b) per row: x [..., D], W [D, V] (bfloat16 or float32), b [V] float32 or None, labels [...] int32 (rows with
+    ignore_label are padding).  Returns dict(loss) of the labels' shape, float32."""
+    import torch
+    desc = _check_ce(x, W, b, labels, ignore_label, 0, 0)
+    with _CallOn(x.device, stream):
+        loss = torch.empty(labels.shape, dtype=torch.float32, device=x.device)
+        ws = _layer_workspace(workspace, rnnt_ce_loss_workspace_bytes(desc, False, budget_bytes), x.device)
+        st = rnnt_ce_loss_fwd(desc, _aligned(x), _aligned(W), _aligned(b), labels, loss, ws)
+    if st != 0:
+        raise RnntError(st, "rnnt_ce_loss_fwd")
+    return dict(loss=loss)
+
+
+def run_ce_fwd_bwd(x, W, b, labels, row_weight=None, ignore_label=-1, accumulate_into=None, param_grads_bf16=0,
+                   workspace: Optional[Workspace] = None, budget_bytes: int = 0, stream=None):
+    """run_ce_fwd and the gradients of sum(row_weight * loss) (row_weight [...] float32, None: ones).  accumulate_into: (dW, db) float32 to add to;
+    param_grads_bf16: the descriptor's field.  Returns dict(loss, dx, dW, db)."""
+    import torch
+    desc = _check_ce(x, W, b, labels, ignore_label, accumulate_into is not None, param_grads_bf16)
+    if row_weight is not None:
+        _check_tensor("row_weight", row_weight, torch.float32, x.device, labels.shape)
+    with _CallOn(x.device, stream):
+        loss = torch.empty(labels.shape, dtype=torch.float32, device=x.device)
+        dx = torch.empty_like(x)
+        if accumulate_into is not None:
+            dW, db = accumulate_into
+            for name, t, s in (("dW", dW, (desc.D, desc.V)), ("db", db, (desc.V,))):
+                if t is not None:
+                    _check_tensor(name, t, torch.float32, x.device, s)
+        else:
+            kind = [torch.bfloat16 if desc.param_grads_bf16 >> bit & 1 else torch.float32 for bit in (0, 1)]
+            dW = torch.empty(desc.D, desc.V, dtype=kind[0], device=x.device)
+            db = torch.empty(desc.V, dtype=kind[1], device=x.device)
+        ws = _layer_workspace(workspace, rnnt_ce_loss_workspace_bytes(desc, True, budget_bytes), x.device)
+        st = rnnt_ce_loss_fwd_bwd(desc, _aligned(x), _aligned(W), _aligned(b), labels, row_weight, loss, dx, dW, db, ws)
+    if st != 0:
+        raise RnntError(st, "rnnt_ce_loss_fwd_bwd")
+    return dict(loss=loss, dx=dx, dW=dW, db=db)

@@ -141,13 +141,13 @@ hipError_t timed(int cls, hipStream_t stream, F&& launch) {
 // What the last failed HIP call was (process-wide, for rnnt_last_hip_error).
 hipError_t g_last_hip_error = hipSuccess;
 int g_last_hip_line = 0;
+const char* g_last_hip_file = "api.cpp";
 
 #define RNNT_HIP(expr)                           \
     do {                                         \
         const hipError_t rnnt_e_ = (expr);       \
         if (rnnt_e_ != hipSuccess) {             \
-            g_last_hip_error = rnnt_e_;          \
-            g_last_hip_line = __LINE__;          \
+            note_hip_error(rnnt_e_, "api.cpp", __LINE__); \
             (void)hipGetLastError();             \
             return RNNT_ERR_HIP;                 \
         }                                        \
@@ -910,11 +910,17 @@ extern "C" rnnt_status rnnt_debug_mfma_loop_fp8(const void* frags, float* out, i
     return RNNT_OK;
 }
 
+void rnnt::note_hip_error(hipError_t e, const char* file, int line) {
+    g_last_hip_error = e;
+    g_last_hip_line = line;
+    g_last_hip_file = file;
+}
+
 extern "C" const char* rnnt_last_hip_error(void) {
     static char text[160];
     if (g_last_hip_error == hipSuccess) return "";
-    snprintf(text, sizeof text, "%s (%s) at api.cpp:%d", hipGetErrorName(g_last_hip_error),
-             hipGetErrorString(g_last_hip_error), g_last_hip_line);
+    snprintf(text, sizeof text, "%s (%s) at %s:%d", hipGetErrorName(g_last_hip_error),
+             hipGetErrorString(g_last_hip_error), g_last_hip_file, g_last_hip_line);
     return text;
 }
 

@@ -1,0 +1,251 @@
+// bf16 matrix products of the layers beside the transducer loss (device code): C[m, n] = sum_k A(m, k) B(k, n), one output tile per workgroup, what
+// becomes of a result is up to an epilogue that is handed eight consecutive columns of a row.
+#pragma once
+#include "device_common.h"
+#include "layers.h"
+
+namespace rnnt {
+
+namespace {
+
+// An operand lies in memory either with k contiguous (KC: element (i, k) at p[i * ld + k]) or with k slow (KS: at p[k * ld + i]); its rows are 16-byte
+// aligned.  A stage is 64 of k:
+//   KC: [row][64 k], 128 bytes per row, so a copy instruction takes eight whole cache lines; 16-byte granule g of row r lies at place g ^ (r % 8), which
+//       spreads the 32 rows of an MFMA fragment's 16-byte reads over all banks;
+//   KS: [k][R columns], granule c of row k at place c ^ 4 (k % 4) (conflict-free for the transposing LDS reads that turn it into fragments).
+// The copies go global -> LDS without registers.  Rows (KC) or columns (KS) beyond n_i read the last ones again: their results are not
+// stored.  Beyond the last k there are zeros: K is a multiple of 64 for KC; the last stage of a KS operand whose K is none is taken from `tail`, 64 rows
+// that end in zeros.
+constexpr int GK = 64;
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x8_t __attribute__((ext_vector_type(8)));
+
+template <int R, bool KS, int WAVES>
+struct TileLoader {
+    static constexpr int BYTES = R * GK * 2;
+    static constexpr int PW = BYTES / 1024 / WAVES;               // copies per wave and stage
+    static constexpr int KR = KS ? 512 / R : 0;                   // rows of k per copy
+    static constexpr int NV = KS ? (KR == 2 ? 2 : 1) : PW;
+    static_assert(!KS || KR == 2 || KR == 4, "256 or 128 columns");
+    static_assert(PW % 2 == 0, "the places of two rows of k repeat every second copy");
+    const unsigned char* main;                                    // of this wave's first copy of stage 0
+    const unsigned char* tail;
+    long long step, ld;                                           // bytes
+    int last;                                                     // the stage that is read from `tail`, or -1
+    unsigned voff[NV];
+
+    __device__ __forceinline__ void init(const GemmOperand& o, long long i0, long long n_i, int wave, int lane) {
+        ld = o.ld * 2;
+        last = o.tail != nullptr ? o.tail_stage : -1;
+        if constexpr (KS) {
+            const int per = R / 8, slot = lane & (per - 1);
+            main = (const unsigned char*)o.p + i0 * 2 + (long long)(wave * PW * KR) * ld;
+            tail = (const unsigned char*)o.tail + i0 * 2 + (long long)(wave * PW * KR) * ld;
+            step = GK * ld;
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int dk = lane / per, k = v * KR + dk;
+                long long col = i0 + (slot ^ (4 * (k & 3))) * 8;
+                col = col < n_i - 8 ? col : n_i - 8;
+                voff[v] = (unsigned)(dk * ld + (col - i0) * 2);
+            }
+        } else {
+            main = (const unsigned char*)o.p + i0 * ld;
+            tail = nullptr;
+            step = GK * 2;
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                long long r = i0 + (wave * PW + v) * 8 + (lane >> 3);
+                r = r < n_i ? r : n_i - 1;
+                voff[v] = (unsigned)((r - i0) * ld + ((lane & 7) ^ (lane >> 3)) * 16);
+            }
+        }
+    }
+    // copy t of stage `st` into the operand's LDS area at lds (of this wave's first copy)
+    template <int T>
+    __device__ __forceinline__ void copy(const unsigned char* st, unsigned lds) const {
+        if constexpr (KS) lds_dma16_s(st + (long long)(T * KR) * ld, voff[T % NV], lds + T * 1024);
+        else lds_dma16_s(st, voff[T], lds + T * 1024);
+    }
+    __device__ __forceinline__ const unsigned char* stage(int s) const {
+        const unsigned char* p = KS && s == last ? tail : main + s * step;
+        // (uniform, and said so: the copies take it in scalar registers)
+        const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)(size_t)p), hi = __builtin_amdgcn_readfirstlane((unsigned)((size_t)p >> 32));
+        size_t u = ((size_t)hi << 32) | lo;
+        // (five wait states between a vector instruction that writes a scalar register and the memory instruction that reads it, which the compiler does
+        // not add inside assembler text)
+        asm volatile("s_nop 4" : "+s"(u));
+        return (const unsigned char*)u;
+    }
+};
+
+// Fragments of one operand, B blocks of 32 rows from i_base (a multiple of 32) on: lane l holds row l % 32, k = 8 (l / 32) .. + 7 of a k16-step.
+template <int R, bool KS, int B>
+struct TileReader {
+    unsigned a[KS ? B : 4];
+    __device__ __forceinline__ void init(int i_base, int lane) {
+        if constexpr (KS) {
+            // transposing read: within 16 lanes, lane 4 j + c supplies 4 columns of row j and lane i receives rows 0..3 of column i
+            const int fg = lane >> 4, fj = (lane >> 2) & 3, fc = lane & 3;
+#pragma unroll
+            for (int b = 0; b < B; ++b) {
+                const int col = i_base + 32 * b + 16 * (fg & 1) + 4 * fc;
+                a[b] = (unsigned)((8 * (fg >> 1) + fj) * R * 2 + (((col >> 3) ^ (fj << 2)) << 4) + (col & 7) * 2);
+            }
+        } else {
+            const int l32 = lane & 31, hb = lane >> 5;
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) a[kk] = (unsigned)((i_base + l32) * 128 + (((2 * kk + hb) ^ (l32 & 7)) << 4));
+        }
+    }
+    template <int KK, int BLK>
+    __device__ __forceinline__ bf16x8 read(const unsigned char* tile) const {
+        if constexpr (KS) {
+            const unsigned char* p = tile + a[BLK] + KK * 16 * R * 2;
+            const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(p));
+            const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(p + 4 * R * 2));
+            const s16x8_t v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            return __builtin_bit_cast(bf16x8, v);
+        } else {
+            return *reinterpret_cast<const bf16x8*>(tile + a[KK] + BLK * 32 * 128);
+        }
+    }
+};
+
+// Tile shapes: 256 x 256 with 8 waves (2 x 4, each 128 x 64), one workgroup per compute unit; 128 x 128 with 4 waves (2 x 2, each 64 x 64), two of them.
+template <int BM_>
+struct TileShape {
+    static constexpr int BM = BM_, BN = BM_, WM = 2, WN = BM_ / 64, WAVES = WM * WN, THREADS = 64 * WAVES;
+    static constexpr int MT = BM / WM / 32, NT = 2;
+    static constexpr unsigned A_BYTES = BM * GK * 2, STAGE = 2 * A_BYTES;
+    static constexpr unsigned SMEM = 2 * STAGE;
+};
+
+// acc[i][j] += the tile's product over the stages [s0, s1): block of 32 rows i of the wave's part, block of 32 columns j.  The matrix instruction takes B's
+// fragment first, so lane l holds row l % 32 and register 4 q + r column 8 q + 4 (l / 32) + r.
+// Two stages of LDS.  A stage's four k16-steps: the fragments of the next step are read behind the MFMAs of the present one.  Before the fourth every wave
+// has read all it needs of the stage and the next one has landed: one barrier, then the copies of the stage after the next go out into the buffer that has
+// become free, and have three k16-steps and more until they are waited for.
+template <class TS, bool AKS, bool BKS>
+__device__ __forceinline__ void gemm_tile(f32x16 (&acc)[TS::MT][TS::NT], const GemmOperand& ga, const GemmOperand& gb, long long m0, long long n0,
+                                          long long M, long long N, int s0, int s1, unsigned char* smem) {
+    constexpr int MT = TS::MT, NT = TS::NT;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const int wm = wave / TS::WN, wn = wave % TS::WN;
+    typedef TileLoader<TS::BM, AKS, TS::WAVES> LA;
+    typedef TileLoader<TS::BN, BKS, TS::WAVES> LB;
+    LA la;
+    LB lb;
+    la.init(ga, m0, M, wave, lane);
+    lb.init(gb, n0, N, wave, lane);
+    TileReader<TS::BM, AKS, MT> ra;
+    TileReader<TS::BN, BKS, NT> rb;
+    ra.init(wm * MT * 32, lane);
+    rb.init(wn * NT * 32, lane);
+    const unsigned base = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem;
+    const unsigned dst_a = base + (unsigned)(wave * LA::PW) * 1024u, dst_b = base + TS::A_BYTES + (unsigned)(wave * LB::PW) * 1024u;
+
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = f32x16{0};
+    if (s0 >= s1) return;
+    auto issue = [&](int s, unsigned buf) {
+        const unsigned char *pa = la.stage(s), *pb = lb.stage(s);
+        static_for<0, LA::PW>([&](auto t) { la.template copy<decltype(t)::value>(pa, dst_a + buf); });
+        static_for<0, LB::PW>([&](auto t) { lb.template copy<decltype(t)::value>(pb, dst_b + buf); });
+    };
+    bf16x8 fa[2][MT], fb[2][NT];
+    issue(s0, 0u);
+    issue(s0 + 1 < s1 ? s0 + 1 : s1 - 1, TS::STAGE);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LA::PW + LB::PW) : "memory");
+    __syncthreads();
+    static_for<0, MT>([&](auto i) { fa[0][decltype(i)::value] = ra.template read<0, decltype(i)::value>(smem); });
+    static_for<0, NT>([&](auto j) { fb[0][decltype(j)::value] = rb.template read<0, decltype(j)::value>(smem + TS::A_BYTES); });
+
+    // the MFMAs of k16-step KK (register set KK % 2); behind them the fragments of the next one are read, and in the last the copies are sent
+    auto multiply = [&](auto kk_tag, const unsigned char* next_tile, int dma_stage, unsigned dma_buf) {
+        constexpr int KK = decltype(kk_tag)::value, set = KK & 1, next = (KK + 1) & 3;
+        const unsigned char *pa = nullptr, *pb = nullptr;
+        if constexpr (KK == 3) {
+            pa = la.stage(dma_stage);
+            pb = lb.stage(dma_stage);
+        }
+        static_for<0, MT * NT>([&](auto idx_tag) {
+            constexpr int idx = decltype(idx_tag)::value, i = idx / NT, j = idx % NT, G = MT * NT;
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[set][j], fa[set][i], acc[i][j], 0, 0, 0);
+            // fragments idx * F / G .. of the F = MT + NT of the next step
+            constexpr int F = MT + NT, f0 = G >= F ? idx : idx * F / G, f1 = G >= F ? idx + 1 : (idx + 1) * F / G;
+            static_for<f0, (f1 < F ? f1 : F)>([&](auto f_tag) {
+                constexpr int f = decltype(f_tag)::value;
+                if constexpr (f < NT) fb[set ^ 1][f] = rb.template read<next, f>(next_tile + TS::A_BYTES);
+                else fa[set ^ 1][f - NT] = ra.template read<next, f - NT>(next_tile);
+            });
+            if constexpr (KK == 3) {
+                constexpr int D = LA::PW + LB::PW, d0 = idx * D / G, d1 = (idx + 1) * D / G;
+                static_for<d0, d1>([&](auto d_tag) {
+                    constexpr int d = decltype(d_tag)::value;
+                    if constexpr (d < LA::PW) la.template copy<d>(pa, dst_a + dma_buf);
+                    else lb.template copy<d - LA::PW>(pb, dst_b + dma_buf);
+                });
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+    unsigned cur = 0;
+    for (int s = s0; s < s1; ++s) {
+        const unsigned char* tile = smem + cur;
+        __builtin_amdgcn_s_waitcnt(WAIT_LGKM0);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(std::integral_constant<int, 0>{}, tile, 0, 0u);
+        __builtin_amdgcn_s_waitcnt(WAIT_LGKM0);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(std::integral_constant<int, 1>{}, tile, 0, 0u);
+        __builtin_amdgcn_s_waitcnt(WAIT_LGKM0);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(std::integral_constant<int, 2>{}, tile, 0, 0u);
+        __builtin_amdgcn_s_waitcnt(WAIT_LGKM0);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");          // the next stage has landed
+        __syncthreads();
+        __builtin_amdgcn_sched_barrier(0);
+        // (past the end: the last stage again, into a buffer nobody reads any more)
+        multiply(std::integral_constant<int, 3>{}, smem + (cur ^ TS::STAGE), s + 2 < s1 ? s + 2 : s1 - 1, cur);
+        cur ^= TS::STAGE;
+    }
+    __builtin_amdgcn_s_waitcnt(WAIT_LGKM0);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");              // no copy may land after this: the epilogue uses LDS
+    __syncthreads();
+}
+
+// Eight columns of the lane's row: granule p of block j of accumulator d, columns 16 p + 8 (l / 32) .. + 7 of the block
+__device__ __forceinline__ void granule8(const f32x16& d, int p, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        unsigned x = __float_as_uint(d[8 * p + i]), y = __float_as_uint(d[8 * p + 4 + i]);
+        swap_halves(x, y);
+        v[i] = __uint_as_float(x);
+        v[4 + i] = __uint_as_float(y);
+    }
+}
+
+// Workgroup L -> (split, tile row, tile column).  Workgroups are dealt round-robin to the 8 XCDs, each with its own L2: an XCD takes a contiguous range of
+// the tiles, in an order that walks blocks of eight tile columns row by row, so that its 32 compute units share rows of A and columns of B.
+struct TilePlace {
+    int split, m, n;
+};
+__device__ __forceinline__ bool place_tile(int L, int mt, int nt, int splits, TilePlace& t) {
+    const int tiles = mt * nt, total = tiles * splits, per = (total + 7) >> 3;
+    const int w = (L & 7) * per + (L >> 3);
+    if ((L >> 3) >= per || w >= total) return false;
+    constexpr int GN = 8;
+    t.split = w / tiles;
+    const int r = w - t.split * tiles, blk = r / (mt * GN), in = r - blk * mt * GN;
+    const int nb = nt - blk * GN < GN ? nt - blk * GN : GN;
+    t.m = in / nb;
+    t.n = blk * GN + in % nb;
+    return true;
+}
+
+}  // namespace
+
+}  // namespace rnnt

@@ -97,6 +97,8 @@ struct PrepArgs {
 };
 constexpr int PREP_TABLE_MAX = 800;
 hipError_t launch_prepare(const PrepArgs& a, hipStream_t stream);
+// What rnnt_last_hip_error reports from now on
+void note_hip_error(hipError_t e, const char* file, int line);
 // dst[i] = bf16(src[i]), n a multiple of 8 (the gradients of a group, accumulated in fp32, on their way out)
 hipError_t launch_f32_to_bf16(const float* src, void* dst, size_t n, hipStream_t stream);
 // plain copy of n floats (n a multiple of 4): the known-size kernel the HBM counters are calibrated with
