@@ -9,8 +9,7 @@
  * Conventions beyond those of rnnt_joint_loss.h: every array is dense; device pointers are 16-byte aligned (RNNT_ERR_UNSUPPORTED otherwise),
  * workspaces 256-byte aligned.  Every call can be recorded into a HIP graph: all it needs is in its arguments and in device memory, it allocates
  * nothing and copies nothing from the host.  Workspaces hold nothing between calls; calls that share one must be ordered (two graphs that may run
- * side by side need two).  With RNNT_BF16 results are summed in a fixed order (equal bits from run to run); with RNNT_F32 the
- * weight gradients are added to with float atomics and can differ in the last bits.
+ * side by side need two).  All sums have a fixed order: equal inputs give equal bits.
  */
 #ifndef RNNT_LAYERS_H
 #define RNNT_LAYERS_H
@@ -114,6 +113,15 @@ rnnt_status rnnt_ce_loss_fwd(const rnnt_ce_desc* desc, const void* x, const void
 rnnt_status rnnt_ce_loss_fwd_bwd(const rnnt_ce_desc* desc, const void* x, const void* W, const float* b, const int32_t* label,
                                  const float* row_weight, float* loss, void* dx, void* dW, void* db, void* workspace, size_t workspace_bytes,
                                  void* hip_stream);
+
+/*
+ * total (dev, float, out) = sum over the rows of row_weight[r] loss[r], without the rows of weight 0 (whose loss may be infinite); row_weight NULL: ones.
+ */
+rnnt_status rnnt_ce_loss_total(const rnnt_ce_desc* desc, const float* loss, const float* row_weight, float* total, void* hip_stream);
+/*
+ * dx, dW, db (each may be NULL) of rnnt_ce_loss_fwd_bwd times *factor (dev, read by the kernel), in place; a factor of 1 moves no data.
+ */
+rnnt_status rnnt_ce_loss_scale(const rnnt_ce_desc* desc, const float* factor, void* dx, void* dW, void* db, void* hip_stream);
 
 #ifdef __cplusplus
 }

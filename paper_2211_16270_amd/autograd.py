@@ -105,28 +105,36 @@ def rnnt_linear(x, W, b=None, activation="none", residual=None, dropout: float =
     return _RnntLinear.apply(x, W, b, activation, residual, float(dropout), rng_state)
 
 
+def _ce_grads(x, W, b, labels, row_weight, ignore_label, budget_bytes):
+    bits = 0 if W.dtype == torch.float32 else 1 | (2 if b is not None and b.dtype == torch.bfloat16 else 0)
+    return Bd.run_ce_fwd_bwd(x, W, None if b is None else b.float(), labels, row_weight, ignore_label, param_grads_bf16=bits, budget_bytes=budget_bytes)
+
+
 class _RnntCeSum(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, W, b, labels, row_weight, ignore_label, budget_bytes):
-        if not any(ctx.needs_input_grad[:3]):
-            loss = Bd.run_ce_fwd(x, W, None if b is None else b.float(), labels, ignore_label, budget_bytes=budget_bytes)["loss"]
+        if any(ctx.needs_input_grad[:3]):
+            out = _ce_grads(x, W, b, labels, row_weight, ignore_label, budget_bytes)
+            ctx.save_for_backward(x, W, b, labels, row_weight)
+            ctx.grads, ctx.opts = out, (ignore_label, budget_bytes)
         else:
-            bf16 = 0 if W.dtype == torch.float32 else 1 | (2 if b is not None and b.dtype == torch.bfloat16 else 0)
-            out = Bd.run_ce_fwd_bwd(x, W, None if b is None else b.float(), labels, row_weight, ignore_label, param_grads_bf16=bf16,
-                                    budget_bytes=budget_bytes)
-            loss = out["loss"]
-            ctx.save_for_backward(out["dx"], out["dW"], out["db"])
-            ctx.b_dtype = None if b is None else b.dtype
-        # (a row of weight 0 counts for nothing, whatever its loss is)
-        return loss.sum() if row_weight is None else torch.where(row_weight == 0, 0.0, loss * row_weight).sum()
+            out = Bd.run_ce_fwd(x, W, None if b is None else b.float(), labels, ignore_label, budget_bytes=budget_bytes)
+        return Bd.run_ce_total(out["loss"], row_weight)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, g):
-        dx, dW, db = ctx.saved_tensors
+        x, W, b, labels, row_weight = ctx.saved_tensors
+        g = g.float().contiguous()
+        if ctx.grads is not None:
+            # the forward call's gradients are handed out, times g in place; a second backward pass of the same graph computes them again
+            out, ctx.grads = ctx.grads, None
+            Bd.run_ce_scale(g, out["dx"], out["dW"], out["db"])
+        else:
+            w = g.expand(labels.shape).contiguous() if row_weight is None else row_weight * g
+            out = _ce_grads(x, W, b, labels, w, *ctx.opts)
         need = ctx.needs_input_grad
-        return ((dx * g).to(dx.dtype) if need[0] else None, (dW * g).to(dW.dtype) if need[1] else None,
-                (db * g).to(ctx.b_dtype) if need[2] else None, None, None, None, None)
+        return (out["dx"] if need[0] else None, out["dW"] if need[1] else None, out["db"].to(b.dtype) if need[2] else None, None, None, None, None)
 
 
 class _RnntCeRows(torch.autograd.Function):
@@ -141,9 +149,7 @@ class _RnntCeRows(torch.autograd.Function):
     def backward(ctx, g):
         x, W, b, labels = ctx.saved_tensors
         need = ctx.needs_input_grad
-        bf16 = 0 if W.dtype == torch.float32 else 1 | (2 if b is not None and b.dtype == torch.bfloat16 else 0)
-        out = Bd.run_ce_fwd_bwd(x, W, None if b is None else b.float(), labels, g.contiguous().float(), ctx.opts[0], param_grads_bf16=bf16,
-                                budget_bytes=ctx.opts[1])
+        out = _ce_grads(x, W, b, labels, g.float().contiguous(), *ctx.opts)
         return (out["dx"] if need[0] else None, out["dW"] if need[1] else None, out["db"].to(b.dtype) if b is not None and need[2] else None,
                 None, None, None)
 

@@ -27,7 +27,7 @@ EXPORTS = ["rnnt_status_string", "rnnt_last_hip_error", "rnnt_joint_loss_workspa
            "rnnt_plan_destroy", "rnnt_joint_loss_fwd_bwd_planned", "rnnt_debug_read_active_tiles"]
 # include/rnnt_layers.h
 LAYER_EXPORTS = ["rnnt_linear_workspace_bytes", "rnnt_linear_fwd", "rnnt_linear_bwd", "rnnt_ce_loss_workspace_bytes", "rnnt_ce_loss_fwd",
-                 "rnnt_ce_loss_fwd_bwd"]
+                 "rnnt_ce_loss_fwd_bwd", "rnnt_ce_loss_total", "rnnt_ce_loss_scale"]
 ACTIVATIONS = ["none", "relu", "silu", "gelu", "tanh"]          # rnnt_activation
 RNNT_STATIC_SCRATCH_BYTES = 128 << 20
 
@@ -160,6 +160,10 @@ def lib() -> ctypes.CDLL:
     L.rnnt_ce_loss_workspace_bytes.argtypes = [cp, ctypes.c_int32, ctypes.c_size_t]
     L.rnnt_ce_loss_fwd.restype = ctypes.c_int
     L.rnnt_ce_loss_fwd.argtypes = [cp] + [vp] * 6 + [ctypes.c_size_t, vp]
+    L.rnnt_ce_loss_total.restype = ctypes.c_int
+    L.rnnt_ce_loss_total.argtypes = [cp] + [vp] * 4
+    L.rnnt_ce_loss_scale.restype = ctypes.c_int
+    L.rnnt_ce_loss_scale.argtypes = [cp] + [vp] * 5
     L.rnnt_ce_loss_fwd_bwd.restype = ctypes.c_int
     L.rnnt_ce_loss_fwd_bwd.argtypes = [cp] + [vp] * 10 + [ctypes.c_size_t, vp]
     _lib = L
@@ -542,6 +546,14 @@ def rnnt_ce_loss_fwd_bwd(desc: RnntCeDesc, x, W, b, label, row_weight, loss, dx,
                                           _ptr(dW), _ptr(db), _ptr(workspace), _nbytes(workspace), _stream_handle(stream)))
 
 
+def rnnt_ce_loss_total(desc: RnntCeDesc, loss, row_weight, total, stream=None) -> int:
+    return int(lib().rnnt_ce_loss_total(ctypes.byref(desc), _ptr(loss), _ptr(row_weight), _ptr(total), _stream_handle(stream)))
+
+
+def rnnt_ce_loss_scale(desc: RnntCeDesc, factor, dx, dW, db, stream=None) -> int:
+    return int(lib().rnnt_ce_loss_scale(ctypes.byref(desc), _ptr(factor), _ptr(dx), _ptr(dW), _ptr(db), _stream_handle(stream)))
+
+
 def _check_tensor(name, t, dtype, device, shape=None):
     if t.device != device or t.dtype != dtype or not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
         raise ValueError(f"{name}: expected a contiguous {dtype} tensor on {device}"
@@ -720,3 +732,30 @@ def run_ce_fwd_bwd(x, W, b, labels, row_weight=None, ignore_label=-1, accumulate
     if st != 0:
         raise RnntError(st, "rnnt_ce_loss_fwd_bwd")
     return dict(loss=loss, dx=dx, dW=dW, db=db)
+
+
+def run_ce_total(loss, row_weight=None, stream=None):
+    """sum(row_weight * loss) without the rows of weight 0, as a float32 scalar on the device."""
+    import torch
+    _check_tensor("loss", loss, torch.float32, loss.device)
+    if row_weight is not None:
+        _check_tensor("row_weight", row_weight, torch.float32, loss.device, loss.shape)
+    with _CallOn(loss.device, stream):
+        total = torch.empty((), dtype=torch.float32, device=loss.device)
+        st = rnnt_ce_loss_total(RnntCeDesc(loss.numel(), 1, 1, RNNT_F32, -1, 0, 0), loss, row_weight, total)
+    if st != 0:
+        raise RnntError(st, "rnnt_ce_loss_total")
+    return total
+
+
+def run_ce_scale(factor, dx, dW, db=None, stream=None):
+    """The gradients of run_ce_fwd_bwd times the scalar float32 tensor `factor`, in place (nothing is moved where it is 1)."""
+    import torch
+    _check_tensor("factor", factor, torch.float32, dx.device)
+    D, V = dW.shape
+    code = RNNT_BF16 if dx.dtype == torch.bfloat16 else RNNT_F32
+    bits = int(dW.dtype == torch.bfloat16) | (2 if db is not None and db.dtype == torch.bfloat16 else 0)
+    with _CallOn(dx.device, stream):
+        st = rnnt_ce_loss_scale(RnntCeDesc(dx.numel() // D, D, V, code, -1, 0, bits), factor, dx, dW, db)
+    if st != 0:
+        raise RnntError(st, "rnnt_ce_loss_scale")

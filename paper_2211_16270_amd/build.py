@@ -13,7 +13,7 @@ LIB_PATH = os.path.join(LIB_DIR, "librnnt_joint_loss.so")
 OBJ_DIR = os.path.join(PKG_DIR, "_build")
 
 SOURCES = ["api.cpp", "plan.cpp", "kernels_prep.hip", "kernels_f32.hip", "kernels_lattice.hip", "kernels_select.hip", "kernels_bf16.hip", "kernels_bf16_scores.hip", "kernels_bf16_dz.hip", "kernels_proj.hip", "kernels_probe.hip",
-           "layers.cpp", "kernels_layers_gemm.hip", "kernels_layers_rows.hip"]
+           "layers.cpp", "kernels_layers_gemm.hip", "kernels_layers_rows.hip", "kernels_layers_few.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 DEVICE_FLAGS = [

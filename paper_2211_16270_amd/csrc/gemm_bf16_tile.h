@@ -117,15 +117,18 @@ template <int BM_>
 struct TileShape {
     static constexpr int BM = BM_, BN = BM_, WM = 2, WN = BM_ / 64, WAVES = WM * WN, THREADS = 64 * WAVES;
     static constexpr int MT = BM / WM / 32, NT = 2;
-    static constexpr unsigned A_BYTES = BM * GK * 2, STAGE = 2 * A_BYTES;
-    static constexpr unsigned SMEM = 2 * STAGE;
+    static constexpr unsigned OPER = BM * GK * 2;                 // bytes of one operand's stage
+    static constexpr unsigned SMEM = 5 * OPER;                    // three of A's, two of B's
+    static constexpr unsigned B_AT = 3 * OPER;
 };
 
-// acc[i][j] += the tile's product over the stages [s0, s1): block of 32 rows i of the wave's part, block of 32 columns j.  The matrix instruction takes B's
+// acc[i][j] = the tile's product over the stages [s0, s1): block of 32 rows i of the wave's part, block of 32 columns j.  The matrix instruction takes B's
 // fragment first, so lane l holds row l % 32 and register 4 q + r column 8 q + 4 (l / 32) + r.
-// Two stages of LDS.  A stage's four k16-steps: the fragments of the next step are read behind the MFMAs of the present one.  Before the fourth every wave
-// has read all it needs of the stage and the next one has landed: one barrier, then the copies of the stage after the next go out into the buffer that has
-// become free, and have three k16-steps and more until they are waited for.
+// LDS holds three stages of A and two of B.  A stage is four k16-steps; the fragments of the next step are read behind the MFMAs of the present one.
+// Before the fourth every wave has read all it needs of the stage and the next one has landed: one barrier per stage.  The copies of A two stages ahead
+// go out in the first two steps (their buffer became free a stage ago), those of B in the fourth, into the buffer that has just become free.  (Two stages of
+// both, all copies in the fourth step: 8192^3 1250 to 1280 TFLOP/s, now 1335; without any copies 1470 to 1510.  The rest of the loss is the prologue and
+// the epilogue, which nothing hides: K = 1024 940 TFLOP/s.)  A wave has priority while it sends MFMAs (K = 1024: 874 without).
 template <class TS, bool AKS, bool BKS>
 __device__ __forceinline__ void gemm_tile(f32x16 (&acc)[TS::MT][TS::NT], const GemmOperand& ga, const GemmOperand& gb, long long m0, long long n0,
                                           long long M, long long N, int s0, int s1, unsigned char* smem) {
@@ -143,89 +146,117 @@ __device__ __forceinline__ void gemm_tile(f32x16 (&acc)[TS::MT][TS::NT], const G
     ra.init(wm * MT * 32, lane);
     rb.init(wn * NT * 32, lane);
     const unsigned base = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem;
-    const unsigned dst_a = base + (unsigned)(wave * LA::PW) * 1024u, dst_b = base + TS::A_BYTES + (unsigned)(wave * LB::PW) * 1024u;
+    const unsigned dst_a = base + (unsigned)(wave * LA::PW) * 1024u, dst_b = base + TS::B_AT + (unsigned)(wave * LB::PW) * 1024u;
 
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[i][j] = f32x16{0};
     if (s0 >= s1) return;
-    auto issue = [&](int s, unsigned buf) {
-        const unsigned char *pa = la.stage(s), *pb = lb.stage(s);
-        static_for<0, LA::PW>([&](auto t) { la.template copy<decltype(t)::value>(pa, dst_a + buf); });
-        static_for<0, LB::PW>([&](auto t) { lb.template copy<decltype(t)::value>(pb, dst_b + buf); });
+    const int last = s1 - 1;
+    auto issue_a = [&](int s, unsigned buf) {
+        const unsigned char* p = la.stage(s);
+        static_for<0, LA::PW>([&](auto t) { la.template copy<decltype(t)::value>(p, dst_a + buf); });
+    };
+    auto issue_b = [&](int s, unsigned buf) {
+        const unsigned char* p = lb.stage(s);
+        static_for<0, LB::PW>([&](auto t) { lb.template copy<decltype(t)::value>(p, dst_b + buf); });
     };
     bf16x8 fa[2][MT], fb[2][NT];
-    issue(s0, 0u);
-    issue(s0 + 1 < s1 ? s0 + 1 : s1 - 1, TS::STAGE);
+    issue_a(s0, 0u);
+    issue_b(s0, 0u);
+    issue_a(s0 < last ? s0 + 1 : last, TS::OPER);
+    issue_b(s0 < last ? s0 + 1 : last, TS::OPER);
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LA::PW + LB::PW) : "memory");
     __syncthreads();
     static_for<0, MT>([&](auto i) { fa[0][decltype(i)::value] = ra.template read<0, decltype(i)::value>(smem); });
-    static_for<0, NT>([&](auto j) { fb[0][decltype(j)::value] = rb.template read<0, decltype(j)::value>(smem + TS::A_BYTES); });
+    static_for<0, NT>([&](auto j) { fb[0][decltype(j)::value] = rb.template read<0, decltype(j)::value>(smem + TS::B_AT); });
 
-    // the MFMAs of k16-step KK (register set KK % 2); behind them the fragments of the next one are read, and in the last the copies are sent
-    auto multiply = [&](auto kk_tag, const unsigned char* next_tile, int dma_stage, unsigned dma_buf) {
+    // the MFMAs of k16-step KK (register set KK % 2); behind them the fragments of the next one are read (at pa, pb) and copies are sent
+    auto multiply = [&](auto kk_tag, const unsigned char* pa, const unsigned char* pb, int dma_stage, unsigned dma_buf) {
         constexpr int KK = decltype(kk_tag)::value, set = KK & 1, next = (KK + 1) & 3;
-        const unsigned char *pa = nullptr, *pb = nullptr;
-        if constexpr (KK == 3) {
-            pa = la.stage(dma_stage);
-            pb = lb.stage(dma_stage);
-        }
+        const unsigned char* src = nullptr;
+        if constexpr (KK == 0 || KK == 1) src = la.stage(dma_stage);
+        if constexpr (KK == 3) src = lb.stage(dma_stage);
         static_for<0, MT * NT>([&](auto idx_tag) {
             constexpr int idx = decltype(idx_tag)::value, i = idx / NT, j = idx % NT, G = MT * NT;
+            if constexpr (idx == 0) __builtin_amdgcn_s_setprio(1);
             acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[set][j], fa[set][i], acc[i][j], 0, 0, 0);
             // fragments idx * F / G .. of the F = MT + NT of the next step
             constexpr int F = MT + NT, f0 = G >= F ? idx : idx * F / G, f1 = G >= F ? idx + 1 : (idx + 1) * F / G;
             static_for<f0, (f1 < F ? f1 : F)>([&](auto f_tag) {
                 constexpr int f = decltype(f_tag)::value;
-                if constexpr (f < NT) fb[set ^ 1][f] = rb.template read<next, f>(next_tile + TS::A_BYTES);
-                else fa[set ^ 1][f - NT] = ra.template read<next, f - NT>(next_tile);
+                if constexpr (f < NT) fb[set ^ 1][f] = rb.template read<next, f>(pb);
+                else fa[set ^ 1][f - NT] = ra.template read<next, f - NT>(pa);
             });
-            if constexpr (KK == 3) {
-                constexpr int D = LA::PW + LB::PW, d0 = idx * D / G, d1 = (idx + 1) * D / G;
-                static_for<d0, d1>([&](auto d_tag) {
-                    constexpr int d = decltype(d_tag)::value;
-                    if constexpr (d < LA::PW) la.template copy<d>(pa, dst_a + dma_buf);
-                    else lb.template copy<d - LA::PW>(pb, dst_b + dma_buf);
-                });
+            if constexpr (KK == 0 || KK == 1) {
+                constexpr int D = LA::PW / 2, d0 = idx * D / G, d1 = (idx + 1) * D / G;
+                static_for<d0, d1>([&](auto d) { la.template copy<KK * D + decltype(d)::value>(src, dst_a + dma_buf); });
             }
+            if constexpr (KK == 3) {
+                constexpr int D = LB::PW, d0 = idx * D / G, d1 = (idx + 1) * D / G;
+                static_for<d0, d1>([&](auto d) { lb.template copy<decltype(d)::value>(src, dst_b + dma_buf); });
+            }
+            if constexpr (idx == G - 1) __builtin_amdgcn_s_setprio(0);
             __builtin_amdgcn_sched_barrier(0);
         });
     };
-    unsigned cur = 0;
+    unsigned a0 = 0, a1 = TS::OPER, a2 = 2 * TS::OPER, b0 = 0;    // A's buffers of this stage, the next, the one after; B's of this stage
     for (int s = s0; s < s1; ++s) {
-        const unsigned char* tile = smem + cur;
+        // (past the end: the last stage again, into buffers nobody reads any more)
+        const int ahead = s + 2 < s1 ? s + 2 : last;
+        const unsigned char *pa = smem + a0, *pb = smem + TS::B_AT + b0;
         __builtin_amdgcn_s_waitcnt(WAIT_LGKM0);
         __builtin_amdgcn_sched_barrier(0);
-        multiply(std::integral_constant<int, 0>{}, tile, 0, 0u);
+        multiply(std::integral_constant<int, 0>{}, pa, pb, ahead, a2);
         __builtin_amdgcn_s_waitcnt(WAIT_LGKM0);
         __builtin_amdgcn_sched_barrier(0);
-        multiply(std::integral_constant<int, 1>{}, tile, 0, 0u);
+        multiply(std::integral_constant<int, 1>{}, pa, pb, ahead, a2);
         __builtin_amdgcn_s_waitcnt(WAIT_LGKM0);
         __builtin_amdgcn_sched_barrier(0);
-        multiply(std::integral_constant<int, 2>{}, tile, 0, 0u);
+        multiply(std::integral_constant<int, 2>{}, pa, pb, 0, 0u);
         __builtin_amdgcn_s_waitcnt(WAIT_LGKM0);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");          // the next stage has landed
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LA::PW) : "memory");       // the next stage has landed; A's after that may be in flight
         __syncthreads();
         __builtin_amdgcn_sched_barrier(0);
-        // (past the end: the last stage again, into a buffer nobody reads any more)
-        multiply(std::integral_constant<int, 3>{}, smem + (cur ^ TS::STAGE), s + 2 < s1 ? s + 2 : s1 - 1, cur);
-        cur ^= TS::STAGE;
+        multiply(std::integral_constant<int, 3>{}, smem + a1, smem + TS::B_AT + (b0 ^ TS::OPER), ahead, b0);
+        const unsigned t = a0;
+        a0 = a1;
+        a1 = a2;
+        a2 = t;
+        b0 ^= TS::OPER;
     }
     __builtin_amdgcn_s_waitcnt(WAIT_LGKM0);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");              // no copy may land after this: the epilogue uses LDS
     __syncthreads();
 }
 
-// Eight columns of the lane's row: granule p of block j of accumulator d, columns 16 p + 8 (l / 32) .. + 7 of the block
-__device__ __forceinline__ void granule8(const f32x16& d, int p, float (&v)[8]) {
+// A 32 x 32 block of results through 4 KiB of LDS of the wave's own: lane l comes away with eight consecutive columns 8 (l % 4) .. + 7 of rows l / 4 and
+// 16 + l / 4, so that what follows touches 64 bytes of a row in one piece.  (16-byte pieces of a row at their place xor (row % 8): all banks.)
+constexpr unsigned TURN_BYTES = 4096;
+__device__ __forceinline__ void turn_block(const f32x16& d, unsigned char* area, int lane) {
+    const int row = lane & 31, hb = lane >> 5;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        unsigned x = __float_as_uint(d[8 * p + i]), y = __float_as_uint(d[8 * p + 4 + i]);
-        swap_halves(x, y);
-        v[i] = __uint_as_float(x);
-        v[4 + i] = __uint_as_float(y);
+    for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<f32x4*>(area + row * 128 + (((2 * q + hb) ^ (row & 7)) << 4)) = f32x4{d[4 * q], d[4 * q + 1], d[4 * q + 2], d[4 * q + 3]};
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+__device__ __forceinline__ void turned8(const unsigned char* area, int half, int lane, float (&v)[8]) {
+    const int row = 16 * half + (lane >> 2), g = lane & 3;
+    const f32x4 a = *reinterpret_cast<const f32x4*>(area + row * 128 + (((2 * g) ^ (row & 7)) << 4));
+    const f32x4 b = *reinterpret_cast<const f32x4*>(area + row * 128 + (((2 * g + 1) ^ (row & 7)) << 4));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        v[j] = a[j];
+        v[4 + j] = b[j];
     }
+}
+__device__ __forceinline__ void turn_done() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
 // Workgroup L -> (split, tile row, tile column).  Workgroups are dealt round-robin to the 8 XCDs, each with its own L2: an XCD takes a contiguous range of

@@ -1,0 +1,193 @@
+// A few rows (at most 64) through a layer: single tokens, beams.  The product is bound by reading W, the call by latency, so one launch does it all.
+#include <algorithm>
+
+#include "layers_device.h"
+
+namespace rnnt {
+
+namespace {
+
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x8_t __attribute__((ext_vector_type(8)));
+constexpr int FW = 8;              // waves of a workgroup: each takes every eighth step of 32 along k
+constexpr int FC = 32;             // columns of a workgroup: 64 bytes of a row of W
+constexpr int FD = 4;              // steps whose loads are in flight
+
+// Eight values of a row as they lie there, zeros from `live` on
+__device__ __forceinline__ bf16x8 raw8(const bf16_t* p, int live) {
+    if (live >= 8) return *reinterpret_cast<const bf16x8_any*>(p);
+    s16x8_t v = s16x8_t{0};
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (j < live) v[j] = reinterpret_cast<const short*>(p)[j];
+    return __builtin_bit_cast(bf16x8, v);
+}
+
+struct FewLinear {
+    LinearEpilogue e;
+    // columns n .. n + 7 (granule g of the workgroup's 32) of row m
+    __device__ __forceinline__ void operator()(int m, int n, int, float (&v)[8]) const {
+        float b[8];
+        LinearStore::bias(e, n, b);
+        LinearStore::store(e, 0, m, n, v, b);
+    }
+};
+// Statistics of the 32 columns of a row (four neighbouring lanes hold them), as k_ce_scores leaves them for its tiles
+struct FewCe {
+    CeEpilogue e;
+    __device__ __forceinline__ void operator()(int m, int n, int block, float (&v)[8]) const {
+        float b[8];
+        load_bias8(e.bias, n < e.V ? n : e.V - 1, e.V, b);
+        const int y = e.label[m] - n;
+        float top = RNNT_NEG_INF;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            v[j] = n + j < e.V ? v[j] + b[j] : RNNT_NEG_INF;
+            top = fmaxf(top, v[j]);
+            if (y == j && n + j < e.V) e.label_score[m] = v[j];
+        }
+        top = fmaxf(top, __shfl_xor(top, 1, 64));
+        top = fmaxf(top, __shfl_xor(top, 2, 64));
+        const float c = top == RNNT_NEG_INF ? 0.0f : top;
+        float s = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            v[j] = __builtin_amdgcn_exp2f(fmaf(v[j] - c, LOG2E_F, 15.0f));
+            s += v[j];
+        }
+        s += __shfl_xor(s, 1, 64);
+        s += __shfl_xor(s, 2, 64);
+        if (n % FC == 0) e.stats[(size_t)m * e.tiles_n + block] = make_float2(top, s);
+        if (e.kept != nullptr) store8((_Float16*)e.kept + (size_t)m * e.pitch + n, 8, v);
+    }
+};
+
+// rows x 32 columns of x W per workgroup, MT blocks of 16 rows.  A wave brings its steps (32 of k) of W through registers into LDS of its own, where the
+// transposing read makes MFMA fragments of them; x comes as fragments from memory.  The eight waves' sums meet in LDS.  Neighbouring column blocks share
+// lines of W: they go to one XCD.  What bounds it: latency (one token, K = 640, N = 2560: the launch, two trips to memory, the reduction).
+// A long sum is split over workgroups too (gridDim.y > 1), whose results go to slots [split][M][N up to 8]: 64 rows, K = 2560, N = 640 19.8 us in 20
+// workgroups, half of it x, which each of them reads whole.
+template <int MT, class E>
+__global__ __launch_bounds__(64 * FW) void k_few_rows(FewJob j, E e, int blocks, float* __restrict__ slots, int per_split) {
+    __shared__ __align__(16) unsigned char smem[FW * MT * 16 * FC * 4];
+    static_assert(MT * 16 * FC * 4 >= 2048, "a step of W per wave");
+    const int per = (blocks + 7) >> 3, block = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    if ((int)(blockIdx.x >> 3) >= per || block >= blocks) return;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, n0 = block * FC;
+    const int K = j.K, N = j.N;
+    unsigned char* area = smem + wave * 2048;
+    const bf16_t* W = (const bf16_t*)j.W + n0 + (lane & 3) * 8;
+    const int wk = lane >> 2, wlive = N - n0 - (lane & 3) * 8, xk = 8 * (lane >> 4);
+    const bf16_t* x[MT];
+    bool row_ok[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int row = 16 * i + (lane & 15);
+        row_ok[i] = row < j.M;
+        x[i] = (const bf16_t*)j.x + (size_t)(row_ok[i] ? row : 0) * K;
+    }
+    f32x4 acc[MT][2];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) acc[i][0] = acc[i][1] = f32x4{0};
+    bf16x8 w[FD][2], a[FD][MT];
+    auto fetch = [&](auto slot_tag, int k0) {
+        constexpr int s = decltype(slot_tag)::value;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int k = k0 + 16 * u + wk;
+            w[s][u] = raw8(W + (size_t)(k < K ? k : 0) * N, k < K ? wlive : 0);
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) a[s][i] = raw8(x[i] + (k0 + xk < K ? k0 + xk : 0), row_ok[i] ? K - (k0 + xk) : 0);
+    };
+    const int fj = (lane >> 2) & 3, fc = lane & 3, fg = lane >> 4;
+    auto step = [&](auto slot_tag) {
+        constexpr int s = decltype(slot_tag)::value;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) *reinterpret_cast<bf16x8*>(area + (16 * u + wk) * 64 + (lane & 3) * 16) = w[s][u];
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        bf16x8 f[2];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            // lane 16 g + 4 j + c supplies columns 4 c .. of row 8 g + j (+ 4); lane i of the 16 receives rows 8 g .. + 7 of column i
+            const unsigned char* p = area + (8 * fg + fj) * 64 + c * 32 + fc * 8;
+            const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(p));
+            const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(p + 4 * 64));
+            const s16x8_t v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            f[c] = __builtin_bit_cast(bf16x8, v);
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) acc[i][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[c], a[s][i], acc[i][c], 0, 0, 0);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    };
+    const int all = (K + 31) / 32, first = blockIdx.y * per_split, steps = first + per_split < all ? first + per_split : all;
+    static_for<0, FD>([&](auto s) { fetch(s, 32 * (first + wave + FW * decltype(s)::value)); });
+    for (int t = first + wave; t < steps; t += FW * FD)
+        static_for<0, FD>([&](auto s) {
+            constexpr int q = decltype(s)::value;
+            if (t + FW * q < steps) {
+                step(s);
+                fetch(s, 32 * (t + FW * (q + FD)));
+            }
+        });
+    __syncthreads();
+    // register r of lane l: column 4 (l / 16) + r of its 16, row l % 16
+    float* part = reinterpret_cast<float*>(smem);
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+            *reinterpret_cast<f32x4*>(part + ((wave * MT + i) * 16 + (lane & 15)) * FC + c * 16 + 4 * (lane >> 4)) = acc[i][c];
+    __syncthreads();
+    if (tid < MT * 64) {
+        const int m = tid >> 2, g = tid & 3;
+        f32x4 p = f32x4{0}, q = f32x4{0};
+#pragma unroll
+        for (int k = 0; k < FW; ++k) {
+            const float* s = part + ((size_t)k * MT * 16 + m) * FC + g * 8;
+            p += *reinterpret_cast<const f32x4*>(s);
+            q += *reinterpret_cast<const f32x4*>(s + 4);
+        }
+        float v[8] = {p[0], p[1], p[2], p[3], q[0], q[1], q[2], q[3]};
+        if (m >= j.M) return;
+        if (slots == nullptr) e(m, n0 + g * 8, block, v);
+        else {
+            const int Np = (N + 7) / 8 * 8;
+            if (n0 + g * 8 < Np) store8(slots + ((size_t)blockIdx.y * j.M + m) * Np + n0 + g * 8, 8, v);
+        }
+    }
+}
+
+template <class E>
+hipError_t launch_few(const FewJob& j, const E& e, int splits, float* slots, hipStream_t stream) {
+    if (j.M <= 0 || j.M > FEW_ROWS) return j.M <= 0 ? hipSuccess : hipErrorInvalidValue;
+    const int blocks = (j.N + FC - 1) / FC, per = ((j.K + 31) / 32 + splits - 1) / splits;
+    const dim3 grid((unsigned)((blocks + 7) / 8 * 8), (unsigned)splits);
+    if (j.M <= 16) k_few_rows<1, E><<<grid, dim3(64 * FW), 0, stream>>>(j, e, blocks, slots, per);
+    else if (j.M <= 32) k_few_rows<2, E><<<grid, dim3(64 * FW), 0, stream>>>(j, e, blocks, slots, per);
+    else k_few_rows<4, E><<<grid, dim3(64 * FW), 0, stream>>>(j, e, blocks, slots, per);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+// More than four steps per wave are shared by as many workgroups as fill the chip, each with a step per wave at least.
+int few_splits(long long M, int K, int N) {
+    const int steps = (K + 31) / 32, blocks = (N + FC - 1) / FC;
+    if (M > FEW_ROWS || steps <= 4 * FW) return 1;
+    const int most = std::min(steps / FW, std::max(1, 256 / blocks)), per = (steps + most - 1) / most;
+    return (steps + per - 1) / per;
+}
+hipError_t launch_few_linear(const FewJob& j, int splits, float* slots, const LinearEpilogue& e, hipStream_t stream) {
+    const hipError_t err = launch_few(j, FewLinear{e}, splits, splits > 1 ? slots : nullptr, stream);
+    return err != hipSuccess || splits <= 1 ? err : launch_linear_reduce(j.M, j.N, splits, slots, e, stream);
+}
+hipError_t launch_few_ce(const FewJob& j, const CeEpilogue& e, hipStream_t stream) { return launch_few(j, FewCe{e}, 1, nullptr, stream); }
+
+}  // namespace rnnt

@@ -29,56 +29,100 @@ __device__ __forceinline__ JobExtent job_extent(const GemmJob& g) {
 }
 
 template <class TS, bool AKS, bool BKS, class E>
-__global__ __launch_bounds__(TS::THREADS, 2) void k_layer_gemm(GemmJob g, E e, int mt, int nt, int splits, int per_split) {
-    extern __shared__ __align__(16) unsigned char smem[];
+__device__ __forceinline__ void gemm_workgroup(const GemmJob& g, const E& e, int L, int mt, int nt, int splits, int per_split, unsigned char* smem) {
     TilePlace t;
-    if (!place_tile(blockIdx.x, mt, nt, splits, t)) return;
+    if (!place_tile(L, mt, nt, splits, t)) return;
     const JobExtent x = job_extent(g);
     const long long m0 = (long long)t.m * TS::BM, n0 = (long long)t.n * TS::BN;
     if (m0 >= x.M) return;
     const int s0 = t.split * per_split, s1 = s0 + per_split < x.stages ? s0 + per_split : x.stages;
     f32x16 acc[TS::MT][TS::NT];
     gemm_tile<TS, AKS, BKS>(acc, g.A, g.B, m0, n0, g.a_rows, g.b_rows, s0, s1, smem);
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l32 = lane & 31, hb = lane >> 5;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int wm = wave / TS::WN, wn = wave % TS::WN;
     typedef typename EpilogueOf<E>::type Store;
+    unsigned char* area = smem + wave * TURN_BYTES;
 #pragma unroll
-    for (int j = 0; j < TS::NT; ++j)
+    for (int j = 0; j < TS::NT; ++j) {
+        const int n = (int)n0 + (wn * TS::NT + j) * 32 + 8 * (lane & 3);
+        float b[8];
+        Store::bias(e, n, b);
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
-            const int n = (int)n0 + (wn * TS::NT + j) * 32 + 16 * p + 8 * hb;
-            float b[8];
-            Store::bias(e, n, b);
-#pragma unroll
-            for (int i = 0; i < TS::MT; ++i) {
-                const long long m = m0 + (wm * TS::MT + i) * 32 + l32;
+        for (int i = 0; i < TS::MT; ++i) {
+            turn_block(acc[i][j], area, lane);
+#pragma unroll 1
+            for (int half = 0; half < 2; ++half) {
                 float v[8];
-                granule8(acc[i][j], p, v);
-                Store::store(e, t.split, m, n, v, b);
+                turned8(area, half, lane, v);
+                Store::store(e, t.split, m0 + (wm * TS::MT + i) * 32 + 16 * half + (lane >> 2), n, v, b);
             }
+            turn_done();
         }
+    }
+}
+
+// A product and how its workgroups are dealt out
+template <class E>
+struct TileJob {
+    GemmJob g;
+    E e;
+    int mt, nt, splits, per_split;
+    __host__ __device__ long long workgroups() const { return ((long long)mt * nt * splits + 7) / 8 * 8; }
+};
+template <class TS, bool AKS, bool BKS, class E>
+__global__ __launch_bounds__(TS::THREADS, 2) void k_layer_gemm(TileJob<E> j) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    gemm_workgroup<TS, AKS, BKS, E>(j.g, j.e, blockIdx.x, j.mt, j.nt, j.splits, j.per_split, smem);
+}
+// dx and dW
+template <class TS>
+__global__ __launch_bounds__(TS::THREADS, 2) void k_layer_grads(TileJob<StoreEpilogue> x, TileJob<StoreEpilogue> w, int wgs_w) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int L = blockIdx.x;
+    if (L < wgs_w) gemm_workgroup<TS, true, true, StoreEpilogue>(w.g, w.e, L, w.mt, w.nt, w.splits, w.per_split, smem);
+    else gemm_workgroup<TS, false, false, StoreEpilogue>(x.g, x.e, L - wgs_w, x.mt, x.nt, x.splits, x.per_split, smem);
 }
 
 // The sum of the splits' results, in order, and the epilogue.  One thread per eight columns.
 template <class E>
-__global__ __launch_bounds__(256) void k_layer_reduce(GemmJob g, E e, const float* __restrict__ slots, int splits, long long Np, long long stride,
-                                                      long long total) {
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (i >= total) return;
-    const long long per = Np / 8, m = i / per;
+struct ReduceJob {
+    GemmJob g;
+    E e;
+    const float* slots;
+    int splits;
+    long long Np, stride, total;
+    __host__ __device__ unsigned workgroups() const { return splits > 1 ? (unsigned)((total + 255) / 256) : 0u; }
+};
+template <class E>
+__device__ __forceinline__ void reduce_workgroup(const ReduceJob<E>& r, unsigned block) {
+    const long long i = (long long)block * 256 + threadIdx.x;
+    if (i >= r.total) return;
+    const long long per = r.Np / 8, m = i / per;
     const int n = (int)(i - m * per) * 8;
-    if (m >= job_extent(g).M) return;
-    const float* s = slots + (size_t)m * Np + n;
+    if (m >= job_extent(r.g).M) return;
+    const float* s = r.slots + (size_t)m * r.Np + n;
     f32x4 a = f32x4{0}, b = f32x4{0};
 #pragma unroll 4
-    for (int k = 0; k < splits; ++k, s += stride) {
+    for (int k = 0; k < r.splits; ++k, s += r.stride) {
         a += *reinterpret_cast<const f32x4*>(s);
         b += *reinterpret_cast<const f32x4*>(s + 4);
     }
     float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}, bias[8];
     typedef typename EpilogueOf<E>::type Store;
-    Store::bias(e, n, bias);
-    Store::store(e, 0, m, n, v, bias);
+    Store::bias(r.e, n, bias);
+    Store::store(r.e, 0, m, n, v, bias);
+}
+template <class E>
+__global__ __launch_bounds__(256) void k_layer_reduce(ReduceJob<E> r) {
+    reduce_workgroup(r, blockIdx.x);
+}
+__global__ __launch_bounds__(256) void k_layer_reduce_grads(ReduceJob<StoreEpilogue> x, ReduceJob<StoreEpilogue> w, SumJob db, int db_blocks, int db_rows) {
+    __shared__ float red[8][32];
+    unsigned L = blockIdx.x;
+    if (L < x.workgroups()) return reduce_workgroup(x, L);
+    L -= x.workgroups();
+    if (L < w.workgroups()) return reduce_workgroup(w, L);
+    sum_parts(db, db_blocks, db_rows, (int)(L - w.workgroups()), red);
 }
 
 // Scores of a tile and what the softmax needs of them: each row's maximum over the tile's columns, the sum of the exponentials relative to it and, where
@@ -151,18 +195,22 @@ __global__ __launch_bounds__(TS::THREADS, 2) void k_ce_scores(GemmJob g, CeEpilo
         s = both_halves_sum(s);
         if (hb == 0) sum[wn * TS::BM + row] = s;
         if constexpr (KEEP) {
-            _Float16* dst = (_Float16*)e.kept + (size_t)(m0 + row) * e.pitch + n0 + wn * TS::NT * 32 + 8 * hb;
+            unsigned char* area = smem + 2 * TS::WN * TS::BM * 4 + wave * TURN_BYTES;
 #pragma unroll
-            for (int j = 0; j < TS::NT; ++j)
+            for (int j = 0; j < TS::NT; ++j) {
+                turn_block(acc[i][j], area, lane);
 #pragma unroll
-                for (int p = 0; p < 2; ++p) {
+                for (int half = 0; half < 2; ++half) {
                     float v[8];
-                    granule8(acc[i][j], p, v);
+                    turned8(area, half, lane, v);
                     f16x8 h;
 #pragma unroll
                     for (int k = 0; k < 8; ++k) h[k] = (_Float16)v[k];
-                    *reinterpret_cast<f16x8*>(dst + j * 32 + 16 * p) = h;
+                    *reinterpret_cast<f16x8*>((_Float16*)e.kept + (size_t)(m0 + (wm * TS::MT + i) * 32 + 16 * half + (lane >> 2)) * e.pitch + n0 +
+                                              (wn * TS::NT + j) * 32 + 8 * (lane & 3)) = h;
                 }
+                turn_done();
+            }
         }
         if (wn == 0 && hb == 0) e.stats[(size_t)(m0 + row) * e.tiles_n + t.n].x = m;
     }
@@ -194,43 +242,70 @@ hipError_t launch_tiles(long long tiles, hipStream_t stream, const ARGS&... args
     return hipGetLastError();
 }
 
+template <class TS, class E>
+TileJob<E> tile_job(const GemmJob& g, const E& e, int splits, int per_split) {
+    return TileJob<E>{g, e, (int)((g.M + TS::BM - 1) / TS::BM), (int)((g.N + TS::BN - 1) / TS::BN), splits, per_split};
+}
+inline long long padded8(long long n) { return (n + 7) / 8 * 8; }
+StoreEpilogue slot_epilogue(const GemmJob& g, float* slots) {
+    return StoreEpilogue{slots, nullptr, nullptr, padded8(g.N), g.M * padded8(g.N), g.M, (int)padded8(g.N), false};
+}
+template <class E>
+ReduceJob<E> reduce_job(const GemmJob& g, const E& e, const float* slots, int splits) {
+    return ReduceJob<E>{g, e, slots, splits, padded8(g.N), g.M * padded8(g.N), g.M * (padded8(g.N) / 8)};
+}
+
 template <class TS, bool AKS, bool BKS, class E>
 hipError_t gemm_of(const GemmJob& g, const GemmPlan& p, float* slots, const E& e, hipStream_t stream) {
-    const int mt = (int)((g.M + TS::BM - 1) / TS::BM), nt = (int)((g.N + TS::BN - 1) / TS::BN);
-    if (p.splits <= 1) return launch_tiles<&k_layer_gemm<TS, AKS, BKS, E>, TS>((long long)mt * nt, stream, g, e, mt, nt, 1, g.stages);
-    const long long Np = (g.N + 7) / 8 * 8, stride = g.M * Np;
-    const StoreEpilogue slot{slots, nullptr, nullptr, Np, stride, g.M, (int)Np, false, true};
-    hipError_t err = launch_tiles<&k_layer_gemm<TS, AKS, BKS, StoreEpilogue>, TS>((long long)mt * nt * p.splits, stream, g, slot, mt, nt, p.splits,
-                                                                                   p.per_split);
+    if (p.splits <= 1) {
+        const TileJob<E> j = tile_job<TS>(g, e, 1, g.stages);
+        return launch_tiles<&k_layer_gemm<TS, AKS, BKS, E>, TS>(j.workgroups(), stream, j);
+    }
+    const TileJob<StoreEpilogue> j = tile_job<TS>(g, slot_epilogue(g, slots), p.splits, p.per_split);
+    hipError_t err = launch_tiles<&k_layer_gemm<TS, AKS, BKS, StoreEpilogue>, TS>(j.workgroups(), stream, j);
     if (err != hipSuccess) return err;
-    const long long total = g.M * (Np / 8);
-    if ((total + 255) / 256 > 0x7fffffffLL) return hipErrorInvalidValue;
-    k_layer_reduce<E><<<dim3((unsigned)((total + 255) / 256)), dim3(256), 0, stream>>>(g, e, slots, p.splits, Np, stride, total);
+    const ReduceJob<E> r = reduce_job(g, e, slots, p.splits);
+    if ((r.total + 255) / 256 > 0x7fffffffLL) return hipErrorInvalidValue;
+    k_layer_reduce<E><<<dim3(r.workgroups()), dim3(256), 0, stream>>>(r);
     return hipGetLastError();
 }
-template <bool AKS, bool BKS, class E>
-hipError_t gemm_of(const GemmJob& g, const GemmPlan& p, float* slots, const E& e, hipStream_t stream) {
-    if (g.M <= 0 || g.N <= 0) return hipSuccess;
-    return p.tile == 256 ? gemm_of<TileShape<256>, AKS, BKS, E>(g, p, slots, e, stream) : gemm_of<TileShape<128>, AKS, BKS, E>(g, p, slots, e, stream);
+
+template <class TS>
+hipError_t grad_gemms(const GradGemm& dx, const GradGemm& dw, hipStream_t stream) {
+    TileJob<StoreEpilogue> x{}, w{};
+    if (dx.g.M > 0) x = tile_job<TS>(dx.g, dx.splits > 1 ? slot_epilogue(dx.g, dx.slots) : dx.e, dx.splits, dx.splits > 1 ? dx.per_split : dx.g.stages);
+    if (dw.g.M > 0) w = tile_job<TS>(dw.g, dw.splits > 1 ? slot_epilogue(dw.g, dw.slots) : dw.e, dw.splits, dw.splits > 1 ? dw.per_split : dw.g.stages);
+    const long long nx = x.workgroups(), nw = w.workgroups();
+    if (nx + nw > 0x7ffffff0LL) return hipErrorInvalidValue;
+    return launch_tiles<&k_layer_grads<TS>, TS>(nx + nw, stream, x, w, (int)nw);
 }
 
 }  // namespace
 
 // Rounds of the chip (256 compute units; one large tile each, or two small ones) times a round's time, in units of a large tile's stage (about 1.5 us;
 // a small one, with its neighbour beside it, 0.7), with five stages' time for a round's start and end; the slots' way to memory and back.
+namespace {
+constexpr double STAGE_TIME[2] = {1.0, 0.7}, ENDS_TIME[2] = {5.0, 4.0}, AT_ONCE[2] = {256.0, 512.0}, BYTES_PER_UNIT = 6e6, LAUNCH_TIME = 3.0;
+double tile_count(int tile, long long M, long long N) { return (double)((M + tile - 1) / tile) * (double)((N + tile - 1) / tile); }
+double slot_time(const GemmPlan& p, long long M, long long N) {
+    return p.splits > 1 ? (double)gemm_slot_bytes(p, M, N) * 2.0 / BYTES_PER_UNIT : 0.0;
+}
+bool split_ok(const GemmPlan& p, int stages, long long M, long long N, size_t slot_cap) {
+    if (p.splits == 1) return true;
+    return p.splits <= std::max(1, stages / 2) && (p.splits - 1) * p.per_split < stages && gemm_slot_bytes(p, M, N) <= slot_cap;
+}
+}  // namespace
 GemmPlan plan_gemm(long long M, long long N, int stages, size_t slot_cap) {
     GemmPlan best{256, 1, stages};
     double least = 1e300;
-    for (int tile : {256, 128}) {
-        const double tiles = (double)((M + tile - 1) / tile) * (double)((N + tile - 1) / tile);
-        const double at_once = tile == 256 ? 256.0 : 512.0, stage = tile == 256 ? 1.0 : 0.7, ends = tile == 256 ? 5.0 : 4.0;
-        for (int splits = 1; splits <= 64 && splits <= std::max(1, stages / 2); ++splits) {
+    for (int k = 0; k < 2; ++k) {
+        const int tile = k == 0 ? 256 : 128;
+        const double tiles = tile_count(tile, M, N);
+        for (int splits = 1; splits <= 64; ++splits) {
             const GemmPlan p{tile, splits, (stages + splits - 1) / splits};
-            if ((p.splits - 1) * p.per_split >= stages && splits > 1) continue;      // an empty split
-            if (splits > 1 && gemm_slot_bytes(p, M, N) > slot_cap) break;
-            const double rounds = std::max(1.0, (double)(long long)((tiles * splits + at_once - 1) / at_once));
-            double t = rounds * (p.per_split * stage + ends);
-            if (splits > 1) t += 3.0 + (double)gemm_slot_bytes(p, M, N) * 2.0 / 6e6;       // (6 MB per unit)
+            if (!split_ok(p, stages, M, N, slot_cap)) continue;
+            const double rounds = std::max(1.0, (double)(long long)((tiles * splits + AT_ONCE[k] - 1) / AT_ONCE[k]));
+            const double t = rounds * (p.per_split * STAGE_TIME[k] + ENDS_TIME[k]) + (splits > 1 ? LAUNCH_TIME + slot_time(p, M, N) : 0.0);
             if (t < least) {
                 least = t;
                 best = p;
@@ -239,12 +314,62 @@ GemmPlan plan_gemm(long long M, long long N, int stages, size_t slot_cap) {
     }
     return best;
 }
+// The same for two products that share a launch: workgroups of both, the longer ones first, fill the chip one after the other.
+PairPlan plan_pair(long long Mx, long long Nx, int stages_x, long long Mw, long long Nw, int stages_w, size_t slot_cap) {
+    static const int SPLITS[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64};
+    PairPlan best{256, {256, 1, stages_x}, {256, 1, stages_w}};
+    double least = 1e300;
+    for (int k = 0; k < 2; ++k) {
+        const int tile = k == 0 ? 256 : 128;
+        const double tx = tile_count(tile, Mx, Nx), tw = tile_count(tile, Mw, Nw);
+        for (int sx : SPLITS) {
+            const GemmPlan px{tile, sx, (stages_x + sx - 1) / sx};
+            if (!split_ok(px, stages_x, Mx, Nx, slot_cap)) continue;
+            const double ux = px.per_split * STAGE_TIME[k] + ENDS_TIME[k];
+            for (int sw : SPLITS) {
+                const GemmPlan pw{tile, sw, (stages_w + sw - 1) / sw};
+                if (!split_ok(pw, stages_w, Mw, Nw, slot_cap)) continue;
+                const double uw = pw.per_split * STAGE_TIME[k] + ENDS_TIME[k];
+                const double nx = tx * sx, nw = tw * sw, work = (nx * ux + nw * uw) / AT_ONCE[k];
+                // at least one workgroup's time; the last round is on average half empty
+                const double t = std::max(std::max(nx > 0 ? ux : 0.0, nw > 0 ? uw : 0.0), work + 0.5 * std::min(ux, uw) * (work > std::max(ux, uw))) +
+                                 (sx > 1 || sw > 1 ? LAUNCH_TIME + slot_time(px, Mx, Nx) + slot_time(pw, Mw, Nw) : 0.0);
+                if (t < least) {
+                    least = t;
+                    best = PairPlan{tile, px, pw};
+                }
+            }
+        }
+    }
+    return best;
+}
 
 hipError_t launch_linear_gemm(const GemmJob& g, const GemmPlan& p, float* slots, const LinearEpilogue& e, hipStream_t stream) {
-    return gemm_of<false, true, LinearEpilogue>(g, p, slots, e, stream);
+    if (g.M <= 0 || g.N <= 0) return hipSuccess;
+    return p.tile == 256 ? gemm_of<TileShape<256>, false, true, LinearEpilogue>(g, p, slots, e, stream)
+                         : gemm_of<TileShape<128>, false, true, LinearEpilogue>(g, p, slots, e, stream);
 }
-hipError_t launch_store_gemm(bool k_slow, const GemmJob& g, const GemmPlan& p, float* slots, const StoreEpilogue& e, hipStream_t stream) {
-    return k_slow ? gemm_of<true, true, StoreEpilogue>(g, p, slots, e, stream) : gemm_of<false, false, StoreEpilogue>(g, p, slots, e, stream);
+hipError_t launch_linear_reduce(long long M, int N, int splits, const float* slots, const LinearEpilogue& e, hipStream_t stream) {
+    GemmJob g{};
+    g.M = M;
+    g.N = N;
+    const ReduceJob<LinearEpilogue> r = reduce_job(g, e, slots, splits);
+    k_layer_reduce<LinearEpilogue><<<dim3(r.workgroups()), dim3(256), 0, stream>>>(r);
+    return hipGetLastError();
+}
+hipError_t launch_grad_gemms(int tile, const GradGemm& dx, const GradGemm& dw, const SumJob& db, hipStream_t stream) {
+    if (dx.g.M > 0 || dw.g.M > 0) {
+        const hipError_t e = tile == 256 ? grad_gemms<TileShape<256>>(dx, dw, stream) : grad_gemms<TileShape<128>>(dx, dw, stream);
+        if (e != hipSuccess) return e;
+    }
+    ReduceJob<StoreEpilogue> x{}, w{};
+    if (dx.g.M > 0) x = reduce_job(dx.g, dx.e, dx.slots, dx.splits);
+    if (dw.g.M > 0) w = reduce_job(dw.g, dw.e, dw.slots, dw.splits);
+    const long long n = (long long)x.workgroups() + w.workgroups() + (db.part != nullptr ? (db.N + 31) / 32 : 0);
+    if (n == 0) return hipSuccess;
+    if (n > 0x7fffffffLL) return hipErrorInvalidValue;
+    k_layer_reduce_grads<<<dim3((unsigned)n), dim3(256), 0, stream>>>(x, w, db, (int)sum_blocks(db.rows, db.N), sum_rows(db.rows, db.N));
+    return hipGetLastError();
 }
 hipError_t launch_ce_gemm(const GemmJob& g, int tile, const CeEpilogue& e, hipStream_t stream) {
     if (g.M <= 0) return hipSuccess;

@@ -20,29 +20,6 @@ __global__ __launch_bounds__(256) void k_layer_pad(const T* __restrict__ src, lo
     }
 }
 
-// Eight consecutive values of a row, as floats
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, int live, bool vec, float (&v)[8]) {
-    if (vec) {
-        if constexpr (sizeof(T) == 2) {
-            typedef T t8 __attribute__((ext_vector_type(8)));
-            const t8 x = *reinterpret_cast<const t8*>(p);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = (float)x[j];
-        } else {
-            const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                v[j] = a[j];
-                v[4 + j] = b[j];
-            }
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = j < live ? (float)p[j] : 0.0f;
-    }
-}
-
 // The sums of 32 column granules over the eight thread rows of a workgroup -> part[n]
 __device__ __forceinline__ void fold_columns(float (&sum)[8], float (*red)[256], float* __restrict__ part, int n, int N, int tid) {
     const int row = tid >> 5, g = tid & 31;
@@ -55,27 +32,27 @@ __device__ __forceinline__ void fold_columns(float (&sum)[8], float (*red)[256],
     if (n + tid < N) part[n + tid] = t;
 }
 
-// dz = dy act'(z) mask / (1 - p): a workgroup takes 128 rows x 256 columns, 8 thread rows x 32 granules of 8 columns.
+// dz = dy act'(z) mask / (1 - p): a workgroup takes R rows x 256 columns, 8 thread rows x 32 granules of 8 columns.
 template <typename T, typename S>
-__global__ __launch_bounds__(256) void k_layer_dz(DzArgs a) {
+__global__ __launch_bounds__(256) void k_layer_dz(DzArgs a, int R) {
     constexpr bool FAST = sizeof(T) == 2;
     __shared__ __align__(16) float red[8][256];
     const int nb = (int)((a.ld + 255) / 256), rb = blockIdx.x / nb;
     const int tid = threadIdx.x, n0 = (blockIdx.x - rb * nb) * 256, n = n0 + (tid & 31) * 8;
-    const long long r0 = (long long)rb * SUM_ROWS;
+    const long long r0 = (long long)rb * R;
     const int live = a.N - n < 0 ? 0 : a.N - n < 8 ? a.N - n : 8;
     float sum[8] = {};
 #pragma unroll 2
-    for (int i = 0; i < SUM_ROWS / 8; ++i) {
+    for (int i = 0; i < R / 8; ++i) {
         const long long m = r0 + i * 8 + (tid >> 5);
         if (m >= a.rows_to || n >= a.ld) break;
         float v[8] = {};
         if (m < a.M && live > 0) {
             const size_t at = (size_t)m * a.N + n;
-            load8((const T*)a.dy + at, live, a.vec && live == 8, v);
+            load8((const T*)a.dy + at, live, v);
             if (a.saved != nullptr) {
                 float z[8];
-                load8((const S*)a.saved + at, live, a.vec && live == 8, z);
+                load8((const S*)a.saved + at, live, z);
                 act_grad8<FAST>(a.act, z, v);
             }
             drop8(a.drop, m, n, v);
@@ -101,32 +78,24 @@ __global__ __launch_bounds__(256) void k_layer_dz(DzArgs a) {
     if (a.part != nullptr && r0 < a.M) fold_columns(sum, red, a.part + (size_t)rb * a.ld, n0, a.N, tid);
 }
 
-// 32 columns x 8 thread rows per workgroup; the partial sums are added in a fixed order
-template <typename O>
-__global__ __launch_bounds__(256) void k_layer_sum_parts(const float* __restrict__ part, int blocks, long long ld, int N, const int* __restrict__ count,
-                                                         long long row0, const float* __restrict__ prev, O* __restrict__ out) {
+__global__ __launch_bounds__(256) void k_layer_sum_parts(SumJob j, int blocks, int R) {
     __shared__ float red[8][32];
-    const int c = threadIdx.x & 31, row = threadIdx.x >> 5, n = blockIdx.x * 32 + c;
-    if (count != nullptr) {
-        long long r = (long long)*count - row0;
-        r = r < 0 ? 0 : (r + SUM_ROWS - 1) / SUM_ROWS;
-        blocks = r < blocks ? (int)r : blocks;
-    }
-    float s = 0.0f;
-    if (n < N)
-        for (int b = row; b < blocks; b += 8) s += part[(size_t)b * ld + n];
-    red[row][c] = s;
-    __syncthreads();
-    if (row == 0 && n < N) {
-        float t = prev != nullptr ? prev[n] : 0.0f;
+    sum_parts(j, blocks, R, blockIdx.x, red);
+}
+
+// The splits' sum, in order
+__device__ __forceinline__ void load8_sum(const float* p, int splits, long long stride, int live, float (&v)[8]) {
+    load8(p, live, v);
+    for (int k = 1; k < splits; ++k) {
+        float x[8];
+        load8(p + k * stride, live, x);
 #pragma unroll
-        for (int r = 0; r < 8; ++r) t += red[r][c];
-        out[n] = (O)t;
+        for (int j = 0; j < 8; ++j) v[j] += x[j];
     }
 }
 
 // z (pitch ld, may be saved or y) + bias -> saved, y; one thread per eight columns
-__global__ __launch_bounds__(256) void k_linear_rows_f32(const float* z, long long ld, const float* __restrict__ bias, const float* __restrict__ residual,
+__global__ __launch_bounds__(256) void k_linear_rows_f32(const float* z, long long ld, int splits, long long stride, const float* __restrict__ bias, const float* __restrict__ residual,
                                                          float* y, float* saved, long long M, int N, int act, Dropout drop, long long groups,
                                                          long long total) {
     const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
@@ -134,48 +103,49 @@ __global__ __launch_bounds__(256) void k_linear_rows_f32(const float* z, long lo
     const long long m = i / groups;
     const int n = (int)(i - m * groups) * 8, live = N - n < 8 ? N - n : 8;
     const size_t at = (size_t)m * N + n;
-    const bool vec = live == 8 && N % 4 == 0;
     float v[8], b[8];
-    load8(z + (size_t)m * ld + n, live, vec, v);
+    load8_sum(z + (size_t)m * ld + n, splits, stride, live, v);
     load_bias8(bias, n, N, b);
-    auto store8 = [&](float* to) {
-        if (vec) {
-            *reinterpret_cast<f32x4*>(to + at) = f32x4{v[0], v[1], v[2], v[3]};
-            *reinterpret_cast<f32x4*>(to + at + 4) = f32x4{v[4], v[5], v[6], v[7]};
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (j < live) to[at + j] = v[j];
-        }
-    };
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] += b[j];
-    if (saved != nullptr) store8(saved);
+    if (saved != nullptr) store8(saved + at, live, v);
     act8<false>(act, v);
     drop8(drop, m, n, v);
     if (residual != nullptr) {
         float r[8];
-        load8(residual + at, live, vec, r);
+        load8(residual + at, live, r);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] += r[j];
     }
-    store8(y);
+    store8(y + at, live, v);
 }
 
-__global__ __launch_bounds__(256) void k_layer_crop_f32(const float* __restrict__ src, long long ld, float* __restrict__ dst, int N, long long total,
-                                                        bool add) {
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
-        const long long r = i / N;
-        const float v = src[r * ld + (i - r * N)];
-        dst[i] = add ? dst[i] + v : v;
+__global__ __launch_bounds__(256) void k_layer_reduce_f32(const float* __restrict__ src, long long ld, int splits, long long stride,
+                                                          const int* __restrict__ row_map, float* __restrict__ dst, int N, bool add, long long groups,
+                                                          long long total) {
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (i >= total) return;
+    const long long m = i / groups;
+    const int n = (int)(i - m * groups) * 8, live = N - n < 8 ? N - n : 8;
+    const long long row = row_map != nullptr ? row_map[m] : m;
+    if (row < 0) return;
+    float v[8];
+    load8_sum(src + (size_t)m * ld + n, splits, stride, live, v);
+    float* to = dst + (size_t)row * N + n;
+    if (add) {
+        float p[8];
+        load8(to, live, p);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += p[j];
     }
+    store8(to, live, v);
 }
 
 // ---- cross entropy --------------------------------------------------------------------------------------------------
 // Each workgroup counts the real rows before its own SCAN_ROWS (the labels come from the L2) and numbers its own.
 constexpr int SCAN_THREADS = 1024, SCAN_PER = 4, SCAN_ROWS = SCAN_THREADS * SCAN_PER;
 __global__ __launch_bounds__(SCAN_THREADS) void k_ce_rows(const int* __restrict__ labels, const float* __restrict__ weight, long long R, int ignore,
-                                                          long long cap, CeRows r) {
+                                                          long long cap, int* __restrict__ place, CeRows r) {
     __shared__ int wave_sum[SCAN_THREADS / 64], wave_before[SCAN_THREADS / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const long long first = (long long)blockIdx.x * SCAN_ROWS;
@@ -212,7 +182,7 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_ce_rows(const int* __restrict_
         const long long i = first + tid * SCAN_PER + k;
         if (i >= R) break;
         const bool real = y[k] != ignore;
-        r.place[i] = real ? at : -1;
+        place[i] = real ? at : -1;
         if (real) {
             r.index[at] = (int)i;
             r.label[at] = y[k];
@@ -231,101 +201,190 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_ce_rows(const int* __restrict_
     }
 }
 
-// One wavefront per row of x (its copy, or loss = 0 and dx = 0), then per row behind the last
-template <typename T>
-__global__ __launch_bounds__(256) void k_ce_gather(const T* __restrict__ x, long long R, int D, CeRows r, T* __restrict__ xp, long long ld,
-                                                   long long fill_to, float* __restrict__ loss, T* __restrict__ dx, bool vec) {
-    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
+// A workgroup takes 16 rows of x, a wavefront four: their copies, or loss = 0 and dx = 0.  The workgroups behind those fill what lies behind the last row.
+// SCAN: a workgroup counts the real rows before its own itself (the labels come from the L2), which saves a launch; else k_ce_rows has left `place`.
+constexpr int GATHER_ROWS = 16;
+typedef int i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+template <typename T, bool SCAN>
+__global__ __launch_bounds__(256) void k_ce_gather(const T* __restrict__ x, long long R, int D, const int* __restrict__ labels,
+                                                   const float* __restrict__ weight, int ignore, long long cap, const int* __restrict__ place, CeRows r,
+                                                   T* __restrict__ xp, long long ld, long long fill_to, float* __restrict__ loss, T* __restrict__ dx,
+                                                   int row_wgs) {
+    __shared__ int wave_count[4], at_row[GATHER_ROWS];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const long long first = (long long)blockIdx.x * GATHER_ROWS;
+    const bool fill = (int)blockIdx.x >= row_wgs;
+    long long n = 0;                                              // real rows before this workgroup's, for the filling ones: all of them
+    if constexpr (SCAN) {
+        const long long upto = fill ? R : first;
+        int c = 0;
+        long long i = tid * 4;
+#pragma unroll 4
+        for (; i + 4 <= upto; i += 1024) {
+            const i32x4_any y = *reinterpret_cast<const i32x4_any*>(labels + i);
+            c += (y[0] != ignore) + (y[1] != ignore) + (y[2] != ignore) + (y[3] != ignore);
+        }
+        for (; i < upto; ++i) c += labels[i] != ignore;           // (one thread's last three at most)
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) c += __shfl_xor(c, o, 64);
+        if (lane == 0) wave_count[wave] = c;
+        __syncthreads();
+        n = wave_count[0] + wave_count[1] + wave_count[2] + wave_count[3];
+        if (!fill && tid < GATHER_ROWS) {
+            const int y = first + tid < R ? labels[first + tid] : ignore;
+            const bool real = y != ignore;
+            const unsigned before = (unsigned)__ballot(real) & ((1u << tid) - 1u);
+            const int at = (int)n + __popc(before);
+            at_row[tid] = real ? at : -1;
+            if (real) {
+                r.index[at] = (int)(first + tid);
+                r.label[at] = y;
+                r.weight[at] = weight != nullptr ? weight[first + tid] : 1.0f;
+            }
+        }
+        __syncthreads();
+    } else if (fill) n = *r.count;
     constexpr int E = 16 / sizeof(T);
     typedef T piece __attribute__((ext_vector_type(E)));
-    if (row < R) {
-        const int to = r.place[row];
-        const T* src = x + (size_t)row * D;
-        if (to < 0) {
-            if (lane == 0) loss[row] = 0.0f;
-            if (dx != nullptr)
-                for (int c = lane; c < D; c += 64) dx[(size_t)row * D + c] = (T)0;
-            return;
-        }
-        T* dst = xp + (size_t)to * ld;
-        if (vec) {
-            for (int c = lane * E; c < D; c += 64 * E) *reinterpret_cast<piece*>(dst + c) = *reinterpret_cast<const piece*>(src + c);
-            for (int c = D + lane; c < ld; c += 64) dst[c] = (T)0;
-        } else {
-            for (int c = lane; c < ld; c += 64) dst[c] = c < D ? src[c] : (T)0;
+    if (!fill) {
+        const bool vec = D % E == 0;
+#pragma unroll
+        for (int k = 0; k < GATHER_ROWS / 4; ++k) {
+            const long long row = first + wave * (GATHER_ROWS / 4) + k;
+            if (row >= R) break;
+            const int to = SCAN ? at_row[wave * (GATHER_ROWS / 4) + k] : place[row];
+            const T* src = x + (size_t)row * D;
+            if (to < 0) {
+                if (lane == 0) loss[row] = 0.0f;
+                if (dx != nullptr)
+                    for (int c = lane; c < D; c += 64) dx[(size_t)row * D + c] = (T)0;
+                continue;
+            }
+            T* dst = xp + (size_t)to * ld;
+            if (vec) {
+                for (int c = lane * E; c < D; c += 64 * E) *reinterpret_cast<piece*>(dst + c) = *reinterpret_cast<const piece*>(src + c);
+                for (int c = D + lane; c < ld; c += 64) dst[c] = (T)0;
+            } else {
+                for (int c = lane; c < ld; c += 64) dst[c] = c < D ? src[c] : (T)0;
+            }
         }
         return;
     }
     // zeros behind the last row, up to fill_to (0: the next multiple of 256)
-    const long long n = *r.count, end = fill_to != 0 ? fill_to : (n + 255) / 256 * 256, at = n + (row - R);
-    if (at < end)
+    const int wg = blockIdx.x - row_wgs, wgs = gridDim.x - row_wgs;
+    const long long end = fill_to != 0 ? fill_to : (n + 255) / 256 * 256;
+    for (long long at = n + wg * 4 + wave; at < end; at += wgs * 4)
         for (int c = lane; c < ld; c += 64) xp[(size_t)at * ld + c] = (T)0;
+    if constexpr (SCAN) {
+        if (wg == 0 && tid == 0) *r.count = (int)n;
+        for (long long i = n + wg * 256 + tid; i < cap; i += wgs * 256) {
+            r.index[i] = -1;
+            r.label[i] = -1;
+            r.weight[i] = 0.0f;
+        }
+    }
 }
 
-// One wavefront per row: lse = M + ln(S / 2^15) out of the tiles' statistics, loss = lse - score of the label, and per tile the factor that makes
-// weight * probability of a kept exponential.
-__global__ __launch_bounds__(256) void k_ce_finish(CeRows r, long long row0, long long rows, const float* __restrict__ label_score,
-                                                   float2* __restrict__ stats, int tiles_n, int V, float* __restrict__ loss, bool grads) {
+// Row i of a chunk: lse = M + ln(S / 2^15) out of the parts' statistics, loss = lse - score of the label (at < 0: not written); its scale.
+__device__ __forceinline__ float2 ce_finish_row(const CeChunk& c, long long i, int at, float M, float S) {
+    const float m = M == RNNT_NEG_INF ? 0.0f : M;
+    const int y = c.r.label[c.row0 + i];
+    // (no entry of the vocabulary is possible, or the label is none of them: +inf)
+    const bool none = S == 0.0f || (unsigned)y >= (unsigned)c.V;
+    if (at >= 0) c.loss[at] = none ? -RNNT_NEG_INF : (m - c.label_score[i]) + LN2_F * (__builtin_amdgcn_logf(S) - 15.0f);
+    return make_float2(m, S == 0.0f || c.identity ? 0.0f : c.r.weight[c.row0 + i] / S);
+}
+
+// One wavefront per row
+__global__ __launch_bounds__(256) void k_ce_finish(CeChunk c) {
     const long long i = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (i >= rows) return;
-    const int lane = threadIdx.x & 63, at = r.index[row0 + i];
-    float2* st = stats + (size_t)i * tiles_n;
-    if (at < 0) return;
+    if (i >= c.rows) return;
+    const int lane = threadIdx.x & 63;
+    int at;
+    if (c.identity) {
+        at = (int)i;
+        if (c.r.label[i] == c.ignore) {
+            if (lane == 0) c.loss[at] = 0.0f;
+            return;
+        }
+    } else {
+        at = c.r.index[c.row0 + i];
+        if (at < 0) return;
+    }
+    const float2* st = c.stats + (size_t)i * c.tiles_n;
     float m = RNNT_NEG_INF;
-    for (int t = lane; t < tiles_n; t += 64) m = fmaxf(m, st[t].x);
-    const float M = wave_max(m), c = M == RNNT_NEG_INF ? 0.0f : M;
+    for (int t = lane; t < c.tiles_n; t += 64) m = fmaxf(m, st[t].x);
+    const float M = wave_max(m), z = M == RNNT_NEG_INF ? 0.0f : M;
     float s = 0.0f;
-    for (int t = lane; t < tiles_n; t += 64) s += st[t].y * __builtin_amdgcn_exp2f((st[t].x - c) * LOG2E_F);
+    for (int t = lane; t < c.tiles_n; t += 64) s += st[t].y * __builtin_amdgcn_exp2f((st[t].x - z) * LOG2E_F);
     const float S = wave_sum(s);
     if (lane == 0) {
-        const int y = r.label[row0 + i];
-        // (no entry of the vocabulary is possible, or the label is none of them: +inf)
-        const bool none = S == 0.0f || (unsigned)y >= (unsigned)V;
-        loss[at] = none ? -RNNT_NEG_INF : (c - label_score[i]) + LN2_F * (__builtin_amdgcn_logf(S) - 15.0f);
+        const float2 f = ce_finish_row(c, i, at, M, S);
+        if (c.scale != nullptr) c.scale[i] = f;
     }
-    if (!grads) return;
-    const float w = S == 0.0f ? 0.0f : r.weight[row0 + i] / S;
-    for (int t = lane; t < tiles_n; t += 64) st[t].x = S == 0.0f ? 0.0f : w * __builtin_amdgcn_exp2f((st[t].x - c) * LOG2E_F);
 }
 
-// A workgroup takes 128 rows x 256 columns
-__global__ __launch_bounds__(256) void k_ce_grad(CeRows r, long long row0, void* __restrict__ kept, long long pitch, const float2* __restrict__ stats,
-                                                 int tiles_n, int tile_log2, int V, float* __restrict__ part, long long part_ld) {
+// A workgroup takes R rows x 256 columns.  FINISH: it also forms its rows' sums (those of the first columns write the losses).
+template <bool FINISH>
+__global__ __launch_bounds__(256) void k_ce_grad(CeChunk c, void* __restrict__ kept, long long pitch, float* __restrict__ part, int R) {
     __shared__ __align__(16) float red[8][256];
-    const int nb = (V + 255) / 256, rb = blockIdx.x / nb;
+    __shared__ float2 scale[128];
+    const int nb = (c.V + 255) / 256, rb = blockIdx.x / nb;
     const int tid = threadIdx.x, n0 = (blockIdx.x - rb * nb) * 256, n = n0 + (tid & 31) * 8;
-    const long long r0 = (long long)rb * SUM_ROWS;
-    long long live = (long long)*r.count - row0;
-    if (r0 >= live) return;
-    // rows up to the next multiple of 64 are read by the weight gradient's product: zeros there (their exponentials are finite, their weight 0)
-    live = (live + 63) / 64 * 64;
+    const long long r0 = (long long)rb * R;
+    const CeRows& r = c.r;
+    const long long row0 = c.row0;
+    // rows up to the next multiple of 64 are read by the weight gradient's product: zeros there
+    const long long real_rows = (long long)*r.count - row0, live = (real_rows + 63) / 64 * 64;
+    if (r0 >= live || real_rows <= 0) return;
+    if (tid < R) {
+        float2 f = make_float2(0.0f, 0.0f);
+        if (r0 + tid < real_rows) {
+            if constexpr (FINISH) {
+                const float2* st = c.stats + (size_t)(r0 + tid) * c.tiles_n;
+                float M = RNNT_NEG_INF, S = 0.0f;
+                for (int t = 0; t < c.tiles_n; ++t) M = fmaxf(M, st[t].x);
+                const float z = M == RNNT_NEG_INF ? 0.0f : M;
+                for (int t = 0; t < c.tiles_n; ++t) S += st[t].y * __builtin_amdgcn_exp2f((st[t].x - z) * LOG2E_F);
+                f = ce_finish_row(c, r0 + tid, n0 == 0 ? r.index[row0 + r0 + tid] : -1, M, S);
+            } else f = c.scale[r0 + tid];
+        }
+        scale[tid] = f;
+    }
+    __syncthreads();
     float sum[8] = {};
-    const int t = n >> tile_log2;
-    if (t < tiles_n)
+    const int t = n >> c.tile_log2;
+    if (t < c.tiles_n)
 #pragma unroll 4
-        for (int i = 0; i < SUM_ROWS / 8; ++i) {
-            const long long m = r0 + i * 8 + (tid >> 5);
+        for (int i = 0; i < R / 8; ++i) {
+            const int in = i * 8 + (tid >> 5);
+            const long long m = r0 + in;
             if (m >= live) break;
             f16x8* at = reinterpret_cast<f16x8*>((_Float16*)kept + (size_t)m * pitch + n);
-            const f16x8 h = *at;
-            const float w = r.weight[row0 + m];
-            const bool real = r.index[row0 + m] >= 0;
-            const float f = real ? stats[(size_t)m * tiles_n + t].x : 0.0f;
-            const int y = r.label[row0 + m] - n;
-            float v[8];
+            bf16x8 o = bf16x8{0};
+            if (m < real_rows) {
+                const f16x8 h = *at;
+                const float2 f = scale[in];
+                // (a row without a possible entry has f.y = 0 and parts of -inf; its exponentials are zeros)
+                const float k = f.y * __builtin_amdgcn_exp2f((c.stats[(size_t)m * c.tiles_n + t].x - f.x) * LOG2E_F);
+                const int y = r.label[row0 + m] - n;
+                float v[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                v[j] = real ? (float)h[j] * f : 0.0f;
-                if (y == j) v[j] -= w;
-                sum[j] += v[j];
+                for (int j = 0; j < 8; ++j) v[j] = (float)h[j] * k;
+                if ((unsigned)y < 8u && n + y < c.V) {
+                    const float w = r.weight[row0 + m];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] -= y == j ? w : 0.0f;
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    sum[j] += v[j];
+                    o[j] = (bf16_t)v[j];
+                }
             }
-            bf16x8 o;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = (bf16_t)v[j];
             *reinterpret_cast<bf16x8*>(at) = o;
         }
-    if (part != nullptr) fold_columns(sum, red, part + (size_t)rb * part_ld, n0, V, tid);
+    if (part != nullptr) fold_columns(sum, red, part + (size_t)rb * pitch, n0, c.V, tid);
 }
 
 // fp32: a workgroup per row of scores: maximum and sum of the exponentials in one pass, the gradient in a second one
@@ -366,36 +425,88 @@ __global__ __launch_bounds__(256) void k_ce_rows_f32(CeRows r, long long row0, f
     }
 }
 
-__global__ __launch_bounds__(256) void k_layer_col_sums_f32(const float* __restrict__ x, long long rows, long long ld, int N, float* __restrict__ part) {
+__global__ __launch_bounds__(256) void k_layer_col_sums_f32(const float* __restrict__ x, long long rows, long long ld, int N, float* __restrict__ part,
+                                                            int R) {
     __shared__ __align__(16) float red[8][256];
     const int nb = (N + 255) / 256, rb = blockIdx.x / nb;
     const int tid = threadIdx.x, n0 = (blockIdx.x - rb * nb) * 256, n = n0 + (tid & 31) * 8;
     const int live = ld - n < 8 ? (int)(ld - n) : 8;
-    const long long r0 = (long long)rb * SUM_ROWS;
+    const long long r0 = (long long)rb * R;
     float sum[8] = {};
     if (n < ld)
 #pragma unroll 4
-        for (int i = 0; i < SUM_ROWS / 8; ++i) {
+        for (int i = 0; i < R / 8; ++i) {
             const long long m = r0 + i * 8 + (tid >> 5);
             if (m >= rows) break;
             float v[8];
-            load8(x + (size_t)m * ld + n, live, live == 8, v);
+            load8(x + (size_t)m * ld + n, live, v);
 #pragma unroll
             for (int j = 0; j < 8; ++j) sum[j] += v[j];
         }
     fold_columns(sum, red, part + (size_t)rb * ld, n0, N, tid);
 }
 
-__global__ __launch_bounds__(256) void k_ce_scatter_f32(CeRows r, long long row0, long long rows, const float* __restrict__ src, long long ld, int D,
-                                                        float* __restrict__ dx) {
-    const long long i = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (i >= rows) return;
-    const int at = r.index[row0 + i];
-    if (at < 0) return;
-    for (int c = threadIdx.x & 63; c < D; c += 64) dx[(size_t)at * D + c] = src[(size_t)i * ld + c];
+// One workgroup: a fixed order; partial sums in fp64 (a sum of many losses of one size)
+__global__ __launch_bounds__(1024) void k_ce_total(const float* __restrict__ loss, const float* __restrict__ weight, long long R, float* __restrict__ total) {
+    __shared__ double part[16];
+    double s = 0.0;
+#pragma unroll 8
+    for (long long i = threadIdx.x; i < R; i += 1024) {
+        const float w = weight != nullptr ? weight[i] : 1.0f;
+        if (w != 0.0f) s += (double)w * (double)loss[i];
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double t = 0.0;
+        for (int w = 0; w < 16; ++w) t += part[w];
+        *total = (float)t;
+    }
+}
+
+struct ScaleArgs {
+    void* p[3];
+    long long n[3];
+    bool bf16[3];
+};
+__global__ __launch_bounds__(256) void k_layer_scale(const float* __restrict__ factor, ScaleArgs a) {
+    const float f = *factor;
+    if (f == 1.0f) return;
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+        for (long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 8; i < a.n[k]; i += (long long)gridDim.x * 2048) {
+            const int live = a.n[k] - i < 8 ? (int)(a.n[k] - i) : 8;
+            float v[8];
+            if (a.bf16[k]) load8((const bf16_t*)a.p[k] + i, live, v);
+            else load8((const float*)a.p[k] + i, live, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] *= f;
+            if (a.bf16[k]) store8((bf16_t*)a.p[k] + i, live, v);
+            else store8((float*)a.p[k] + i, live, v);
+        }
 }
 
 }  // namespace
+
+hipError_t launch_ce_total(const float* loss, const float* weight, long long R, float* total, hipStream_t stream) {
+    k_ce_total<<<dim3(1), dim3(1024), 0, stream>>>(loss, weight, R, total);
+    return hipGetLastError();
+}
+hipError_t launch_scale(const float* factor, void* const (&p)[3], const long long (&n)[3], const bool (&bf16)[3], hipStream_t stream) {
+    ScaleArgs a;
+    long long most = 0;
+    for (int k = 0; k < 3; ++k) {
+        a.p[k] = p[k];
+        a.n[k] = n[k];
+        a.bf16[k] = bf16[k];
+        most = std::max(most, n[k]);
+    }
+    if (most == 0) return hipSuccess;
+    k_layer_scale<<<dim3((unsigned)std::min<long long>(2048, (most + 2047) / 2048)), dim3(256), 0, stream>>>(factor, a);
+    return hipGetLastError();
+}
 
 hipError_t launch_pad(const void* src, int size, long long rows, long long cols, long long r0, void* dst, long long rows_to, long long ld_to,
                       hipStream_t stream) {
@@ -409,63 +520,73 @@ hipError_t launch_pad(const void* src, int size, long long rows, long long cols,
 }
 
 hipError_t launch_dz(bool bf16, const DzArgs& a, hipStream_t stream) {
-    const long long n = (std::max(a.M, a.rows_to) + SUM_ROWS - 1) / SUM_ROWS * ((a.ld + 255) / 256);
+    const int R = sum_rows(a.M, a.N);
+    const long long n = (std::max(a.M, a.rows_to) + R - 1) / R * ((a.ld + 255) / 256);
     if (!grid_fits(n)) return hipErrorInvalidValue;
     const dim3 grid((unsigned)n);
-    if (bf16) k_layer_dz<bf16_t, _Float16><<<grid, dim3(256), 0, stream>>>(a);
-    else k_layer_dz<float, float><<<grid, dim3(256), 0, stream>>>(a);
+    if (bf16) k_layer_dz<bf16_t, _Float16><<<grid, dim3(256), 0, stream>>>(a, R);
+    else k_layer_dz<float, float><<<grid, dim3(256), 0, stream>>>(a, R);
     return hipGetLastError();
 }
 
-hipError_t launch_sum_parts(const float* part, int blocks, long long ld, int N, const int* count, long long row0, const float* prev, void* out,
-                            bool bf16, hipStream_t stream) {
-    if (N <= 0) return hipSuccess;
-    const dim3 grid(blocks_of(N, 32));
-    if (bf16) k_layer_sum_parts<bf16_t><<<grid, dim3(256), 0, stream>>>(part, blocks, ld, N, count, row0, prev, (bf16_t*)out);
-    else k_layer_sum_parts<float><<<grid, dim3(256), 0, stream>>>(part, blocks, ld, N, count, row0, prev, (float*)out);
+hipError_t launch_sum_parts(const SumJob& j, hipStream_t stream) {
+    if (j.N <= 0 || j.part == nullptr) return hipSuccess;
+    k_layer_sum_parts<<<dim3(blocks_of(j.N, 32)), dim3(256), 0, stream>>>(j, (int)sum_blocks(j.rows, j.N), sum_rows(j.rows, j.N));
     return hipGetLastError();
 }
 
-hipError_t launch_linear_rows_f32(const float* z, long long ld, const float* bias, const float* residual, float* y, float* saved, long long M, int N,
-                                  int act, const Dropout& drop, hipStream_t stream) {
+hipError_t launch_linear_rows_f32(const float* z, long long ld, int splits, long long stride, const float* bias, const float* residual, float* y,
+                                  float* saved, long long M, int N, int act, const Dropout& drop, hipStream_t stream) {
     const long long groups = (N + 7) / 8, total = M * groups;
     if (total <= 0) return hipSuccess;
     if (!grid_fits((total + 255) / 256)) return hipErrorInvalidValue;
-    k_linear_rows_f32<<<dim3(blocks_of(total, 256)), dim3(256), 0, stream>>>(z, ld, bias, residual, y, saved, M, N, act, drop, groups, total);
+    k_linear_rows_f32<<<dim3(blocks_of(total, 256)), dim3(256), 0, stream>>>(z, ld, splits, stride, bias, residual, y, saved, M, N, act, drop, groups,
+                                                                             total);
     return hipGetLastError();
 }
-hipError_t launch_crop_f32(const float* src, long long ld, float* dst, long long rows, int N, bool add, hipStream_t stream) {
-    const long long total = rows * N;
+hipError_t launch_reduce_f32(const float* src, long long ld, int splits, long long stride, const int* row_map, float* dst, long long rows, int N, bool add,
+                             hipStream_t stream) {
+    const long long groups = (N + 7) / 8, total = rows * groups;
     if (total <= 0) return hipSuccess;
-    k_layer_crop_f32<<<dim3((unsigned)std::min<long long>((total + 255) / 256, 16384)), dim3(256), 0, stream>>>(src, ld, dst, N, total, add);
+    if (!grid_fits((total + 255) / 256)) return hipErrorInvalidValue;
+    k_layer_reduce_f32<<<dim3(blocks_of(total, 256)), dim3(256), 0, stream>>>(src, ld, splits, stride, row_map, dst, N, add, groups, total);
     return hipGetLastError();
 }
 
-hipError_t launch_ce_rows(const int* labels, const float* weight, long long R, int ignore, long long cap, const CeRows& r, hipStream_t stream) {
-    k_ce_rows<<<dim3(blocks_of(R, SCAN_ROWS)), dim3(SCAN_THREADS), 0, stream>>>(labels, weight, R, ignore, cap, r);
+namespace {
+template <typename T>
+hipError_t gather(const void* x, long long R, int D, const int* labels, const float* weight, int ignore, long long cap, int* place, const CeRows& r, void* xp,
+                  long long ld, long long fill_to, float* loss, void* dx, hipStream_t stream) {
+    const unsigned row_wgs = blocks_of(R, GATHER_ROWS), fill_wgs = (unsigned)std::min<long long>(256, blocks_of(std::max(256LL, fill_to), 16));
+    const dim3 grid(row_wgs + fill_wgs);
+    if (R <= GATHER_SCAN) {
+        k_ce_gather<T, true><<<grid, dim3(256), 0, stream>>>((const T*)x, R, D, labels, weight, ignore, cap, nullptr, r, (T*)xp, ld, fill_to, loss, (T*)dx,
+                                                             (int)row_wgs);
+    } else {
+        k_ce_rows<<<dim3(blocks_of(R, SCAN_ROWS)), dim3(SCAN_THREADS), 0, stream>>>(labels, weight, R, ignore, cap, place, r);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        k_ce_gather<T, false><<<grid, dim3(256), 0, stream>>>((const T*)x, R, D, labels, weight, ignore, cap, place, r, (T*)xp, ld, fill_to, loss, (T*)dx,
+                                                              (int)row_wgs);
+    }
     return hipGetLastError();
 }
-hipError_t launch_ce_gather(const void* x, int size, long long R, int D, const CeRows& r, void* xp, long long ld, long long fill_to, float* loss, void* dx,
-                            hipStream_t stream) {
-    const bool vec = ((size_t)D * size) % 16 == 0;
-    const dim3 grid(blocks_of(R + std::max(256LL, fill_to), 4));
-    if (size == 2)
-        k_ce_gather<unsigned short><<<grid, dim3(256), 0, stream>>>((const unsigned short*)x, R, D, r, (unsigned short*)xp, ld, fill_to, loss,
-                                                                    (unsigned short*)dx, vec);
-    else k_ce_gather<unsigned><<<grid, dim3(256), 0, stream>>>((const unsigned*)x, R, D, r, (unsigned*)xp, ld, fill_to, loss, (unsigned*)dx, vec);
+}  // namespace
+hipError_t launch_ce_gather(const void* x, int size, long long R, int D, const int* labels, const float* weight, int ignore, long long cap, int* place,
+                            const CeRows& r, void* xp, long long ld, long long fill_to, float* loss, void* dx, hipStream_t stream) {
+    return size == 2 ? gather<unsigned short>(x, R, D, labels, weight, ignore, cap, place, r, xp, ld, fill_to, loss, dx, stream)
+                     : gather<unsigned>(x, R, D, labels, weight, ignore, cap, place, r, xp, ld, fill_to, loss, dx, stream);
+}
+hipError_t launch_ce_finish(const CeChunk& c, hipStream_t stream) {
+    k_ce_finish<<<dim3(blocks_of(c.rows, 4)), dim3(256), 0, stream>>>(c);
     return hipGetLastError();
 }
-hipError_t launch_ce_finish(const CeRows& r, long long row0, long long rows, const float* label_score, float2* stats, int tiles_n, int V, float* loss,
-                            bool grads, hipStream_t stream) {
-    k_ce_finish<<<dim3(blocks_of(rows, 4)), dim3(256), 0, stream>>>(r, row0, rows, label_score, stats, tiles_n, V, loss, grads);
-    return hipGetLastError();
-}
-hipError_t launch_ce_grad(const CeRows& r, long long row0, long long rows, void* kept, long long pitch, const float2* stats, int tiles_n, int tile, int V,
-                          float* part, hipStream_t stream) {
-    const long long n = (long long)blocks_of(V, 256) * blocks_of(rows, SUM_ROWS);
+hipError_t launch_ce_grad(const CeChunk& c, void* kept, long long pitch, float* part, hipStream_t stream) {
+    const int R = sum_rows(c.rows, c.V);
+    const long long n = (long long)blocks_of(c.V, 256) * sum_blocks(c.rows, c.V);
     if (!grid_fits(n)) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)n);
-    k_ce_grad<<<grid, dim3(256), 0, stream>>>(r, row0, kept, pitch, stats, tiles_n, tile == 256 ? 8 : 7, V, part, pitch);
+    if (ce_grad_finishes(c.tiles_n)) k_ce_grad<true><<<dim3((unsigned)n), dim3(256), 0, stream>>>(c, kept, pitch, part, R);
+    else k_ce_grad<false><<<dim3((unsigned)n), dim3(256), 0, stream>>>(c, kept, pitch, part, R);
     return hipGetLastError();
 }
 hipError_t launch_ce_rows_f32(const CeRows& r, long long row0, long long rows, float* scores, long long ld, int V, const float* b, float* loss,
@@ -474,15 +595,11 @@ hipError_t launch_ce_rows_f32(const CeRows& r, long long row0, long long rows, f
     return hipGetLastError();
 }
 hipError_t launch_col_sums_f32(const float* x, long long rows, long long ld, int N, float* part, hipStream_t stream) {
-    const long long n = (long long)blocks_of(N, 256) * blocks_of(rows, SUM_ROWS);
+    const int R = sum_rows(rows, N);
+    const long long n = (long long)blocks_of(N, 256) * sum_blocks(rows, N);
     if (!grid_fits(n)) return hipErrorInvalidValue;
     const dim3 grid((unsigned)n);
-    k_layer_col_sums_f32<<<grid, dim3(256), 0, stream>>>(x, rows, ld, N, part);
+    k_layer_col_sums_f32<<<grid, dim3(256), 0, stream>>>(x, rows, ld, N, part, R);
     return hipGetLastError();
 }
-hipError_t launch_scatter_f32(const CeRows& r, long long row0, long long rows, const float* src, long long ld, int D, float* dx, hipStream_t stream) {
-    k_ce_scatter_f32<<<dim3(blocks_of(rows, 4)), dim3(256), 0, stream>>>(r, row0, rows, src, ld, D, dx);
-    return hipGetLastError();
-}
-
 }  // namespace rnnt

@@ -47,6 +47,19 @@ struct Carver {
 };
 bool workspace_ok(const void* ws, size_t have, size_t need) { return need == 0 || (ws != nullptr && (uintptr_t)ws % 256 == 0 && have >= need); }
 
+// fp32 products: two workgroups of 128 x 128 per compute unit, so a sum over k is cut into as many parts as make 512 of them, each at least 64 deep
+// (2048 x 512 out of a depth of 4096: 180 us in one part, 64 workgroups); at most 16384 deep, so that its rounding does not grow with it.  Parts are
+// stored apart and added in order.
+int splits_f32(long long M, long long N, long long K) {
+    const double tiles = (double)((M + 127) / 128) * (double)((N + 127) / 128);
+    long long s = tiles >= 512.0 ? 1 : (long long)(512.0 / std::max(1.0, tiles));
+    s = std::min(s, std::max(1LL, K / 64));
+    while (s > 1 && (double)s * (double)M * (double)N * 4.0 > (double)SLOT_CAP) --s;
+    s = std::max(s, (K + 16383) / 16384);
+    return K > 0 ? gemm_f32_split_count(K, (int)s) : 1;
+}
+size_t slots_f32(int splits, long long rows, long long ld) { return (size_t)splits * (size_t)rows * (size_t)ld * 4; }
+
 // ---- linear -------------------------------------------------------------------------------------------------------------
 rnnt_status check_linear(const rnnt_linear_desc* d, bool backward) {
     if (!d) return RNNT_ERR_NULL;
@@ -69,10 +82,14 @@ Dropout make_dropout(const rnnt_linear_desc& d, const uint64_t* rng) {
 // Where the operands of the products lie.  bf16: rows of 64 elements' multiples along a contiguous contraction, 8 along the other index, else a padded copy.
 struct LinearPlan {
     bool bf16, backward;
+    bool few;                             // forward pass of at most FEW_ROWS rows: one launch on the arrays as they are
+    int few_splits;
     bool copy_x, copy_w, own_dz;
     long long Kp, Np, Mp;                 // pitches of the copies and of dz; rows of dz
-    size_t off_x, off_w, off_dz, off_xt, off_dyt, off_part, off_slots, off_out, bytes;
-    GemmPlan y, dx, dw;
+    size_t off_x, off_w, off_dz, off_xt, off_dyt, off_part, off_slots, off_slots_w, bytes;
+    GemmPlan y;
+    PairPlan grads;
+    int y32, dx32, dw32;                  // fp32: parts of the three sums
 };
 LinearPlan plan_linear(const rnnt_linear_desc& d, bool backward) {
     LinearPlan p{};
@@ -86,7 +103,11 @@ LinearPlan plan_linear(const rnnt_linear_desc& d, bool backward) {
         p.Kp = up(K, 64);
         p.Np = up(N, 64);
         p.Mp = up(M, 64);
-        if (!backward) {
+        if (!backward && M <= FEW_ROWS) {
+            p.few = true;
+            p.few_splits = few_splits(M, d.K, d.N);
+            p.off_slots = c.take(p.few_splits > 1 ? (size_t)p.few_splits * M * up(N, 8) * 4 : 0);
+        } else if (!backward) {
             p.copy_x = K % 64 != 0;
             p.copy_w = K % 64 != 0 || N % 8 != 0;
             p.y = plan_gemm(M, N, (int)(p.Kp / 64), SLOT_CAP);
@@ -97,15 +118,15 @@ LinearPlan plan_linear(const rnnt_linear_desc& d, bool backward) {
             p.own_dz = !plain || N % 64 != 0;
             p.copy_x = K % 8 != 0;
             p.copy_w = N % 64 != 0;
-            p.dx = plan_gemm(M, K, (int)(p.Np / 64), SLOT_CAP);
-            p.dw = plan_gemm(K, N, (int)(p.Mp / 64), SLOT_CAP);
+            p.grads = plan_pair(M, K, (int)(p.Np / 64), K, N, (int)(p.Mp / 64), SLOT_CAP);
             p.off_dz = c.take(p.own_dz ? (size_t)p.Mp * p.Np * 2 : 0);
             p.off_x = c.take(p.copy_x ? (size_t)p.Mp * p.Kp * 2 : 0);
             p.off_w = c.take(p.copy_w ? (size_t)K * p.Np * 2 : 0);
             p.off_xt = c.take(!p.copy_x && M % 64 != 0 ? (size_t)64 * K * 2 : 0);
             p.off_dyt = c.take(!p.own_dz && M % 64 != 0 ? (size_t)64 * N * 2 : 0);
-            p.off_part = c.take((size_t)((M + SUM_ROWS - 1) / SUM_ROWS) * p.Np * 4);
-            p.off_slots = c.take(std::max(gemm_slot_bytes(p.dx, M, K), gemm_slot_bytes(p.dw, K, N)));
+            p.off_part = c.take((size_t)sum_capacity(M, N) * p.Np * 4);
+            p.off_slots = c.take(gemm_slot_bytes(p.grads.dx, M, K));
+            p.off_slots_w = c.take(gemm_slot_bytes(p.grads.dw, K, N));
         }
     } else {
         p.Kp = up(K, 4);
@@ -115,23 +136,29 @@ LinearPlan plan_linear(const rnnt_linear_desc& d, bool backward) {
         p.off_x = c.take(p.copy_x ? (size_t)M * p.Kp * e : 0);
         p.off_w = c.take(p.copy_w ? (size_t)p.Kp * p.Np * e : 0);
         if (!backward) {
-            p.off_out = c.take(N % 4 != 0 ? (size_t)M * p.Np * e : 0);
+            p.y32 = splits_f32(M, p.Np, p.Kp);
+            p.off_slots = c.take(p.y32 > 1 || N % 4 != 0 ? slots_f32(p.y32, M, p.Np) : 0);
         } else {
             p.own_dz = !plain || N % 4 != 0;
             p.off_dz = c.take(p.own_dz ? (size_t)M * p.Np * e : 0);
-            p.off_part = c.take((size_t)((M + SUM_ROWS - 1) / SUM_ROWS) * p.Np * 4);
-            p.off_out = c.take(p.copy_w ? (size_t)p.Kp * p.Np * e : 0);
+            p.off_part = c.take((size_t)sum_capacity(M, N) * p.Np * 4);
+            p.dx32 = splits_f32(M, K, p.Np);
+            p.dw32 = splits_f32(p.Kp, p.Np, M);
+            p.off_slots = c.take(std::max(p.dx32 > 1 ? slots_f32(p.dx32, M, K) : 0, slots_f32(p.dw32, p.Kp, p.Np)));
         }
     }
     p.bytes = c.bytes;
     return p;
 }
 
-const RowMask NO_MASK{nullptr, 1, 0};
-
 rnnt_status linear_fwd_bf16(const rnnt_linear_desc& d, const LinearPlan& p, const void* x, const void* W, const float* b, const void* residual,
                             const Dropout& drop, void* y, void* saved, unsigned char* ws, hipStream_t stream) {
     const long long M = d.M, K = d.K, N = d.N;
+    const LinearEpilogue e{b, residual, y, saved, d.activation, drop, M, d.N};
+    if (p.few) {
+        LAYER_HIP(launch_few_linear(FewJob{x, W, (int)M, d.K, d.N}, p.few_splits, (float*)(ws + p.off_slots), e, stream));
+        return RNNT_OK;
+    }
     if (p.copy_x) LAYER_HIP(launch_pad(x, 2, M, K, 0, ws + p.off_x, M, p.Kp, stream));
     if (p.copy_w) LAYER_HIP(launch_pad(W, 2, K, N, 0, ws + p.off_w, p.Kp, p.Np, stream));
     GemmJob g{};
@@ -141,7 +168,6 @@ rnnt_status linear_fwd_bf16(const rnnt_linear_desc& d, const LinearPlan& p, cons
     g.N = N;
     g.b_rows = p.copy_w ? p.Np : N;
     g.stages = (int)(p.Kp / 64);
-    const LinearEpilogue e{b, residual, y, saved, d.activation, drop, M, d.N, N % 8 == 0};
     LAYER_HIP(launch_linear_gemm(g, p.y, (float*)(ws + p.off_slots), e, stream));
     return RNNT_OK;
 }
@@ -152,24 +178,23 @@ rnnt_status linear_bwd_bf16(const rnnt_linear_desc& d, const LinearPlan& p, cons
     float* part = (float*)(ws + p.off_part);
     if (M > 0 && (db || (p.own_dz && (dx || dW)))) {
         const DzArgs a{dy, d.activation == ACT_NONE ? nullptr : saved, p.own_dz ? ws + p.off_dz : nullptr, db ? part : nullptr, M,
-                       p.own_dz ? p.Mp : M, d.N, p.Np, d.activation, drop, N % 8 == 0};
+                       p.own_dz ? p.Mp : M, d.N, p.Np, d.activation, drop};
         LAYER_HIP(launch_dz(true, a, stream));
     }
-    if (db)
-        LAYER_HIP(launch_sum_parts(part, (int)((M + SUM_ROWS - 1) / SUM_ROWS), p.Np, d.N, nullptr, 0, d.accumulate_params ? (const float*)db : nullptr, db,
-                                   (d.param_grads_bf16 & 2) != 0, stream));
     const void* dz = p.own_dz ? ws + p.off_dz : dy;
     const long long ld_dz = p.own_dz ? p.Np : N;
+    GradGemm gx{}, gw{};
     if (dx && M > 0) {
         if (p.copy_w) LAYER_HIP(launch_pad(W, 2, K, N, 0, ws + p.off_w, K, p.Np, stream));
-        GemmJob g{};
-        g.A = GemmOperand{dz, ld_dz, nullptr, -1};
-        g.B = GemmOperand{p.copy_w ? ws + p.off_w : W, p.copy_w ? p.Np : N, nullptr, -1};
-        g.M = g.a_rows = M;
-        g.N = g.b_rows = K;
-        g.stages = (int)(p.Np / 64);
-        const StoreEpilogue e{dx, nullptr, nullptr, K, 0, M, d.K, true, K % 8 == 0};
-        LAYER_HIP(launch_store_gemm(false, g, p.dx, (float*)(ws + p.off_slots), e, stream));
+        gx.g.A = GemmOperand{dz, ld_dz, nullptr, -1};
+        gx.g.B = GemmOperand{p.copy_w ? ws + p.off_w : W, p.copy_w ? p.Np : N, nullptr, -1};
+        gx.g.M = gx.g.a_rows = M;
+        gx.g.N = gx.g.b_rows = K;
+        gx.g.stages = (int)(p.Np / 64);
+        gx.splits = p.grads.dx.splits;
+        gx.per_split = p.grads.dx.per_split;
+        gx.slots = (float*)(ws + p.off_slots);
+        gx.e = StoreEpilogue{dx, nullptr, nullptr, K, 0, M, d.K, true};
     }
     if (dW) {
         const bool ragged = M % 64 != 0;
@@ -177,17 +202,20 @@ rnnt_status linear_bwd_bf16(const rnnt_linear_desc& d, const LinearPlan& p, cons
         if (p.copy_x) LAYER_HIP(launch_pad(x, 2, M, K, 0, ws + p.off_x, p.Mp, p.Kp, stream));
         else if (ragged) LAYER_HIP(launch_pad(x, 2, M, K, whole, ws + p.off_xt, 64, K, stream));
         if (!p.own_dz && ragged) LAYER_HIP(launch_pad(dy, 2, M, N, whole, ws + p.off_dyt, 64, N, stream));
-        GemmJob g{};
-        g.A = GemmOperand{p.copy_x ? ws + p.off_x : x, p.copy_x ? p.Kp : K, !p.copy_x && ragged ? ws + p.off_xt : nullptr, (int)(whole / 64)};
-        g.B = GemmOperand{dz, ld_dz, !p.own_dz && ragged ? ws + p.off_dyt : nullptr, (int)(whole / 64)};
-        g.M = K;
-        g.a_rows = p.copy_x ? p.Kp : K;
-        g.N = N;
-        g.b_rows = ld_dz;
-        g.stages = (int)(p.Mp / 64);
-        const StoreEpilogue e{dW, d.accumulate_params ? (const float*)dW : nullptr, nullptr, N, 0, K, d.N, (d.param_grads_bf16 & 1) != 0, N % 8 == 0};
-        LAYER_HIP(launch_store_gemm(true, g, p.dw, (float*)(ws + p.off_slots), e, stream));
+        gw.g.A = GemmOperand{p.copy_x ? ws + p.off_x : x, p.copy_x ? p.Kp : K, !p.copy_x && ragged ? ws + p.off_xt : nullptr, (int)(whole / 64)};
+        gw.g.B = GemmOperand{dz, ld_dz, !p.own_dz && ragged ? ws + p.off_dyt : nullptr, (int)(whole / 64)};
+        gw.g.M = K;
+        gw.g.a_rows = p.copy_x ? p.Kp : K;
+        gw.g.N = N;
+        gw.g.b_rows = ld_dz;
+        gw.g.stages = (int)(p.Mp / 64);
+        gw.splits = p.grads.dw.splits;
+        gw.per_split = p.grads.dw.per_split;
+        gw.slots = (float*)(ws + p.off_slots_w);
+        gw.e = StoreEpilogue{dW, d.accumulate_params ? (const float*)dW : nullptr, nullptr, N, 0, K, d.N, (d.param_grads_bf16 & 1) != 0};
     }
+    const SumJob sum{db ? part : nullptr, M, p.Np, d.N, nullptr, 0, d.accumulate_params ? (const float*)db : nullptr, db, (d.param_grads_bf16 & 2) != 0};
+    LAYER_HIP(launch_grad_gemms(p.grads.tile, gx, gw, sum, stream));
     return RNNT_OK;
 }
 
@@ -196,10 +224,10 @@ rnnt_status linear_fwd_f32(const rnnt_linear_desc& d, const LinearPlan& p, const
     const long long M = d.M, K = d.K, N = d.N;
     if (p.copy_x) LAYER_HIP(launch_pad(x, 4, M, K, 0, ws + p.off_x, M, p.Kp, stream));
     if (p.copy_w) LAYER_HIP(launch_pad(W, 4, K, N, 0, ws + p.off_w, p.Kp, p.Np, stream));
-    float* z = N % 4 != 0 ? (float*)(ws + p.off_out) : saved ? saved : y;
-    LAYER_HIP(launch_gemm_f32_masked(0, 1, p.copy_x ? (const float*)(ws + p.off_x) : x, p.Kp, NO_MASK, p.copy_w ? (const float*)(ws + p.off_w) : W, p.Np,
-                                     NO_MASK, z, p.Np, nullptr, 0, M, p.Np, p.Kp, 1, stream));
-    LAYER_HIP(launch_linear_rows_f32(z, p.Np, b, residual, y, saved, M, d.N, d.activation, drop, stream));
+    float* z = p.y32 > 1 || N % 4 != 0 ? (float*)(ws + p.off_slots) : saved ? saved : y;
+    LAYER_HIP(launch_gemm_f32_split(0, 1, p.copy_x ? (const float*)(ws + p.off_x) : x, p.Kp, p.copy_w ? (const float*)(ws + p.off_w) : W, p.Np, z, p.Np, M,
+                                    p.Np, p.Kp, p.y32, M * p.Np, stream));
+    LAYER_HIP(launch_linear_rows_f32(z, p.Np, p.y32, M * p.Np, b, residual, y, saved, M, d.N, d.activation, drop, stream));
     return RNNT_OK;
 }
 
@@ -209,25 +237,27 @@ rnnt_status linear_bwd_f32(const rnnt_linear_desc& d, const LinearPlan& p, const
     float* part = (float*)(ws + p.off_part);
     if (M > 0 && (db || (p.own_dz && (dx || dW)))) {
         const DzArgs a{dy, d.activation == ACT_NONE ? nullptr : saved, p.own_dz ? ws + p.off_dz : nullptr, db ? part : nullptr, M, M, d.N, p.Np,
-                       d.activation, drop, N % 4 == 0};
+                       d.activation, drop};
         LAYER_HIP(launch_dz(false, a, stream));
     }
     if (db)
-        LAYER_HIP(launch_sum_parts(part, (int)((M + SUM_ROWS - 1) / SUM_ROWS), p.Np, d.N, nullptr, 0, d.accumulate_params ? db : nullptr, db, false,
-                                   stream));
+        LAYER_HIP(launch_sum_parts(SumJob{part, M, p.Np, d.N, nullptr, 0, d.accumulate_params ? db : nullptr, db, false}, stream));
     const float* dz = p.own_dz ? (const float*)(ws + p.off_dz) : dy;
     if (p.copy_w && dx && M > 0) LAYER_HIP(launch_pad(W, 4, K, N, 0, ws + p.off_w, p.Kp, p.Np, stream));
-    if (dx && M > 0)
-        LAYER_HIP(launch_gemm_f32_masked(0, 0, dz, p.Np, NO_MASK, p.copy_w ? (const float*)(ws + p.off_w) : W, p.Np, NO_MASK, dx, K, nullptr, 0, M, K,
-                                         p.Np, 1, stream));
-    if (dW) {
+    float* slots = (float*)(ws + p.off_slots);
+    if (dx && M > 0) {
+        LAYER_HIP(launch_gemm_f32_split(0, 0, dz, p.Np, p.copy_w ? (const float*)(ws + p.off_w) : W, p.Np, p.dx32 > 1 ? slots : dx, K, M, K, p.Np, p.dx32,
+                                        M * K, stream));
+        if (p.dx32 > 1) LAYER_HIP(launch_reduce_f32(slots, K, p.dx32, M * K, nullptr, dx, M, d.K, false, stream));
+    }
+    if (dW && M == 0) {
+        if (!d.accumulate_params) LAYER_HIP(launch_pad(nullptr, 4, 0, 0, 0, dW, K, N, stream));
+    } else if (dW) {
         if (p.copy_x) LAYER_HIP(launch_pad(x, 4, M, K, 0, ws + p.off_x, M, p.Kp, stream));
-        float* out = p.copy_w ? (float*)(ws + p.off_out) : dW;
-        if (p.copy_w || !d.accumulate_params) LAYER_HIP(launch_pad(nullptr, 4, 0, 0, 0, out, p.Kp, p.Np, stream));
-        if (M > 0)
-            LAYER_HIP(launch_gemm_f32_masked(1, 1, p.copy_x ? (const float*)(ws + p.off_x) : x, p.Kp, NO_MASK, dz, p.Np, NO_MASK, out, p.Np, nullptr, 1,
-                                             p.Kp, p.Np, M, k_splits_f32(p.Kp, p.Np, M), stream));
-        if (p.copy_w) LAYER_HIP(launch_crop_f32(out, p.Np, dW, K, d.N, d.accumulate_params != 0, stream));
+        const bool direct = p.dw32 == 1 && !p.copy_w && !d.accumulate_params;
+        LAYER_HIP(launch_gemm_f32_split(1, 1, p.copy_x ? (const float*)(ws + p.off_x) : x, p.Kp, dz, p.Np, direct ? dW : slots, p.Np, p.Kp, p.Np, M, p.dw32,
+                                        p.Kp * p.Np, stream));
+        if (!direct) LAYER_HIP(launch_reduce_f32(slots, p.Np, p.dw32, p.Kp * p.Np, nullptr, dW, K, d.N, d.accumulate_params != 0, stream));
     }
     return RNNT_OK;
 }
@@ -245,12 +275,15 @@ rnnt_status check_ce(const rnnt_ce_desc* d, bool grads) {
 }
 
 struct CePlan {
-    bool bf16, grads, copy_w, copy_out;
+    bool bf16, grads, copy_w;
+    bool few;                             // at most FEW_ROWS rows: scores by one launch on W as it is
+    bool identity;                        // ... and without gradients on x as it is
     long long cap, chunk, Dp, Vp, pitch;  // rows (a multiple of 256) in all and per chunk; padded widths; elements of a chunk row
-    int chunks, tile, tiles_n;
-    size_t off_count, off_index, off_label, off_weight, off_place, off_x, off_w, off_chunk, off_score, off_stats, off_part, off_slots, off_acc, off_dbacc,
-        off_dx, off_out, bytes;
-    GemmPlan dx, dw;
+    int chunks, tile, tile_log2, tiles_n;
+    size_t off_count, off_index, off_label, off_weight, off_place, off_x, off_w, off_chunk, off_score, off_stats, off_scale, off_part, off_slots, off_slots_w, off_acc,
+        off_dbacc, bytes;
+    PairPlan pair;
+    int dx32, dw32;                       // fp32: parts of the gradients' sums
 };
 CePlan plan_ce_chunk(const rnnt_ce_desc& d, bool grads, long long chunk) {
     CePlan p{};
@@ -264,28 +297,42 @@ CePlan plan_ce_chunk(const rnnt_ce_desc& d, bool grads, long long chunk) {
     p.Dp = up(D, p.bf16 ? 64 : 4);
     p.Vp = up(V, p.bf16 ? 64 : 4);
     p.copy_w = p.Dp != D || p.Vp != V;
-    p.copy_out = !p.bf16 && p.copy_w;
+    p.few = p.bf16 && R <= FEW_ROWS;
+    p.identity = p.few && !grads;
     Carver c;
+    if (p.identity) {
+        p.copy_w = false;
+        p.tile = FEW_TILE;
+        p.tile_log2 = 5;
+        p.tiles_n = (int)((V + FEW_TILE - 1) / FEW_TILE);
+        p.off_score = c.take((size_t)FEW_ROWS * 4);
+        p.off_stats = c.take((size_t)R * p.tiles_n * 8);
+        p.bytes = c.bytes;
+        return p;
+    }
     p.off_count = c.take(4);
     p.off_index = c.take((size_t)p.cap * 4);
     p.off_label = c.take((size_t)p.cap * 4);
     p.off_weight = c.take((size_t)p.cap * 4);
-    p.off_place = c.take((size_t)p.cap * 4);
+    p.off_place = c.take(R > GATHER_SCAN ? (size_t)p.cap * 4 : 0);
     p.off_x = c.take((size_t)p.cap * p.Dp * e);
     p.off_w = c.take(p.copy_w ? (size_t)p.Dp * p.Vp * e : 0);
     if (p.bf16) {
         // (a row is 128 bytes longer than whole tiles: rows of a power-of-two length would all start in the same memory channel)
         p.pitch = up(V, 256) + 64;
-        p.tile = plan_gemm(p.chunk, V, (int)(p.Dp / 64), 0).tile;
-        p.tiles_n = (int)((V + p.tile - 1) / p.tile);
+        p.tile = p.few ? FEW_TILE : plan_gemm(p.chunk, V, (int)(p.Dp / 64), 0).tile;
+        p.tile_log2 = p.few ? 5 : p.tile == 256 ? 8 : 7;
+        // (few: the columns of zeros up to Vp have parts of their own)
+        p.tiles_n = (int)(((p.few ? p.Vp : V) + p.tile - 1) / p.tile);
         p.off_score = c.take((size_t)p.chunk * 4);
         p.off_stats = c.take((size_t)p.chunk * p.tiles_n * 8);
+        p.off_scale = c.take((size_t)p.chunk * 8);
         if (grads) {
             p.off_chunk = c.take((size_t)p.chunk * p.pitch * 2);
-            p.off_part = c.take((size_t)(p.chunk / SUM_ROWS) * p.pitch * 4);
-            p.dx = plan_gemm(p.chunk, D, (int)(p.Vp / 64), SLOT_CAP);
-            p.dw = plan_gemm(D, V, (int)(p.chunk / 64), SLOT_CAP);
-            p.off_slots = c.take(std::max(gemm_slot_bytes(p.dx, p.chunk, D), gemm_slot_bytes(p.dw, D, V)));
+            p.off_part = c.take((size_t)sum_capacity(p.chunk, V) * p.pitch * 4);
+            p.pair = plan_pair(p.chunk, D, (int)(p.Vp / 64), D, V, (int)(p.chunk / 64), SLOT_CAP);
+            p.off_slots = c.take(gemm_slot_bytes(p.pair.dx, p.chunk, D));
+            p.off_slots_w = c.take(gemm_slot_bytes(p.pair.dw, D, V));
             // the weight gradient's sum over the chunks, where its output is bfloat16
             p.off_acc = c.take(p.chunks > 1 && (d.param_grads_bf16 & 1) ? (size_t)D * V * 4 : 0);
             p.off_dbacc = c.take(p.chunks > 1 ? (size_t)V * 4 : 0);
@@ -294,9 +341,10 @@ CePlan plan_ce_chunk(const rnnt_ce_desc& d, bool grads, long long chunk) {
         p.pitch = p.Vp;
         p.off_chunk = c.take((size_t)p.chunk * p.pitch * 4);
         if (grads) {
-            p.off_part = c.take((size_t)(p.chunk / SUM_ROWS) * p.pitch * 4);
-            p.off_dx = c.take((size_t)p.chunk * D * 4);
-            p.off_out = c.take(p.copy_out ? (size_t)p.Dp * p.Vp * 4 : 0);
+            p.off_part = c.take((size_t)sum_capacity(p.chunk, V) * p.pitch * 4);
+            p.dx32 = splits_f32(p.chunk, D, p.Vp);
+            p.dw32 = splits_f32(p.Dp, p.Vp, p.chunk);
+            p.off_slots = c.take(std::max(slots_f32(p.dx32, p.chunk, D), slots_f32(p.dw32, p.Dp, p.Vp)));
             p.off_dbacc = c.take(p.chunks > 1 ? (size_t)V * 4 : 0);
         }
     }
@@ -328,26 +376,32 @@ CePlan plan_ce(const rnnt_ce_desc& d, bool grads, size_t budget) {
 rnnt_status run_ce(const rnnt_ce_desc& d, const CePlan& p, const void* x, const void* W, const float* b, const int32_t* label, const float* row_weight,
                    float* loss, void* dx, void* dW, void* db, unsigned char* ws, hipStream_t stream) {
     const long long D = d.D, V = d.V;
-    const CeRows rows{(int*)(ws + p.off_count), (int*)(ws + p.off_index), (int*)(ws + p.off_label), (float*)(ws + p.off_weight), (int*)(ws + p.off_place)};
+    const CeRows rows{(int*)(ws + p.off_count), (int*)(ws + p.off_index), (int*)(ws + p.off_label), (float*)(ws + p.off_weight)};
     const int size = p.bf16 ? 2 : 4;
+    if (p.identity) {
+        if (d.R == 0) return RNNT_OK;
+        CeRows own{};
+        own.label = const_cast<int*>(label);
+        const CeEpilogue e{b, d.V, label, (float*)(ws + p.off_score), (float2*)(ws + p.off_stats), p.tiles_n, nullptr, 0};
+        LAYER_HIP(launch_few_ce(FewJob{x, W, (int)d.R, d.D, d.V}, e, stream));
+        LAYER_HIP(launch_ce_finish(CeChunk{own, 0, d.R, e.label_score, e.stats, p.tiles_n, p.tile_log2, d.V, nullptr, loss, true, d.ignore_label}, stream));
+        return RNNT_OK;
+    }
     void* xp = ws + p.off_x;
     if (d.R > 0) {
-        LAYER_HIP(launch_ce_rows(label, row_weight, d.R, d.ignore_label, p.cap, rows, stream));
-        LAYER_HIP(launch_ce_gather(x, size, d.R, d.D, rows, xp, p.Dp, p.bf16 ? 0 : p.cap, loss, p.grads ? dx : nullptr, stream));
+        LAYER_HIP(launch_ce_gather(x, size, d.R, d.D, label, row_weight, d.ignore_label, p.cap, (int*)(ws + p.off_place), rows, xp, p.Dp,
+                                   p.bf16 ? 0 : p.cap, loss, p.grads ? dx : nullptr, stream));
     } else if (!p.grads) return RNNT_OK;
     else LAYER_HIP(launch_pad(nullptr, 4, 0, 0, 0, rows.count, 1, 1, stream));       // (no rows: the gradients of an empty sum)
     if (p.copy_w) LAYER_HIP(launch_pad(W, size, D, V, 0, ws + p.off_w, p.Dp, p.Vp, stream));
     const void* Wu = p.copy_w ? ws + p.off_w : W;
     unsigned char* chunk = ws + p.off_chunk;
     float* part = (float*)(ws + p.off_part);
-    float* dw_f32 = p.copy_out ? (float*)(ws + p.off_out) : (float*)dW;
-    if (!p.bf16 && p.grads && (p.copy_out || !d.accumulate_params)) LAYER_HIP(launch_pad(nullptr, 4, 0, 0, 0, dw_f32, p.Dp, p.Vp, stream));
     for (int k = 0; k < p.chunks; ++k) {
         const long long row0 = (long long)k * p.chunk, n = std::min(p.chunk, p.cap - row0);
         const bool first = k == 0, last = k == p.chunks - 1;
         const unsigned char* xc = (const unsigned char*)xp + (size_t)row0 * p.Dp * size;
         if (p.bf16) {
-            CeRows at = rows;
             GemmJob g{};
             g.A = GemmOperand{xc, p.Dp, nullptr, -1};
             g.B = GemmOperand{Wu, p.Vp, nullptr, -1};
@@ -360,64 +414,73 @@ rnnt_status run_ce(const rnnt_ce_desc& d, const CePlan& p, const void* x, const 
             g.row0 = row0;
             const CeEpilogue e{b, d.V, rows.label + row0, (float*)(ws + p.off_score), (float2*)(ws + p.off_stats), p.tiles_n,
                                p.grads ? chunk : nullptr, p.pitch};
+            const CeChunk c{rows, row0, n, e.label_score, e.stats, p.tiles_n, p.tile_log2, d.V, (float2*)(ws + p.off_scale), loss, false, 0};
             if (d.R > 0) {
-                LAYER_HIP(launch_ce_gemm(g, p.tile, e, stream));
-                LAYER_HIP(launch_ce_finish(at, row0, n, e.label_score, e.stats, p.tiles_n, d.V, loss, p.grads, stream));
+                if (p.few) LAYER_HIP(launch_few_ce(FewJob{xc, Wu, (int)d.R, (int)p.Dp, (int)p.Vp}, e, stream));
+                else LAYER_HIP(launch_ce_gemm(g, p.tile, e, stream));
+                if (!p.grads || !ce_grad_finishes(p.tiles_n)) LAYER_HIP(launch_ce_finish(c, stream));
             }
             if (!p.grads) continue;
-            if (d.R > 0) LAYER_HIP(launch_ce_grad(at, row0, n, chunk, p.pitch, e.stats, p.tiles_n, p.tile, d.V, db ? part : nullptr, stream));
+            if (d.R > 0) LAYER_HIP(launch_ce_grad(c, chunk, p.pitch, db ? part : nullptr, stream));
+            GradGemm gx{}, gw{};
             if (d.R > 0) {
-                GemmJob gx = g;
-                gx.A = GemmOperand{chunk, p.pitch, nullptr, -1};
-                gx.N = gx.b_rows = D;
-                gx.stages = (int)(p.Vp / 64);
-                const StoreEpilogue ex{dx, nullptr, rows.index + row0, D, 0, n, d.D, true, D % 8 == 0};
-                LAYER_HIP(launch_store_gemm(false, gx, p.dx, (float*)(ws + p.off_slots), ex, stream));
+                gx.g = g;
+                gx.g.A = GemmOperand{chunk, p.pitch, nullptr, -1};
+                gx.g.N = gx.g.b_rows = D;
+                gx.g.stages = (int)(p.Vp / 64);
+                gx.splits = p.pair.dx.splits;
+                gx.per_split = p.pair.dx.per_split;
+                gx.slots = (float*)(ws + p.off_slots);
+                gx.e = StoreEpilogue{dx, nullptr, rows.index + row0, D, 0, n, d.D, true};
             }
-            GemmJob gw{};
-            gw.A = GemmOperand{xc, p.Dp, nullptr, -1};
-            gw.B = GemmOperand{chunk, p.pitch, nullptr, -1};
-            gw.M = D;
-            gw.a_rows = p.Dp;
-            gw.N = V;
-            gw.b_rows = p.Vp;
-            gw.stages = (int)(n / 64);
-            gw.limit = GEMM_ROWS_K;
-            gw.count = rows.count;
-            gw.row0 = row0;
+            gw.g.A = GemmOperand{xc, p.Dp, nullptr, -1};
+            gw.g.B = GemmOperand{chunk, p.pitch, nullptr, -1};
+            gw.g.M = D;
+            gw.g.a_rows = p.Dp;
+            gw.g.N = V;
+            gw.g.b_rows = p.Vp;
+            gw.g.stages = (int)(n / 64);
+            gw.g.limit = GEMM_ROWS_K;
+            gw.g.count = rows.count;
+            gw.g.row0 = row0;
+            gw.splits = p.pair.dw.splits;
+            gw.per_split = p.pair.dw.per_split;
+            gw.slots = (float*)(ws + p.off_slots_w);
             const bool w16 = (d.param_grads_bf16 & 1) != 0, b16 = (d.param_grads_bf16 & 2) != 0;
             float* acc = w16 ? (float*)(ws + p.off_acc) : (float*)dW;
-            const StoreEpilogue ew{last ? dW : acc, !first || d.accumulate_params ? acc : nullptr, nullptr, V, 0, D, d.V, last && w16, V % 8 == 0};
-            LAYER_HIP(launch_store_gemm(true, gw, p.dw, (float*)(ws + p.off_slots), ew, stream));
-            if (db) {
-                float* dba = (float*)(ws + p.off_dbacc);
-                LAYER_HIP(launch_sum_parts(part, (int)(n / SUM_ROWS), p.pitch, d.V, rows.count, row0,
-                                           first ? (d.accumulate_params ? (const float*)db : nullptr) : dba, last ? db : (void*)dba, last && b16, stream));
-            }
+            gw.e = StoreEpilogue{last ? dW : acc, !first || d.accumulate_params ? acc : nullptr, nullptr, V, 0, D, d.V, last && w16};
+            float* dba = (float*)(ws + p.off_dbacc);
+            const SumJob sum{db ? part : nullptr, n, p.pitch, d.V, rows.count, row0, first ? (d.accumulate_params ? (const float*)db : nullptr) : dba,
+                             last ? db : (void*)dba, last && b16};
+            LAYER_HIP(launch_grad_gemms(p.pair.tile, gx, gw, sum, stream));
         } else {
             float* S = (float*)chunk;
             if (d.R > 0) {
-                LAYER_HIP(launch_gemm_f32_masked(0, 1, (const float*)xc, p.Dp, NO_MASK, (const float*)Wu, p.Vp, NO_MASK, S, p.pitch, nullptr, 0, n, p.Vp,
-                                                 p.Dp, 1, stream));
+                LAYER_HIP(launch_gemm_f32_split(0, 1, (const float*)xc, p.Dp, (const float*)Wu, p.Vp, S, p.pitch, n, p.Vp, p.Dp, 1, 0, stream));
                 LAYER_HIP(launch_ce_rows_f32(rows, row0, n, S, p.pitch, d.V, b, loss, p.grads, stream));
             }
             if (!p.grads) continue;
-            if (d.R > 0) {
-                float* dxc = (float*)(ws + p.off_dx);
-                LAYER_HIP(launch_gemm_f32_masked(0, 0, S, p.pitch, NO_MASK, (const float*)Wu, p.Vp, NO_MASK, dxc, D, nullptr, 0, n, D, p.Vp, 1, stream));
-                LAYER_HIP(launch_scatter_f32(rows, row0, n, dxc, D, d.D, (float*)dx, stream));
-                LAYER_HIP(launch_gemm_f32_masked(1, 1, (const float*)xc, p.Dp, NO_MASK, S, p.pitch, NO_MASK, dw_f32, p.Vp, nullptr, 1, p.Dp, p.Vp, n,
-                                                 k_splits_f32(p.Dp, p.Vp, n), stream));
+            if (d.R == 0) {
+                if (!d.accumulate_params) LAYER_HIP(launch_pad(nullptr, 4, 0, 0, 0, dW, D, V, stream));
+            } else {
+                float* slots = (float*)(ws + p.off_slots);
+                const int sx = gemm_f32_split_count(p.Vp, p.dx32), sw = gemm_f32_split_count(n, std::min<long long>(p.dw32, std::max(1LL, n / 64)));
+                LAYER_HIP(launch_gemm_f32_split(0, 0, S, p.pitch, (const float*)Wu, p.Vp, slots, D, n, D, p.Vp, sx, n * D, stream));
+                LAYER_HIP(launch_reduce_f32(slots, D, sx, n * D, rows.index + row0, (float*)dx, n, d.D, false, stream));
+                const bool add = !first || d.accumulate_params, direct = sw == 1 && !p.copy_w && !add;
+                LAYER_HIP(launch_gemm_f32_split(1, 1, (const float*)xc, p.Dp, S, p.pitch, direct ? (float*)dW : slots, p.Vp, p.Dp, p.Vp, n, sw,
+                                                p.Dp * p.Vp, stream));
+                if (!direct) LAYER_HIP(launch_reduce_f32(slots, p.Vp, sw, p.Dp * p.Vp, nullptr, (float*)dW, D, d.V, add, stream));
                 if (db) LAYER_HIP(launch_col_sums_f32(S, n, p.pitch, d.V, part, stream));
             }
             if (db) {
                 float* dba = (float*)(ws + p.off_dbacc);
-                LAYER_HIP(launch_sum_parts(part, (int)(n / SUM_ROWS), p.pitch, d.V, rows.count, row0,
-                                           first ? (d.accumulate_params ? (const float*)db : nullptr) : dba, last ? db : (void*)dba, false, stream));
+                LAYER_HIP(launch_sum_parts(SumJob{part, n, p.pitch, d.V, rows.count, row0,
+                                                  first ? (d.accumulate_params ? (const float*)db : nullptr) : dba, last ? db : (void*)dba, false},
+                                           stream));
             }
         }
     }
-    if (p.copy_out && p.grads) LAYER_HIP(launch_crop_f32(dw_f32, p.Vp, (float*)dW, D, d.V, d.accumulate_params != 0, stream));
     return RNNT_OK;
 }
 
@@ -491,4 +554,23 @@ extern "C" rnnt_status rnnt_ce_loss_fwd_bwd(const rnnt_ce_desc* desc, const void
                                             const float* row_weight, float* loss, void* dx, void* dW, void* db, void* workspace,
                                             size_t workspace_bytes, void* hip_stream) {
     return ce_loss(desc, true, x, W, b, label, row_weight, loss, dx, dW, db, workspace, workspace_bytes, hip_stream);
+}
+extern "C" rnnt_status rnnt_ce_loss_total(const rnnt_ce_desc* desc, const float* loss, const float* row_weight, float* total, void* hip_stream) {
+    const rnnt_status st = check_ce(desc, false);
+    if (st != RNNT_OK) return st;
+    if (!total || (desc->R > 0 && !loss)) return RNNT_ERR_NULL;
+    if ((((uintptr_t)loss | (uintptr_t)row_weight | (uintptr_t)total) % 4) != 0) return RNNT_ERR_UNSUPPORTED;
+    LAYER_HIP(launch_ce_total(loss, row_weight, desc->R, total, (hipStream_t)hip_stream));
+    return RNNT_OK;
+}
+extern "C" rnnt_status rnnt_ce_loss_scale(const rnnt_ce_desc* desc, const float* factor, void* dx, void* dW, void* db, void* hip_stream) {
+    const rnnt_status st = check_ce(desc, true);
+    if (st != RNNT_OK) return st;
+    if (!factor) return RNNT_ERR_NULL;
+    if (!aligned({dx, dW, db}) || (uintptr_t)factor % 4 != 0) return RNNT_ERR_UNSUPPORTED;
+    const long long n[3] = {dx ? desc->R * desc->D : 0, dW ? (long long)desc->D * desc->V : 0, db ? desc->V : 0};
+    const bool bf16[3] = {desc->dtype == RNNT_BF16, (desc->param_grads_bf16 & 1) != 0, (desc->param_grads_bf16 & 2) != 0};
+    void* const p[3] = {dx, dW, db};
+    LAYER_HIP(launch_scale(factor, p, n, bf16, (hipStream_t)hip_stream));
+    return RNNT_OK;
 }

@@ -58,7 +58,6 @@ struct LinearEpilogue {
     Dropout drop;
     long long M;
     int N;
-    bool vec;                            // rows of y, residual, saved are 16-byte aligned
 };
 // out = prev + v as bf16 or float; row r goes to row_map[r] (those < 0 nowhere)
 struct StoreEpilogue {
@@ -69,7 +68,7 @@ struct StoreEpilogue {
     long long split_stride;              // elements between the results of two splits
     long long M;
     int N;
-    bool bf16, vec;
+    bool bf16;
 };
 // Scores h = v + bias of a tile row -> their maximum m and S = sum 2^15 e^{h - m} (stats[row * tiles_n + tile]), the label's score, and, where kept is
 // not null, 2^15 e^{h - m} as fp16.
@@ -86,17 +85,63 @@ struct CeEpilogue {
 // k-contiguous A, k-slow B
 hipError_t launch_linear_gemm(const GemmJob& g, const GemmPlan& p, float* slots, const LinearEpilogue& e, hipStream_t stream);
 hipError_t launch_ce_gemm(const GemmJob& g, int tile, const CeEpilogue& e, hipStream_t stream);
-// A and B k-contiguous, or both k-slow
-hipError_t launch_store_gemm(bool k_slow, const GemmJob& g, const GemmPlan& p, float* slots, const StoreEpilogue& e, hipStream_t stream);
+// The same two for at most FEW_ROWS rows, x [M, K] and W [K, N] dense, of any size and alignment; the statistics are of parts of FEW_TILE columns.
+constexpr int FEW_ROWS = 64, FEW_TILE = 32;
+struct FewJob {
+    const void* x;
+    const void* W;
+    int M, K, N;
+};
+int few_splits(long long M, int K, int N);
+hipError_t launch_few_linear(const FewJob& j, int splits, float* slots, const LinearEpilogue& e, hipStream_t stream);
+// the epilogue on the sum of slots [splits][M][N up to 8]
+hipError_t launch_linear_reduce(long long M, int N, int splits, const float* slots, const LinearEpilogue& e, hipStream_t stream);
+hipError_t launch_few_ce(const FewJob& j, const CeEpilogue& e, hipStream_t stream);
+// The two gradients' products, dx (operands k-contiguous) and dW (operands k-slow), in one launch; then, in another, what remains: the sums of their splits
+// and the bias gradient's out of column sums.
+struct GradGemm {
+    GemmJob g;                           // M = 0: none
+    int splits, per_split;
+    float* slots;
+    StoreEpilogue e;
+};
+struct PairPlan {
+    int tile;
+    GemmPlan dx, dw;
+};
+PairPlan plan_pair(long long Mx, long long Nx, int stages_x, long long Mw, long long Nw, int stages_w, size_t slot_cap);
+struct SumJob {
+    const float* part;                   // null: none
+    long long rows, ld;                  // the rows that left the column sums
+    int N;
+    const int* count;                    // of them those below *count - row0, or null
+    long long row0;
+    const float* prev;
+    void* out;
+    bool bf16;
+};
+hipError_t launch_grad_gemms(int tile, const GradGemm& dx, const GradGemm& dw, const SumJob& db, hipStream_t stream);
 
 // ---- passes over memory --------------------------------------------------------------------------------------------
 // dst[rows_to, ld_to] = src[rows, cols] (dense) from row r0 on, zeros elsewhere; element size 2 or 4
 hipError_t launch_pad(const void* src, int size, long long rows, long long cols, long long r0, void* dst, long long rows_to, long long ld_to,
                       hipStream_t stream);
 
-// dz = dy act'(z) mask / (1 - p) into dz [rows_to, ld] (zeros beyond [M, N]; null: not stored), column sums of blocks of SUM_ROWS rows into part
-// [ceil(M / SUM_ROWS), ld] (null: none).  bf16: saved fp16, dz bf16; else both float.
-constexpr int SUM_ROWS = 128;
+// Rows per workgroup of a pass over [rows, cols] that leaves column sums, and so per row of these partial sums: 128 where there are workgroups of
+// 128 x 256 enough, fewer for a small array (1632 x 640 in fp32, dz: 29.6 us with 128, 39 workgroups).
+inline int sum_rows(long long rows, long long cols) {
+    int r = 128;
+    while (r > 16 && (rows + r - 1) / r * ((cols + 255) / 256) < 1024) r /= 2;
+    return r;
+}
+inline long long sum_blocks(long long rows, long long cols) { return (rows + sum_rows(rows, cols) - 1) / sum_rows(rows, cols); }
+// at least sum_blocks(r, cols) for every r <= rows (fewer rows per block below 128 means fewer than 1024 workgroups with twice as many)
+inline long long sum_capacity(long long rows, long long cols) {
+    const long long few = 2048 / ((cols + 255) / 256) + 2, many = (rows + 127) / 128, most = (rows + 15) / 16;
+    return few > many ? (few < most ? few : most) : many;
+}
+// dz = dy act'(z) mask / (1 - p) into dz [rows_to, ld] (zeros beyond [M, N]; null: not stored), column sums of blocks of sum_rows(M, N) rows into part
+// [sum_blocks(M, N), ld] (null: none).  bf16: saved fp16, dz bf16; else both float.
 struct DzArgs {
     const void* dy;
     const void* saved;
@@ -107,17 +152,17 @@ struct DzArgs {
     long long ld;
     int act;
     Dropout drop;
-    bool vec;
 };
 hipError_t launch_dz(bool bf16, const DzArgs& a, hipStream_t stream);
-// out[n] = prev[n] + sum of part[0 .. blocks) [n]; blocks from *count (rows - row0) where count is not null.  out bf16 or float
-hipError_t launch_sum_parts(const float* part, int blocks, long long ld, int N, const int* count, long long row0, const float* prev, void* out,
-                            bool bf16, hipStream_t stream);
-// fp32: z (pitch ld; may be saved or y) + bias -> saved (or null), y = residual + dropout(act(z + bias)); all but z dense [M, N]
-hipError_t launch_linear_rows_f32(const float* z, long long ld, const float* bias, const float* residual, float* y, float* saved, long long M, int N,
-                                  int act, const Dropout& drop, hipStream_t stream);
-// dst [rows, N] (+)= src (pitch ld)
-hipError_t launch_crop_f32(const float* src, long long ld, float* dst, long long rows, int N, bool add, hipStream_t stream);
+// out[n] = prev[n] + sum of the partial sums
+hipError_t launch_sum_parts(const SumJob& j, hipStream_t stream);
+// fp32: z (the sum of `splits` arrays of pitch ld, `stride` apart; one may be saved or y) + bias -> saved (or null), y = residual + dropout(act(z + bias)); all
+// but z dense [M, N]
+hipError_t launch_linear_rows_f32(const float* z, long long ld, int splits, long long stride, const float* bias, const float* residual, float* y,
+                                  float* saved, long long M, int N, int act, const Dropout& drop, hipStream_t stream);
+// dst [.., N] (+)= the sum of `splits` arrays of pitch ld, `stride` apart, rows as they are or row i to row_map[i] (those < 0 nowhere)
+hipError_t launch_reduce_f32(const float* src, long long ld, int splits, long long stride, const int* row_map, float* dst, long long rows, int N, bool add,
+                             hipStream_t stream);
 
 // ---- cross entropy ---------------------------------------------------------------------------------------------------
 // Rows whose label is not `ignore`, in order: their number, places, labels, weights.  Arrays of `cap` entries (a multiple of 256).
@@ -126,24 +171,35 @@ struct CeRows {
     int* index;                          // -1 behind the last
     int* label;
     float* weight;
-    int* place;                          // [R]: of each row in the order, or -1
 };
-hipError_t launch_ce_rows(const int* labels, const float* weight, long long R, int ignore, long long cap, const CeRows& r, hipStream_t stream);
 // x's rows in that order into xp [.., ld] (zeros beyond D and in the rows behind the last up to fill_to, 0: up to a multiple of 256); loss and dx
-// (null: no gradients) of the other rows = 0
-hipError_t launch_ce_gather(const void* x, int size, long long R, int D, const CeRows& r, void* xp, long long ld, long long fill_to, float* loss, void* dx,
-                            hipStream_t stream);
-// per row of a chunk: loss[index], and stats[..].x = factor that turns kept exponentials into weight * probability
-hipError_t launch_ce_finish(const CeRows& r, long long row0, long long rows, const float* label_score, float2* stats, int tiles_n, int V, float* loss,
-                            bool grads, hipStream_t stream);
-// kept -> score gradients bf16, in place; their column sums
-hipError_t launch_ce_grad(const CeRows& r, long long row0, long long rows, void* kept, long long pitch, const float2* stats, int tiles_n, int tile, int V,
-                          float* part, hipStream_t stream);
+// (null: no gradients) of the other rows = 0.  place: scratch of R ints for more than GATHER_SCAN rows.
+constexpr long long GATHER_SCAN = 16384;
+hipError_t launch_ce_gather(const void* x, int size, long long R, int D, const int* labels, const float* weight, int ignore, long long cap, int* place,
+                            const CeRows& r, void* xp, long long ld, long long fill_to, float* loss, void* dx, hipStream_t stream);
+// Rows [row0, row0 + rows) of that order and the statistics of their scores, tiles_n parts of 2^tile_log2 columns each (arrays: of the chunk)
+struct CeChunk {
+    CeRows r;
+    long long row0, rows;
+    const float* label_score;
+    const float2* stats;
+    int tiles_n, tile_log2, V;
+    float2* scale;                       // [rows] {maximum, weight / sum}: what turns a kept exponential into weight * probability
+    float* loss;
+    bool identity;                       // r.label are the caller's labels, every row is its own place and the ones with `ignore` have loss 0
+    int ignore;
+};
+// loss, scale
+hipError_t launch_ce_finish(const CeChunk& c, hipStream_t stream);
+// kept -> score gradients bf16, in place; their column sums (part: null: none).  Does launch_ce_finish's work too where ce_grad_finishes says so.
+inline bool ce_grad_finishes(int tiles_n) { return tiles_n <= 16; }
+hipError_t launch_ce_grad(const CeChunk& c, void* kept, long long pitch, float* part, hipStream_t stream);
 // fp32: scores [rows, V] (pitch ld, without the bias) -> loss and, with grads, score gradients in place (zeros in rows behind the last)
 hipError_t launch_ce_rows_f32(const CeRows& r, long long row0, long long rows, float* scores, long long ld, int V, const float* b, float* loss,
                               bool grads, hipStream_t stream);
+// total = sum of weight[r] loss[r] over the rows whose weight is not 0 (null: ones)
+hipError_t launch_ce_total(const float* loss, const float* weight, long long R, float* total, hipStream_t stream);
+// three arrays (those of length 0: none) times *factor, in place; a factor of 1 moves nothing
+hipError_t launch_scale(const float* factor, void* const (&p)[3], const long long (&n)[3], const bool (&bf16)[3], hipStream_t stream);
 hipError_t launch_col_sums_f32(const float* x, long long rows, long long ld, int N, float* part, hipStream_t stream);
-// dx[index[row0 + i]] = src[i] (fp32, D columns of pitch ld)
-hipError_t launch_scatter_f32(const CeRows& r, long long row0, long long rows, const float* src, long long ld, int D, float* dx, hipStream_t stream);
-
 }  // namespace rnnt

@@ -8,6 +8,61 @@ namespace rnnt {
 namespace {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+// Eight values of a row at their element's alignment (rows of odd length): still one load or store of 16 bytes
+typedef bf16x8 bf16x8_any __attribute__((aligned(2)));
+typedef f16x8 f16x8_any __attribute__((aligned(2)));
+typedef f32x4 f32x4_at4 __attribute__((aligned(4)));
+template <typename T>
+struct Vec8;
+template <>
+struct Vec8<bf16_t> {
+    typedef bf16x8 type;
+    typedef bf16x8_any any;
+};
+template <>
+struct Vec8<_Float16> {
+    typedef f16x8 type;
+    typedef f16x8_any any;
+};
+// The first `live` of eight consecutive values, zeros for the others
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, int live, float (&v)[8]) {
+    if (live >= 8) {
+        if constexpr (sizeof(T) == 2) {
+            const typename Vec8<T>::type x = *reinterpret_cast<const typename Vec8<T>::any*>(p);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = (float)x[j];
+        } else {
+            const f32x4 a = *reinterpret_cast<const f32x4_at4*>(p), b = *reinterpret_cast<const f32x4_at4*>(p + 4);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[j] = a[j];
+                v[4 + j] = b[j];
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = j < live ? (float)p[j] : 0.0f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, int live, const float (&v)[8]) {
+    if (live >= 8) {
+        if constexpr (sizeof(T) == 2) {
+            typename Vec8<T>::type x;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = (T)v[j];
+            *reinterpret_cast<typename Vec8<T>::any*>(p) = x;
+        } else {
+            *reinterpret_cast<f32x4_at4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+            *reinterpret_cast<f32x4_at4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < live) p[j] = (T)v[j];
+    }
+}
 
 // Philox4x32-10 (Salmon, Moraes, Dror, Shaw: Parallel random numbers, as easy as 1, 2, 3; 2011) with key {seed} on the counter {column / 8, row, offset}:
 // the 128 bits of eight columns, 16 for each.
@@ -19,11 +74,11 @@ __device__ __forceinline__ RandomBits8 random_bits8(unsigned long long seed, uns
     unsigned c0 = group, c1 = row, c2 = (unsigned)offset, c3 = (unsigned)(offset >> 32), k0 = (unsigned)seed, k1 = (unsigned)(seed >> 32);
 #pragma unroll
     for (int i = 0; i < 10; ++i) {
-        const unsigned h0 = __umulhi(c0, 0xD2511F53u), l0 = c0 * 0xD2511F53u, h1 = __umulhi(c2, 0xCD9E8D57u), l1 = c2 * 0xCD9E8D57u;
-        c0 = h1 ^ c1 ^ k0;
-        c1 = l1;
-        c2 = h0 ^ c3 ^ k1;
-        c3 = l0;
+        const unsigned long long p0 = (unsigned long long)c0 * 0xD2511F53u, p1 = (unsigned long long)c2 * 0xCD9E8D57u;
+        c0 = (unsigned)(p1 >> 32) ^ c1 ^ k0;
+        c1 = (unsigned)p1;
+        c2 = (unsigned)(p0 >> 32) ^ c3 ^ k1;
+        c3 = (unsigned)p0;
         k0 += 0x9E3779B9u;
         k1 += 0xBB67AE85u;
     }
@@ -43,6 +98,27 @@ __device__ __forceinline__ float sigmoid(float x) {
     if constexpr (FAST) return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-LOG2E_F * x));
     else return 1.0f / (1.0f + expf(-x));
 }
+// Phi(-|x|), the normal distribution's tail, and e^{-x^2/2}.  FAST: erfc(z) = t Q(t) e^{-z^2} with t = 1 / (1 + 0.375 z) and a polynomial Q of degree 6
+// fitted to it for the smallest relative error over z < 9.3 (6.5e-7; in fp32 2e-6 for |x| < 5, 9e-6 where the tail leaves fp32's range): one reciprocal,
+// one exponential.
+template <bool FAST>
+__device__ __forceinline__ float normal_tail(float x, float& bell) {
+    if constexpr (FAST) {
+        const float t = __builtin_amdgcn_rcpf(fmaf(0.375f * 0.70710678118654752f, fabsf(x), 1.0f));
+        bell = __builtin_amdgcn_exp2f(-0.5f * LOG2E_F * x * x);
+        float q = 0.5f * -0.13509601354599f;
+        q = fmaf(q, t, 0.5f * 0.3879377841949463f);
+        q = fmaf(q, t, 0.5f * -0.12959635257720947f);
+        q = fmaf(q, t, 0.5f * 0.2830599546432495f);
+        q = fmaf(q, t, 0.5f * 0.1666656881570816f);
+        q = fmaf(q, t, 0.5f * 0.2156888246536255f);
+        q = fmaf(q, t, 0.5f * 0.21133948862552643f);
+        return q * t * bell;
+    } else {
+        bell = expf(-0.5f * x * x);
+        return 0.5f * erfcf(0.70710678118654752f * fabsf(x));
+    }
+}
 template <bool FAST>
 __device__ __forceinline__ void act8(int act, float (&v)[8]) {
     switch (act) {
@@ -57,7 +133,11 @@ __device__ __forceinline__ void act8(int act, float (&v)[8]) {
             break;
         case ACT_GELU:
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = v[j] == RNNT_NEG_INF ? 0.0f : v[j] * (0.5f * erfcf(-0.70710678118654752f * v[j]));
+            for (int j = 0; j < 8; ++j) {
+                float bell;
+                const float q = normal_tail<FAST>(v[j], bell);
+                v[j] = v[j] == RNNT_NEG_INF ? 0.0f : v[j] * (v[j] > 0.0f ? 1.0f - q : q);
+            }
             break;
         case ACT_TANH:
 #pragma unroll
@@ -84,8 +164,9 @@ __device__ __forceinline__ void act_grad8(int act, const float (&z)[8], float (&
         case ACT_GELU:
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float x = z[j], d = FAST ? __builtin_amdgcn_exp2f(-0.5f * LOG2E_F * x * x) : expf(-0.5f * x * x);
-                g[j] *= fmaf(x * 0.3989422804014327f, d, 0.5f * erfcf(-0.70710678118654752f * x));
+                float bell;
+                const float q = normal_tail<FAST>(z[j], bell);
+                g[j] *= fmaf(z[j] * 0.3989422804014327f, bell, z[j] > 0.0f ? 1.0f - q : q);
             }
             break;
         case ACT_TANH:
@@ -101,11 +182,11 @@ __device__ __forceinline__ void act_grad8(int act, const float (&z)[8], float (&
 
 // A saved pre-activation: fp16 (11 bits, where bf16's eight would add as much to the gradient's error as its own rounding does), beyond the largest
 // one that largest one (there act' has its limit), and a nonzero one stays nonzero (its sign is relu's derivative).
-__device__ __forceinline__ _Float16 saved_f16(float z) {
+__device__ __forceinline__ float for_f16(float z) {
     float c = z > 65504.0f ? 65504.0f : z < -65504.0f ? -65504.0f : z;             // (NaN stays)
     if (c > 0.0f && c < 5.9604644775390625e-8f) c = 5.9604644775390625e-8f;
     if (c < 0.0f && c > -5.9604644775390625e-8f) c = -5.9604644775390625e-8f;
-    return (_Float16)c;
+    return c;
 }
 
 // ---- what becomes of columns n .. n + 7 (n a multiple of 8) of row m of a product --------------------------------------
@@ -117,44 +198,24 @@ struct LinearStore {
     __device__ static __forceinline__ void store(const LinearEpilogue& e, int, long long m, int n, float (&v)[8], const float (&b)[8]) {
         if (m >= e.M || n >= e.N) return;
         const size_t at = (size_t)m * e.N + n;
-        const int live = e.N - n < 8 ? e.N - n : 8;
+        const int live = e.N - n;
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] += b[j];
         if (e.saved != nullptr) {
-            _Float16* s = (_Float16*)e.saved + at;
-            f16x8 h;
+            float h[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) h[j] = saved_f16(v[j]);
-            if (e.vec) *reinterpret_cast<f16x8*>(s) = h;
-            else
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (j < live) s[j] = h[j];
+            for (int j = 0; j < 8; ++j) h[j] = for_f16(v[j]);
+            store8((_Float16*)e.saved + at, live, h);
         }
         act8<true>(e.act, v);
         drop8(e.drop, m, n, v);
         if (e.residual != nullptr) {
-            const bf16_t* r = (const bf16_t*)e.residual + at;
-            if (e.vec) {
-                const bf16x8 x = *reinterpret_cast<const bf16x8*>(r);
+            float r[8];
+            load8((const bf16_t*)e.residual + at, live, r);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] += (float)x[j];
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] += (float)r[j < live ? j : 0];
-            }
+            for (int j = 0; j < 8; ++j) v[j] += r[j];
         }
-        bf16_t* y = (bf16_t*)e.y + at;
-        if (e.vec) {
-            bf16x8 o;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = (bf16_t)v[j];
-            *reinterpret_cast<bf16x8*>(y) = o;
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (j < live) y[j] = (bf16_t)v[j];
-        }
+        store8((bf16_t*)e.y + at, live, v);
     }
     __device__ static __forceinline__ void bias(const LinearEpilogue& e, int n, float (&b)[8]) { load_bias8(e.bias, n < e.N ? n : e.N - 1, e.N, b); }
 };
@@ -167,47 +228,43 @@ struct PlainStore {
             if (row < 0) return;
         }
         const size_t at = (size_t)split * e.split_stride + (size_t)row * e.ld + n;
-        const int live = e.N - n < 8 ? e.N - n : 8;
+        const int live = e.N - n;
         if (e.prev != nullptr) {
-            if (e.vec) {
-                const f32x4 a = *reinterpret_cast<const f32x4*>(e.prev + at), b = *reinterpret_cast<const f32x4*>(e.prev + at + 4);
+            float p[8];
+            load8(e.prev + at, live, p);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    v[j] += a[j];
-                    v[4 + j] += b[j];
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] += e.prev[at + (j < live ? j : 0)];
-            }
+            for (int j = 0; j < 8; ++j) v[j] += p[j];
         }
-        if (e.bf16) {
-            bf16_t* o = (bf16_t*)e.out + at;
-            bf16x8 x;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = (bf16_t)v[j];
-            if (e.vec) *reinterpret_cast<bf16x8*>(o) = x;
-            else
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (j < live) o[j] = x[j];
-        } else {
-            float* o = (float*)e.out + at;
-            if (e.vec) {
-                *reinterpret_cast<f32x4*>(o) = f32x4{v[0], v[1], v[2], v[3]};
-                *reinterpret_cast<f32x4*>(o + 4) = f32x4{v[4], v[5], v[6], v[7]};
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (j < live) o[j] = v[j];
-            }
-        }
+        if (e.bf16) store8((bf16_t*)e.out + at, live, v);
+        else store8((float*)e.out + at, live, v);
     }
     __device__ static __forceinline__ void bias(const StoreEpilogue&, int, float (&b)[8]) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) b[j] = 0.0f;
     }
 };
+// Columns 32 block .. + 31 of a SumJob, by 256 threads in eight rows; the partial sums are added in a fixed order.
+__device__ __forceinline__ void sum_parts(const SumJob& j, int blocks, int R, int block, float (*red)[32]) {
+    const int c = threadIdx.x & 31, row = threadIdx.x >> 5, n = block * 32 + c;
+    if (j.count != nullptr) {
+        long long r = (long long)*j.count - j.row0;
+        r = r < 0 ? 0 : (r + R - 1) / R;
+        blocks = r < blocks ? (int)r : blocks;
+    }
+    float s = 0.0f;
+    if (n < j.N)
+        for (int b = row; b < blocks; b += 8) s += j.part[(size_t)b * j.ld + n];
+    red[row][c] = s;
+    __syncthreads();
+    if (row == 0 && n < j.N) {
+        float t = j.prev != nullptr ? j.prev[n] : 0.0f;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) t += red[r][c];
+        if (j.bf16) ((bf16_t*)j.out)[n] = (bf16_t)t;
+        else ((float*)j.out)[n] = t;
+    }
+}
+
 template <class E>
 struct EpilogueOf;
 template <>
