@@ -38,6 +38,7 @@ typedef struct {
                            65535)                                                                                                       */
     int32_t accumulate_params; /* backward: 0: dW, db are overwritten; 1: added to (they are float then)    */
     int32_t param_grads_bf16;  /* backward, RNNT_BF16 only: bit 0: dW is bfloat16, bit 1: db is bfloat16; else float.  */
+    int32_t bias_bf16;         /* b is 0: float, 1: bfloat16                                                */
 } rnnt_linear_desc;
 
 /*
@@ -49,9 +50,10 @@ typedef struct {
  *
  * x        dev [M, K]   desc->dtype
  * W        dev [K, N]   desc->dtype (the transpose of a torch Linear's weight)
- * b        dev [N]      float, or NULL
+ * b        dev [N]      float or bfloat16 (desc->bias_bf16), or NULL
  * residual dev [M, N]   desc->dtype, or NULL
  * rng      dev [2]      {seed, offset}, read by the kernels when they run (a replayed graph takes what is there then); NULL allowed with p = 0
+ * rng_used dev [2]      out, or NULL: the seed and offset this call took (for its backward pass, where the caller advances rng meanwhile)
  * y        dev [M, N]   desc->dtype, out
  * saved    dev [M, N]   out, or NULL: z for the backward pass, two bytes per entry with RNNT_BF16 (fp16), four with RNNT_F32.  The backward
  *                       pass of RNNT_ACT_NONE does without.
@@ -59,8 +61,8 @@ typedef struct {
  * workspace_bytes >= rnnt_linear_workspace_bytes(desc, 0); with 0 bytes workspace may be NULL.
  */
 size_t rnnt_linear_workspace_bytes(const rnnt_linear_desc* desc, int32_t backward);
-rnnt_status rnnt_linear_fwd(const rnnt_linear_desc* desc, const void* x, const void* W, const float* b, const void* residual,
-                            const uint64_t* rng, void* y, void* saved, void* workspace, size_t workspace_bytes, void* hip_stream);
+rnnt_status rnnt_linear_fwd(const rnnt_linear_desc* desc, const void* x, const void* W, const void* b, const void* residual,
+                            const uint64_t* rng, uint64_t* rng_used, void* y, void* saved, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
  * Gradients for an incoming dy = d/dy: with dz = dy act'(z) m / (1 - p)
@@ -82,6 +84,7 @@ typedef struct {
     int32_t ignore_label; /* rows with this label are padding                                               */
     int32_t accumulate_params; /* 0: dW, db are overwritten; 1: added to (they are float then)              */
     int32_t param_grads_bf16;  /* RNNT_BF16 only: bit 0: dW is bfloat16, bit 1: db is bfloat16; else float  */
+    int32_t bias_bf16;         /* b is 0: float, 1: bfloat16                                                */
 } rnnt_ce_desc;
 
 /*
@@ -94,7 +97,7 @@ typedef struct {
  *
  * x          dev [R, D]  desc->dtype; padding rows may hold anything and are never used
  * W          dev [D, V]  desc->dtype (W_out of rnnt_joint_loss_fwd_bwd)
- * b          dev [V]     float, or NULL; -inf takes an entry out of the vocabulary
+ * b          dev [V]     float or bfloat16 (desc->bias_bf16), or NULL; -inf takes an entry out of the vocabulary
  * label      dev [R]     int32
  * row_weight dev [R]     float, any sign, or NULL (ones); read by the kernels
  * loss       dev [R]     float, out; 0 in padding rows; +inf where the label is outside [0, V) (its gradient then is row_weight softmax(h)) or no entry
@@ -108,9 +111,9 @@ typedef struct {
  * default is used for larger chunks.
  */
 size_t rnnt_ce_loss_workspace_bytes(const rnnt_ce_desc* desc, int32_t grads, size_t budget_bytes);
-rnnt_status rnnt_ce_loss_fwd(const rnnt_ce_desc* desc, const void* x, const void* W, const float* b, const int32_t* label, float* loss,
+rnnt_status rnnt_ce_loss_fwd(const rnnt_ce_desc* desc, const void* x, const void* W, const void* b, const int32_t* label, float* loss,
                              void* workspace, size_t workspace_bytes, void* hip_stream);
-rnnt_status rnnt_ce_loss_fwd_bwd(const rnnt_ce_desc* desc, const void* x, const void* W, const float* b, const int32_t* label,
+rnnt_status rnnt_ce_loss_fwd_bwd(const rnnt_ce_desc* desc, const void* x, const void* W, const void* b, const int32_t* label,
                                  const float* row_weight, float* loss, void* dx, void* dW, void* db, void* workspace, size_t workspace_bytes,
                                  void* hip_stream);
 

@@ -70,30 +70,35 @@ def rnnt_joint_loss(enc, pred, W_out, b_out, labels, T_len, U_len, blank: int = 
                                 keep_scores)
 
 
+def _grads_bf16(W, b):
+    """param_grads_bf16 of leaves W, b: gradients of their types"""
+    return 0 if W.dtype == torch.float32 else 3 if b is not None and b.dtype == torch.bfloat16 else 1
+
+
 class _RnntLinear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, W, b, activation, residual, dropout, rng_state):
-        # the state as the kernels see it now: the caller may advance it before the backward pass
-        rng = rng_state.clone() if rng_state is not None and dropout > 0.0 else None
-        need = any(ctx.needs_input_grad[:3])
-        out = Bd.run_linear_fwd(x, W, None if b is None else b.float(), activation, residual, dropout, rng, save=need)
-        ctx.save_for_backward(x, W, out["saved"], rng)
-        ctx.activation, ctx.dropout, ctx.b_dtype = activation, dropout, None if b is None else b.dtype
+        # (with dropout the call also leaves the state its kernels saw: the caller may advance it before the backward pass)
+        out = Bd.run_linear_fwd(x, W, b, activation, residual, dropout, rng_state, save=any(ctx.needs_input_grad[:3]))
+        ctx.save_for_backward(x, W, out["saved"], out["rng_used"])
+        ctx.opts = activation, dropout, None if b is None else b.dtype, _grads_bf16(W, b)
         return out["y"]
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
         x, W, saved, rng = ctx.saved_tensors
+        activation, dropout, b_dtype, bits = ctx.opts
         need = ctx.needs_input_grad
         want = tuple(k for k, n in zip(("dx", "dW", "db"), need) if n)
-        g = dict(dx=None, dW=None, db=None)
+        dx = dW = db = None
         dy = dy.contiguous()
         if want:
-            bf16 = 0 if W.dtype == torch.float32 else 1 | (2 if ctx.b_dtype == torch.bfloat16 else 0)
-            g = Bd.run_linear_bwd(x, W, dy, ctx.activation, saved, ctx.dropout, rng, param_grads_bf16=bf16, want=want)
-        db = g["db"]
-        return g["dx"], g["dW"], db if db is None else db.to(ctx.b_dtype), None, dy if need[4] else None, None, None
+            g = Bd.run_linear_bwd(x, W, dy, activation, saved, dropout, rng, param_grads_bf16=bits, want=want)
+            dx, dW, db = g["dx"], g["dW"], g["db"]
+            if db is not None and db.dtype != b_dtype:
+                db = db.to(b_dtype)
+        return dx, dW, db, None, dy if need[4] else None, None, None
 
 
 def rnnt_linear(x, W, b=None, activation="none", residual=None, dropout: float = 0.0, rng_state=None):
@@ -106,8 +111,11 @@ def rnnt_linear(x, W, b=None, activation="none", residual=None, dropout: float =
 
 
 def _ce_grads(x, W, b, labels, row_weight, ignore_label, budget_bytes):
-    bits = 0 if W.dtype == torch.float32 else 1 | (2 if b is not None and b.dtype == torch.bfloat16 else 0)
-    return Bd.run_ce_fwd_bwd(x, W, None if b is None else b.float(), labels, row_weight, ignore_label, param_grads_bf16=bits, budget_bytes=budget_bytes)
+    out = Bd.run_ce_fwd_bwd(x, W, b, labels, row_weight, ignore_label, param_grads_bf16=_grads_bf16(W, b), want_db=b is not None,
+                            budget_bytes=budget_bytes)
+    if b is not None and out["db"].dtype != b.dtype:
+        out["db"] = out["db"].to(b.dtype)
+    return out
 
 
 class _RnntCeSum(torch.autograd.Function):
@@ -118,7 +126,7 @@ class _RnntCeSum(torch.autograd.Function):
             ctx.save_for_backward(x, W, b, labels, row_weight)
             ctx.grads, ctx.opts = out, (ignore_label, budget_bytes)
         else:
-            out = Bd.run_ce_fwd(x, W, None if b is None else b.float(), labels, ignore_label, budget_bytes=budget_bytes)
+            out = Bd.run_ce_fwd(x, W, b, labels, ignore_label, budget_bytes=budget_bytes)
         return Bd.run_ce_total(out["loss"], row_weight)
 
     @staticmethod
@@ -134,7 +142,7 @@ class _RnntCeSum(torch.autograd.Function):
             w = g.expand(labels.shape).contiguous() if row_weight is None else row_weight * g
             out = _ce_grads(x, W, b, labels, w, *ctx.opts)
         need = ctx.needs_input_grad
-        return (out["dx"] if need[0] else None, out["dW"] if need[1] else None, out["db"].to(b.dtype) if need[2] else None, None, None, None, None)
+        return (out["dx"] if need[0] else None, out["dW"] if need[1] else None, out["db"] if need[2] else None, None, None, None, None)
 
 
 class _RnntCeRows(torch.autograd.Function):
@@ -142,7 +150,7 @@ class _RnntCeRows(torch.autograd.Function):
     def forward(ctx, x, W, b, labels, ignore_label, budget_bytes):
         ctx.save_for_backward(x, W, b, labels)
         ctx.opts = ignore_label, budget_bytes
-        return Bd.run_ce_fwd(x, W, None if b is None else b.float(), labels, ignore_label, budget_bytes=budget_bytes)["loss"]
+        return Bd.run_ce_fwd(x, W, b, labels, ignore_label, budget_bytes=budget_bytes)["loss"]
 
     @staticmethod
     @torch.autograd.function.once_differentiable
@@ -150,7 +158,7 @@ class _RnntCeRows(torch.autograd.Function):
         x, W, b, labels = ctx.saved_tensors
         need = ctx.needs_input_grad
         out = _ce_grads(x, W, b, labels, g.float().contiguous(), *ctx.opts)
-        return (out["dx"] if need[0] else None, out["dW"] if need[1] else None, out["db"].to(b.dtype) if b is not None and need[2] else None,
+        return (out["dx"] if need[0] else None, out["dW"] if need[1] else None, out["db"] if need[2] else None,
                 None, None, None)
 
 

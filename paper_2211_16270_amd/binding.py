@@ -7,6 +7,7 @@ fallback: if the shared library has not been built, loading raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional
 
@@ -51,12 +52,13 @@ class RnntPlanInfo(ctypes.Structure):
 class RnntLinearDesc(ctypes.Structure):
     _fields_ = [("M", ctypes.c_int64), ("K", ctypes.c_int32), ("N", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("activation", ctypes.c_int32), ("dropout", ctypes.c_float), ("accumulate_params", ctypes.c_int32),
-                ("param_grads_bf16", ctypes.c_int32)]
+                ("param_grads_bf16", ctypes.c_int32), ("bias_bf16", ctypes.c_int32)]
 
 
 class RnntCeDesc(ctypes.Structure):
     _fields_ = [("R", ctypes.c_int64), ("D", ctypes.c_int32), ("V", ctypes.c_int32), ("dtype", ctypes.c_int32),
-                ("ignore_label", ctypes.c_int32), ("accumulate_params", ctypes.c_int32), ("param_grads_bf16", ctypes.c_int32)]
+                ("ignore_label", ctypes.c_int32), ("accumulate_params", ctypes.c_int32), ("param_grads_bf16", ctypes.c_int32),
+                ("bias_bf16", ctypes.c_int32)]
 
 
 class RnntError(RuntimeError):
@@ -153,7 +155,7 @@ def lib() -> ctypes.CDLL:
     L.rnnt_linear_workspace_bytes.restype = ctypes.c_size_t
     L.rnnt_linear_workspace_bytes.argtypes = [lp, ctypes.c_int32]
     L.rnnt_linear_fwd.restype = ctypes.c_int
-    L.rnnt_linear_fwd.argtypes = [lp] + [vp] * 8 + [ctypes.c_size_t, vp]
+    L.rnnt_linear_fwd.argtypes = [lp] + [vp] * 9 + [ctypes.c_size_t, vp]
     L.rnnt_linear_bwd.restype = ctypes.c_int
     L.rnnt_linear_bwd.argtypes = [lp] + [vp] * 9 + [ctypes.c_size_t, vp]
     L.rnnt_ce_loss_workspace_bytes.restype = ctypes.c_size_t
@@ -520,10 +522,10 @@ def rnnt_linear_workspace_bytes(desc: RnntLinearDesc, backward: bool) -> int:
     return int(lib().rnnt_linear_workspace_bytes(ctypes.byref(desc), int(backward)))
 
 
-def rnnt_linear_fwd(desc: RnntLinearDesc, x, W, b, residual, rng, y, saved, workspace=None, stream=None) -> int:
+def rnnt_linear_fwd(desc: RnntLinearDesc, x, W, b, residual, rng, rng_used, y, saved, workspace=None, stream=None) -> int:
     """Raw call: torch CUDA tensors (or None) of the layouts the header states.  Returns the status code; enqueues on `stream` (default: torch's
     current stream) without synchronising."""
-    return int(lib().rnnt_linear_fwd(ctypes.byref(desc), _ptr(x), _ptr(W), _ptr(b), _ptr(residual), _ptr(rng), _ptr(y), _ptr(saved),
+    return int(lib().rnnt_linear_fwd(ctypes.byref(desc), _ptr(x), _ptr(W), _ptr(b), _ptr(residual), _ptr(rng), _ptr(rng_used), _ptr(y), _ptr(saved),
                                      _ptr(workspace), _nbytes(workspace), _stream_handle(stream)))
 
 
@@ -554,11 +556,63 @@ def rnnt_ce_loss_scale(desc: RnntCeDesc, factor, dx, dW, db, stream=None) -> int
     return int(lib().rnnt_ce_loss_scale(ctypes.byref(desc), _ptr(factor), _ptr(dx), _ptr(dW), _ptr(db), _stream_handle(stream)))
 
 
+# What a call of the functions below needs besides its tensors is a function of sizes and types: kept, so that a small call does not spend its time here.
+@functools.lru_cache(maxsize=4096)
+def _linear_call(M, K, N, code, activation, dropout, accumulate, param_grads_bf16, bias_bf16, backward):
+    """(descriptor, reference to it, workspace bytes)"""
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {ACTIVATIONS}, got {activation!r}")
+    if not 0.0 <= dropout < 1.0:
+        raise ValueError(f"dropout must be in [0, 1), got {dropout}")
+    desc = RnntLinearDesc(M, K, N, code, ACTIVATIONS.index(activation), dropout, accumulate, param_grads_bf16, bias_bf16)
+    return desc, ctypes.byref(desc), rnnt_linear_workspace_bytes(desc, backward)
+
+
+@functools.lru_cache(maxsize=4096)
+def _ce_call(R, D, V, code, ignore_label, accumulate, param_grads_bf16, bias_bf16, grads, budget_bytes):
+    desc = RnntCeDesc(R, D, V, code, ignore_label, accumulate, param_grads_bf16, bias_bf16)
+    return desc, ctypes.byref(desc), rnnt_ce_loss_workspace_bytes(desc, grads, budget_bytes)
+
+
 def _check_tensor(name, t, dtype, device, shape=None):
-    if t.device != device or t.dtype != dtype or not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
+    if t.dtype != dtype or t.device != device or not t.is_contiguous() or (shape is not None and t.shape != shape):
         raise ValueError(f"{name}: expected a contiguous {dtype} tensor on {device}"
                          + ("" if shape is None else f" of shape {tuple(shape)}")
                          + f", got {t.dtype} {tuple(t.shape)} on {t.device}" + ("" if t.is_contiguous() else ", not contiguous"))
+
+
+def _layer_dtype(x, W, K):
+    """The dtype code of x [..., K] and W [K, N]."""
+    if not x.is_cuda:
+        raise ValueError(f"x must be a CUDA tensor, got one on {x.device}")
+    code = _DTYPE_CODES.get(str(x.dtype))
+    if code is None:
+        raise ValueError(f"x must be bfloat16 or float32, got {x.dtype}")
+    if x.dim() < 1 or W.dim() != 2 or x.shape[-1] != K or K == 0 or W.shape[1] == 0:
+        raise ValueError(f"x [..., inputs] and W [inputs, outputs] do not fit: {tuple(x.shape)}, {tuple(W.shape)}")
+    _check_tensor("x", x, x.dtype, x.device)
+    _check_tensor("W", W, x.dtype, x.device)
+    return code
+
+
+_DTYPE_CODES = {"torch.bfloat16": RNNT_BF16, "torch.float32": RNNT_F32}
+
+
+def _bias_bf16(b, device, N) -> int:
+    import torch
+    if b is None:
+        return 0
+    bf16 = b.dtype == torch.bfloat16
+    _check_tensor("b", b, b.dtype if bf16 else torch.float32, device, (N,))
+    return int(bf16)
+
+
+def _check_rng(rng_state, dropout, device):
+    import torch
+    if rng_state is not None:
+        _check_tensor("rng_state", rng_state, torch.int64, device, (2,))
+    elif dropout > 0.0:
+        raise ValueError("dropout needs rng_state, an int64 tensor [2] on the device: {seed, offset}")
 
 
 def _aligned(t):
@@ -567,168 +621,161 @@ def _aligned(t):
 
 
 class _CallOn:
-    """The device of the tensors made current, and `stream` (None: that device's current one), for allocations and launches."""
+    """The device of the tensors made current, and `stream` (None: that device's current one), for allocations and launches.  Entering gives the stream's
+    handle."""
+    __slots__ = ("contexts", "index")
 
     def __init__(self, device, stream):
         import torch
-        self.contexts = []
+        self.contexts, self.index = None, device.index
         if stream is not None:
             if stream.device != device:
                 raise ValueError(f"stream on {stream.device}, tensors on {device}")
-            self.contexts.append(torch.cuda.stream(stream))
-        elif torch.cuda.current_device() != device.index:
-            self.contexts.append(torch.cuda.device(device))
+            self.contexts = torch.cuda.stream(stream)
+        elif torch._C._cuda_getDevice() != device.index:
+            self.contexts = torch.cuda.device(device)
 
     def __enter__(self):
-        for c in self.contexts:
-            c.__enter__()
+        import torch
+        if self.contexts is not None:
+            self.contexts.__enter__()
+        return torch._C._cuda_getCurrentRawStream(self.index) or None
 
     def __exit__(self, *exc):
-        for c in reversed(self.contexts):
-            c.__exit__(*exc)
+        if self.contexts is not None:
+            self.contexts.__exit__(*exc)
 
 
-def _layer_dtype(x):
+def _workspace(workspace, nbytes, device):
+    """(the tensor to keep, its address, its bytes)"""
     import torch
-    if not x.is_cuda:
-        raise ValueError("x must be a CUDA tensor")
-    if x.dtype == torch.bfloat16:
-        return RNNT_BF16
-    if x.dtype == torch.float32:
-        return RNNT_F32
-    raise ValueError(f"x must be bfloat16 or float32, got {x.dtype}")
-
-
-def _layer_workspace(workspace, nbytes, device):
-    import torch
-    if workspace is not None:
-        return workspace.buf
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
-
-
-def _check_linear(x, W, activation, dropout, rng_state, accumulate, param_grads_bf16):
-    import torch
-    code = _layer_dtype(x)
-    if x.dim() < 1 or W.dim() != 2 or x.shape[-1] != W.shape[0]:
-        raise ValueError(f"x [..., K] and W [K, N] do not fit: {tuple(x.shape)}, {tuple(W.shape)}")
-    _check_tensor("x", x, x.dtype, x.device)
-    _check_tensor("W", W, x.dtype, x.device)
-    if activation not in ACTIVATIONS:
-        raise ValueError(f"activation must be one of {ACTIVATIONS}, got {activation!r}")
-    if not 0.0 <= dropout < 1.0:
-        raise ValueError(f"dropout must be in [0, 1), got {dropout}")
-    if dropout > 0.0 and rng_state is None:
-        raise ValueError("dropout needs rng_state, an int64 tensor [2] on the device: {seed, offset}")
-    if rng_state is not None:
-        _check_tensor("rng_state", rng_state, torch.int64, x.device, (2,))
-    K, N = W.shape
-    return RnntLinearDesc(x.numel() // K if K else 0, K, N, code, ACTIVATIONS.index(activation), float(dropout), int(accumulate),
-                          int(param_grads_bf16))
+    buf = workspace.buf if workspace is not None else torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    return (None, None, 0) if buf is None else (buf, buf.data_ptr(), buf.numel())
 
 
 def run_linear_fwd(x, W, b=None, activation="none", residual=None, dropout=0.0, rng_state=None, save=False,
                    workspace: Optional[Workspace] = None, stream=None):
     """y = residual + dropout(act(x W + b)): checks the tensors, allocates the outputs (and a workspace unless given), calls rnnt_linear_fwd, raises
-    on a non-zero status.  x [..., K], W [K, N] (bfloat16 or float32), b [N] float32 or None, residual [..., N] or None, rng_state int64 [2] on the
-    device {seed, offset}.  save: also keep what run_linear_bwd needs of an activation.  Returns dict(y, saved)."""
+    on a non-zero status.  x [..., K], W [K, N] (bfloat16 or float32), b [N] (float32 or bfloat16) or None, residual [..., N] or None, rng_state int64 [2]
+    on the device {seed, offset}.  save: also keep what run_linear_bwd needs.  Returns dict(y, saved, rng_used): saved None without an
+    activation, rng_used None without dropout or save."""
     import torch
-    desc = _check_linear(x, W, activation, dropout, rng_state, 0, 0)
-    shape = x.shape[:-1] + (desc.N,)
-    if b is not None:
-        _check_tensor("b", b, torch.float32, x.device, (desc.N,))
+    K, N = W.shape if W.dim() == 2 else (0, 0)
+    code, device = _layer_dtype(x, W, K), x.device
+    dropout = float(dropout)
+    shape = x.shape[:-1] + (N,)
+    bias_bf16 = _bias_bf16(b, device, N)
+    _check_rng(rng_state, dropout, device)
     if residual is not None:
-        _check_tensor("residual", residual, x.dtype, x.device, shape)
-    with _CallOn(x.device, stream):
-        y = torch.empty(shape, dtype=x.dtype, device=x.device)
-        saved = torch.empty(shape, dtype=torch.float16 if desc.dtype == RNNT_BF16 else torch.float32, device=x.device) \
-            if save and desc.activation != 0 else None
-        ws = _layer_workspace(workspace, rnnt_linear_workspace_bytes(desc, False), x.device)
-        st = rnnt_linear_fwd(desc, _aligned(x), _aligned(W), _aligned(b), _aligned(residual), rng_state, y, saved, ws)
+        _check_tensor("residual", residual, x.dtype, device, shape)
+    desc, ref, nbytes = _linear_call(x.numel() // K, K, N, code, activation, dropout, 0, 0, bias_bf16, False)
+    x, W, b, residual = _aligned(x), _aligned(W), _aligned(b), _aligned(residual)
+    with _CallOn(device, stream) as handle:
+        y = torch.empty(shape, dtype=x.dtype, device=device)
+        saved = rng_used = None
+        if save:
+            if desc.activation != 0:
+                saved = torch.empty(shape, dtype=torch.float16 if code == RNNT_BF16 else torch.float32, device=device)
+            if dropout > 0.0:
+                rng_used = torch.empty_like(rng_state)
+        ws, ws_ptr, ws_bytes = _workspace(workspace, nbytes, device)
+        st = lib().rnnt_linear_fwd(ref, x.data_ptr(), W.data_ptr(), _ptr(b), _ptr(residual), _ptr(rng_state), _ptr(rng_used), y.data_ptr(),
+                                   _ptr(saved), ws_ptr, ws_bytes, handle)
     if st != 0:
         raise RnntError(st, "rnnt_linear_fwd")
-    return dict(y=y, saved=saved)
+    if rng_used is not None and desc.M == 0:
+        rng_used.copy_(rng_state)
+    return dict(y=y, saved=saved, rng_used=rng_used)
 
 
 def run_linear_bwd(x, W, dy, activation="none", saved=None, dropout=0.0, rng_state=None, accumulate_into=None, param_grads_bf16=0,
                    want=("dx", "dW", "db"), workspace: Optional[Workspace] = None, stream=None):
-    """Gradients of run_linear_fwd for an incoming dy [..., N]; rng_state must hold what the forward call read.  accumulate_into: (dW, db) float32
-    to add to; param_grads_bf16: the descriptor's field; want: which of dx, dW, db.  Returns dict(dx, dW, db) (None: not wanted)."""
+    """Gradients of run_linear_fwd for an incoming dy [..., N]; rng_state must hold what the forward call read (its rng_used).  accumulate_into: (dW, db)
+    float32 to add to (either may be None); param_grads_bf16: the descriptor's field; want: which of dx, dW, db.  Returns dict(dx, dW, db) (None: not
+    wanted)."""
     import torch
-    desc = _check_linear(x, W, activation, dropout, rng_state, accumulate_into is not None, param_grads_bf16)
-    shape = x.shape[:-1] + (desc.N,)
-    _check_tensor("dy", dy, x.dtype, x.device, shape)
+    K, N = W.shape if W.dim() == 2 else (0, 0)
+    code, device = _layer_dtype(x, W, K), x.device
+    dropout = float(dropout)
+    shape = x.shape[:-1] + (N,)
+    _check_tensor("dy", dy, x.dtype, device, shape)
+    _check_rng(rng_state, dropout, device)
+    desc, ref, nbytes = _linear_call(x.numel() // K, K, N, code, activation, dropout, int(accumulate_into is not None), int(param_grads_bf16), 0, True)
     if desc.activation != 0:
         if saved is None:
             raise ValueError(f"the backward pass of {activation} needs what the forward call saved")
-        _check_tensor("saved", saved, torch.float16 if desc.dtype == RNNT_BF16 else torch.float32, x.device, shape)
-    with _CallOn(x.device, stream):
+        _check_tensor("saved", saved, torch.float16 if code == RNNT_BF16 else torch.float32, device, shape)
+    x, W, dy, saved = _aligned(x), _aligned(W), _aligned(dy), _aligned(saved)
+    with _CallOn(device, stream) as handle:
         dx = torch.empty_like(x) if "dx" in want else None
-        if accumulate_into is not None:
-            dW, db = accumulate_into
-            for name, t, s in (("dW", dW, (desc.K, desc.N)), ("db", db, (desc.N,))):
-                if t is not None:
-                    _check_tensor(name, t, torch.float32, x.device, s)
-        else:
-            kind = [torch.bfloat16 if desc.param_grads_bf16 >> bit & 1 else torch.float32 for bit in (0, 1)]
-            dW = torch.empty(desc.K, desc.N, dtype=kind[0], device=x.device) if "dW" in want else None
-            db = torch.empty(desc.N, dtype=kind[1], device=x.device) if "db" in want else None
-        ws = _layer_workspace(workspace, rnnt_linear_workspace_bytes(desc, True), x.device)
-        st = rnnt_linear_bwd(desc, _aligned(x), _aligned(W), _aligned(saved), rng_state, _aligned(dy), dx, dW, db, ws)
+        dW, db = _param_grads(accumulate_into, param_grads_bf16, want, (K, N), (N,), device)
+        ws, ws_ptr, ws_bytes = _workspace(workspace, nbytes, device)
+        st = lib().rnnt_linear_bwd(ref, x.data_ptr(), W.data_ptr(), _ptr(saved), _ptr(rng_state), dy.data_ptr(), _ptr(dx), _ptr(dW), _ptr(db), ws_ptr,
+                                   ws_bytes, handle)
     if st != 0:
         raise RnntError(st, "rnnt_linear_bwd")
     return dict(dx=dx, dW=dW, db=db)
 
 
-def _check_ce(x, W, b, labels, ignore_label, accumulate, param_grads_bf16):
+def _param_grads(accumulate_into, bf16_bits, want, w_shape, b_shape, device):
     import torch
-    code = _layer_dtype(x)
-    if x.dim() < 1 or W.dim() != 2 or x.shape[-1] != W.shape[0]:
-        raise ValueError(f"x [..., D] and W [D, V] do not fit: {tuple(x.shape)}, {tuple(W.shape)}")
-    _check_tensor("x", x, x.dtype, x.device)
-    _check_tensor("W", W, x.dtype, x.device)
-    D, V = W.shape
-    if b is not None:
-        _check_tensor("b", b, torch.float32, x.device, (V,))
+    if accumulate_into is not None:
+        dW, db = accumulate_into
+        for name, t, shape in (("dW", dW, w_shape), ("db", db, b_shape)):
+            if t is not None:
+                _check_tensor(name, t, torch.float32, device, shape)
+        return dW, db
+    dW = torch.empty(w_shape, dtype=torch.bfloat16 if bf16_bits & 1 else torch.float32, device=device) if "dW" in want else None
+    db = torch.empty(b_shape, dtype=torch.bfloat16 if bf16_bits & 2 else torch.float32, device=device) if "db" in want else None
+    return dW, db
+
+
+def _check_ce(x, W, b, labels):
+    import torch
+    D, V = W.shape if W.dim() == 2 else (0, 0)
+    code = _layer_dtype(x, W, D)
     _check_tensor("labels", labels, torch.int32, x.device, x.shape[:-1])
-    return RnntCeDesc(labels.numel(), D, V, code, int(ignore_label), int(accumulate), int(param_grads_bf16))
+    return D, V, code, _bias_bf16(b, x.device, V)
 
 
 def run_ce_fwd(x, W, b, labels, ignore_label=-1, workspace: Optional[Workspace] = None, budget_bytes: int = 0, stream=None):
-    """Cross entropy of softmax(x W + b) per row: x [..., D], W [D, V] (bfloat16 or float32), b [V] float32 or None, labels [...] int32 (rows with
-    ignore_label are padding).  Returns dict(loss) of the labels' shape, float32."""
+    """Cross entropy of softmax(x W + b) per row: x [..., D], W [D, V] (bfloat16 or float32), b [V] (float32 or bfloat16) or None, labels [...] int32
+    (rows with ignore_label are padding).  Returns dict(loss) of the labels' shape, float32."""
     import torch
-    desc = _check_ce(x, W, b, labels, ignore_label, 0, 0)
-    with _CallOn(x.device, stream):
-        loss = torch.empty(labels.shape, dtype=torch.float32, device=x.device)
-        ws = _layer_workspace(workspace, rnnt_ce_loss_workspace_bytes(desc, False, budget_bytes), x.device)
-        st = rnnt_ce_loss_fwd(desc, _aligned(x), _aligned(W), _aligned(b), labels, loss, ws)
+    D, V, code, bias_bf16 = _check_ce(x, W, b, labels)
+    device = x.device
+    desc, ref, nbytes = _ce_call(labels.numel(), D, V, code, int(ignore_label), 0, 0, bias_bf16, False, int(budget_bytes))
+    x, W, b = _aligned(x), _aligned(W), _aligned(b)
+    with _CallOn(device, stream) as handle:
+        loss = torch.empty(labels.shape, dtype=torch.float32, device=device)
+        ws, ws_ptr, ws_bytes = _workspace(workspace, nbytes, device)
+        st = lib().rnnt_ce_loss_fwd(ref, x.data_ptr(), W.data_ptr(), _ptr(b), labels.data_ptr(), loss.data_ptr(), ws_ptr, ws_bytes, handle)
     if st != 0:
         raise RnntError(st, "rnnt_ce_loss_fwd")
     return dict(loss=loss)
 
 
-def run_ce_fwd_bwd(x, W, b, labels, row_weight=None, ignore_label=-1, accumulate_into=None, param_grads_bf16=0,
+def run_ce_fwd_bwd(x, W, b, labels, row_weight=None, ignore_label=-1, accumulate_into=None, param_grads_bf16=0, want_db=True,
                    workspace: Optional[Workspace] = None, budget_bytes: int = 0, stream=None):
-    """run_ce_fwd and the gradients of sum(row_weight * loss) (row_weight [...] float32, None: ones).  accumulate_into: (dW, db) float32 to add to;
-    param_grads_bf16: the descriptor's field.  Returns dict(loss, dx, dW, db)."""
+    """run_ce_fwd and the gradients of sum(row_weight * loss) (row_weight [...] float32, None: ones).  accumulate_into: (dW, db) float32 to add to (db
+    may be None); param_grads_bf16: the descriptor's field.  Returns dict(loss, dx, dW, db)."""
     import torch
-    desc = _check_ce(x, W, b, labels, ignore_label, accumulate_into is not None, param_grads_bf16)
+    D, V, code, bias_bf16 = _check_ce(x, W, b, labels)
+    device = x.device
     if row_weight is not None:
-        _check_tensor("row_weight", row_weight, torch.float32, x.device, labels.shape)
-    with _CallOn(x.device, stream):
-        loss = torch.empty(labels.shape, dtype=torch.float32, device=x.device)
+        _check_tensor("row_weight", row_weight, torch.float32, device, labels.shape)
+    if accumulate_into is not None and accumulate_into[0] is None:
+        raise ValueError("accumulate_into: dW is needed")
+    desc, ref, nbytes = _ce_call(labels.numel(), D, V, code, int(ignore_label), int(accumulate_into is not None), int(param_grads_bf16), bias_bf16, True,
+                                 int(budget_bytes))
+    x, W, b = _aligned(x), _aligned(W), _aligned(b)
+    with _CallOn(device, stream) as handle:
+        loss = torch.empty(labels.shape, dtype=torch.float32, device=device)
         dx = torch.empty_like(x)
-        if accumulate_into is not None:
-            dW, db = accumulate_into
-            for name, t, s in (("dW", dW, (desc.D, desc.V)), ("db", db, (desc.V,))):
-                if t is not None:
-                    _check_tensor(name, t, torch.float32, x.device, s)
-        else:
-            kind = [torch.bfloat16 if desc.param_grads_bf16 >> bit & 1 else torch.float32 for bit in (0, 1)]
-            dW = torch.empty(desc.D, desc.V, dtype=kind[0], device=x.device)
-            db = torch.empty(desc.V, dtype=kind[1], device=x.device)
-        ws = _layer_workspace(workspace, rnnt_ce_loss_workspace_bytes(desc, True, budget_bytes), x.device)
-        st = rnnt_ce_loss_fwd_bwd(desc, _aligned(x), _aligned(W), _aligned(b), labels, row_weight, loss, dx, dW, db, ws)
+        dW, db = _param_grads(accumulate_into, param_grads_bf16, ("dW", "db") if want_db else ("dW",), (D, V), (V,), device)
+        ws, ws_ptr, ws_bytes = _workspace(workspace, nbytes, device)
+        st = lib().rnnt_ce_loss_fwd_bwd(ref, x.data_ptr(), W.data_ptr(), _ptr(b), labels.data_ptr(), _ptr(row_weight), loss.data_ptr(), dx.data_ptr(),
+                                        dW.data_ptr(), _ptr(db), ws_ptr, ws_bytes, handle)
     if st != 0:
         raise RnntError(st, "rnnt_ce_loss_fwd_bwd")
     return dict(loss=loss, dx=dx, dW=dW, db=db)
@@ -742,7 +789,7 @@ def run_ce_total(loss, row_weight=None, stream=None):
         _check_tensor("row_weight", row_weight, torch.float32, loss.device, loss.shape)
     with _CallOn(loss.device, stream):
         total = torch.empty((), dtype=torch.float32, device=loss.device)
-        st = rnnt_ce_loss_total(RnntCeDesc(loss.numel(), 1, 1, RNNT_F32, -1, 0, 0), loss, row_weight, total)
+        st = rnnt_ce_loss_total(RnntCeDesc(loss.numel(), 1, 1, RNNT_F32, -1, 0, 0, 0), loss, row_weight, total)
     if st != 0:
         raise RnntError(st, "rnnt_ce_loss_total")
     return total
@@ -756,6 +803,6 @@ def run_ce_scale(factor, dx, dW, db=None, stream=None):
     code = RNNT_BF16 if dx.dtype == torch.bfloat16 else RNNT_F32
     bits = int(dW.dtype == torch.bfloat16) | (2 if db is not None and db.dtype == torch.bfloat16 else 0)
     with _CallOn(dx.device, stream):
-        st = rnnt_ce_loss_scale(RnntCeDesc(dx.numel() // D, D, V, code, -1, 0, bits), factor, dx, dW, db)
+        st = rnnt_ce_loss_scale(RnntCeDesc(dx.numel() // D, D, V, code, -1, 0, bits, 0), factor, dx, dW, db)
     if st != 0:
         raise RnntError(st, "rnnt_ce_loss_scale")

@@ -25,6 +25,7 @@ __device__ __forceinline__ bf16x8 raw8(const bf16_t* p, int live) {
 
 struct FewLinear {
     LinearEpilogue e;
+    __device__ __forceinline__ void first() const { pass_rng(e); }
     // columns n .. n + 7 (granule g of the workgroup's 32) of row m
     __device__ __forceinline__ void operator()(int m, int n, int, float (&v)[8]) const {
         float b[8];
@@ -35,6 +36,7 @@ struct FewLinear {
 // Statistics of the 32 columns of a row (four neighbouring lanes hold them), as k_ce_scores leaves them for its tiles
 struct FewCe {
     CeEpilogue e;
+    __device__ __forceinline__ void first() const {}
     __device__ __forceinline__ void operator()(int m, int n, int block, float (&v)[8]) const {
         float b[8];
         load_bias8(e.bias, n < e.V ? n : e.V - 1, e.V, b);
@@ -73,6 +75,7 @@ __global__ __launch_bounds__(64 * FW) void k_few_rows(FewJob j, E e, int blocks,
     static_assert(MT * 16 * FC * 4 >= 2048, "a step of W per wave");
     const int per = (blocks + 7) >> 3, block = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
     if ((int)(blockIdx.x >> 3) >= per || block >= blocks) return;
+    if (block == 0 && slots == nullptr) e.first();
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, n0 = block * FC;
     const int K = j.K, N = j.N;
     unsigned char* area = smem + wave * 2048;

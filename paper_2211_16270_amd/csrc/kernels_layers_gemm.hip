@@ -72,6 +72,7 @@ struct TileJob {
 template <class TS, bool AKS, bool BKS, class E>
 __global__ __launch_bounds__(TS::THREADS, 2) void k_layer_gemm(TileJob<E> j) {
     extern __shared__ __align__(16) unsigned char smem[];
+    if (blockIdx.x == 0) pass_rng(j.e);
     gemm_workgroup<TS, AKS, BKS, E>(j.g, j.e, blockIdx.x, j.mt, j.nt, j.splits, j.per_split, smem);
 }
 // dx and dW
@@ -114,6 +115,7 @@ __device__ __forceinline__ void reduce_workgroup(const ReduceJob<E>& r, unsigned
 }
 template <class E>
 __global__ __launch_bounds__(256) void k_layer_reduce(ReduceJob<E> r) {
+    if (blockIdx.x == 0) pass_rng(r.e);
     reduce_workgroup(r, blockIdx.x);
 }
 __global__ __launch_bounds__(256) void k_layer_reduce_grads(ReduceJob<StoreEpilogue> x, ReduceJob<StoreEpilogue> w, SumJob db, int db_blocks, int db_rows) {
@@ -150,7 +152,7 @@ __global__ __launch_bounds__(TS::THREADS, 2) void k_ce_scores(GemmJob g, CeEpilo
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int n = (int)n0 + (wn * TS::NT + j) * 32 + 8 * q + 4 * hb + r;
-                const float b = e.bias == nullptr ? 0.0f : e.bias[n < e.V ? n : e.V - 1];
+                const float b = e.bias.at(n < e.V ? n : e.V - 1);
 #pragma unroll
                 for (int i = 0; i < TS::MT; ++i) acc[i][j][4 * q + r] = n < e.V ? acc[i][j][4 * q + r] + b : RNNT_NEG_INF;
             }
@@ -286,60 +288,61 @@ hipError_t grad_gemms(const GradGemm& dx, const GradGemm& dw, hipStream_t stream
 // a small one, with its neighbour beside it, 0.7), with five stages' time for a round's start and end; the slots' way to memory and back.
 namespace {
 constexpr double STAGE_TIME[2] = {1.0, 0.7}, ENDS_TIME[2] = {5.0, 4.0}, AT_ONCE[2] = {256.0, 512.0}, BYTES_PER_UNIT = 6e6, LAUNCH_TIME = 3.0;
-double tile_count(int tile, long long M, long long N) { return (double)((M + tile - 1) / tile) * (double)((N + tile - 1) / tile); }
-double slot_time(const GemmPlan& p, long long M, long long N) {
-    return p.splits > 1 ? (double)gemm_slot_bytes(p, M, N) * 2.0 / BYTES_PER_UNIT : 0.0;
-}
-bool split_ok(const GemmPlan& p, int stages, long long M, long long N, size_t slot_cap) {
-    if (p.splits == 1) return true;
-    return p.splits <= std::max(1, stages / 2) && (p.splits - 1) * p.per_split < stages && gemm_slot_bytes(p, M, N) <= slot_cap;
+constexpr int SPLITS[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 32, 48, 64}, N_SPLITS = sizeof(SPLITS) / sizeof(int);
+struct Choice {
+    GemmPlan p;
+    double workgroups, time, extra;      // number, each one's time, the slots' time
+};
+// The splits of a product with tiles of shape k that are possible
+int choices(int k, long long M, long long N, int stages, size_t slot_cap, Choice (&c)[N_SPLITS]) {
+    const int tile = k == 0 ? 256 : 128;
+    const double tiles = (double)((M + tile - 1) / tile) * (double)((N + tile - 1) / tile);
+    int n = 0;
+    for (int splits : SPLITS) {
+        const GemmPlan p{tile, splits, (stages + splits - 1) / splits};
+        const size_t bytes = gemm_slot_bytes(p, M, N);
+        if (splits > 1 && (splits > stages / 2 || (splits - 1) * p.per_split >= stages || bytes > slot_cap)) continue;
+        c[n++] = Choice{p, tiles * splits, p.per_split * STAGE_TIME[k] + ENDS_TIME[k], (double)bytes * 2.0 / BYTES_PER_UNIT};
+    }
+    return n;
 }
 }  // namespace
 GemmPlan plan_gemm(long long M, long long N, int stages, size_t slot_cap) {
     GemmPlan best{256, 1, stages};
     double least = 1e300;
     for (int k = 0; k < 2; ++k) {
-        const int tile = k == 0 ? 256 : 128;
-        const double tiles = tile_count(tile, M, N);
-        for (int splits = 1; splits <= 64; ++splits) {
-            const GemmPlan p{tile, splits, (stages + splits - 1) / splits};
-            if (!split_ok(p, stages, M, N, slot_cap)) continue;
-            const double rounds = std::max(1.0, (double)(long long)((tiles * splits + AT_ONCE[k] - 1) / AT_ONCE[k]));
-            const double t = rounds * (p.per_split * STAGE_TIME[k] + ENDS_TIME[k]) + (splits > 1 ? LAUNCH_TIME + slot_time(p, M, N) : 0.0);
+        Choice c[N_SPLITS];
+        const int n = choices(k, M, N, stages, slot_cap, c);
+        for (int i = 0; i < n; ++i) {
+            const double rounds = std::max(1.0, (double)(long long)((c[i].workgroups + AT_ONCE[k] - 1) / AT_ONCE[k]));
+            const double t = rounds * c[i].time + (c[i].p.splits > 1 ? LAUNCH_TIME + c[i].extra : 0.0);
             if (t < least) {
                 least = t;
-                best = p;
+                best = c[i].p;
             }
         }
     }
     return best;
 }
-// The same for two products that share a launch: workgroups of both, the longer ones first, fill the chip one after the other.
+// The same for two products that share a launch: workgroups of both fill the chip one after the other.
 PairPlan plan_pair(long long Mx, long long Nx, int stages_x, long long Mw, long long Nw, int stages_w, size_t slot_cap) {
-    static const int SPLITS[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64};
     PairPlan best{256, {256, 1, stages_x}, {256, 1, stages_w}};
     double least = 1e300;
     for (int k = 0; k < 2; ++k) {
-        const int tile = k == 0 ? 256 : 128;
-        const double tx = tile_count(tile, Mx, Nx), tw = tile_count(tile, Mw, Nw);
-        for (int sx : SPLITS) {
-            const GemmPlan px{tile, sx, (stages_x + sx - 1) / sx};
-            if (!split_ok(px, stages_x, Mx, Nx, slot_cap)) continue;
-            const double ux = px.per_split * STAGE_TIME[k] + ENDS_TIME[k];
-            for (int sw : SPLITS) {
-                const GemmPlan pw{tile, sw, (stages_w + sw - 1) / sw};
-                if (!split_ok(pw, stages_w, Mw, Nw, slot_cap)) continue;
-                const double uw = pw.per_split * STAGE_TIME[k] + ENDS_TIME[k];
-                const double nx = tx * sx, nw = tw * sw, work = (nx * ux + nw * uw) / AT_ONCE[k];
+        Choice x[N_SPLITS], w[N_SPLITS];
+        const int nx = choices(k, Mx, Nx, stages_x, slot_cap, x), nw = choices(k, Mw, Nw, stages_w, slot_cap, w);
+        for (int i = 0; i < nx; ++i)
+            for (int j = 0; j < nw; ++j) {
                 // at least one workgroup's time; the last round is on average half empty
-                const double t = std::max(std::max(nx > 0 ? ux : 0.0, nw > 0 ? uw : 0.0), work + 0.5 * std::min(ux, uw) * (work > std::max(ux, uw))) +
-                                 (sx > 1 || sw > 1 ? LAUNCH_TIME + slot_time(px, Mx, Nx) + slot_time(pw, Mw, Nw) : 0.0);
+                const double work = (x[i].workgroups * x[i].time + w[j].workgroups * w[j].time) / AT_ONCE[k];
+                const double longest = std::max(x[i].workgroups > 0 ? x[i].time : 0.0, w[j].time), shortest = std::min(x[i].time, w[j].time);
+                double t = work > longest ? work + 0.5 * shortest : longest;
+                if (x[i].p.splits > 1 || w[j].p.splits > 1) t += LAUNCH_TIME + x[i].extra + w[j].extra;
                 if (t < least) {
                     least = t;
-                    best = PairPlan{tile, px, pw};
+                    best = PairPlan{k == 0 ? 256 : 128, x[i].p, w[j].p};
                 }
             }
-        }
     }
     return best;
 }

@@ -95,10 +95,11 @@ __device__ __forceinline__ void load8_sum(const float* p, int splits, long long 
 }
 
 // z (pitch ld, may be saved or y) + bias -> saved, y; one thread per eight columns
-__global__ __launch_bounds__(256) void k_linear_rows_f32(const float* z, long long ld, int splits, long long stride, const float* __restrict__ bias, const float* __restrict__ residual,
-                                                         float* y, float* saved, long long M, int N, int act, Dropout drop, long long groups,
-                                                         long long total) {
+__global__ __launch_bounds__(256) void k_linear_rows_f32(const float* z, long long ld, int splits, long long stride, Bias bias, const float* __restrict__ residual,
+                                                         float* y, float* saved, long long M, int N, int act, Dropout drop,
+                                                         unsigned long long* rng_used, long long groups, long long total) {
     const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (rng_used != nullptr && i < 2) rng_used[i] = drop.state[i];
     if (i >= total) return;
     const long long m = i / groups;
     const int n = (int)(i - m * groups) * 8, live = N - n < 8 ? N - n : 8;
@@ -389,7 +390,7 @@ __global__ __launch_bounds__(256) void k_ce_grad(CeChunk c, void* __restrict__ k
 
 // fp32: a workgroup per row of scores: maximum and sum of the exponentials in one pass, the gradient in a second one
 __global__ __launch_bounds__(256) void k_ce_rows_f32(CeRows r, long long row0, float* __restrict__ scores, long long ld, int V,
-                                                     const float* __restrict__ b, float* __restrict__ loss, bool grads) {
+                                                     Bias b, float* __restrict__ loss, bool grads) {
     __shared__ float2 part[4];
     const long long i = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, at = r.index[row0 + i];
@@ -402,7 +403,7 @@ __global__ __launch_bounds__(256) void k_ce_rows_f32(CeRows r, long long row0, f
     }
     const int y = r.label[row0 + i];
     const bool known = (unsigned)y < (unsigned)V;
-    auto score = [&](int v) { return b != nullptr ? h[v] + b[v] : h[v]; };
+    auto score = [&](int v) { return h[v] + b.at(v); };
     const float hy = known ? score(y) : 0.0f;
     float m = RNNT_NEG_INF, s = 0.0f;
     for (int v = tid; v < V; v += 256) m = fmaxf(m, score(v));
@@ -535,13 +536,13 @@ hipError_t launch_sum_parts(const SumJob& j, hipStream_t stream) {
     return hipGetLastError();
 }
 
-hipError_t launch_linear_rows_f32(const float* z, long long ld, int splits, long long stride, const float* bias, const float* residual, float* y,
-                                  float* saved, long long M, int N, int act, const Dropout& drop, hipStream_t stream) {
+hipError_t launch_linear_rows_f32(const float* z, long long ld, int splits, long long stride, const Bias& bias, const float* residual, float* y,
+                                  float* saved, long long M, int N, int act, const Dropout& drop, unsigned long long* rng_used, hipStream_t stream) {
     const long long groups = (N + 7) / 8, total = M * groups;
     if (total <= 0) return hipSuccess;
     if (!grid_fits((total + 255) / 256)) return hipErrorInvalidValue;
-    k_linear_rows_f32<<<dim3(blocks_of(total, 256)), dim3(256), 0, stream>>>(z, ld, splits, stride, bias, residual, y, saved, M, N, act, drop, groups,
-                                                                             total);
+    k_linear_rows_f32<<<dim3(blocks_of(total, 256)), dim3(256), 0, stream>>>(z, ld, splits, stride, bias, residual, y, saved, M, N, act, drop,
+                                                                             rng_used, groups, total);
     return hipGetLastError();
 }
 hipError_t launch_reduce_f32(const float* src, long long ld, int splits, long long stride, const int* row_map, float* dst, long long rows, int N, bool add,
@@ -589,7 +590,7 @@ hipError_t launch_ce_grad(const CeChunk& c, void* kept, long long pitch, float* 
     else k_ce_grad<false><<<dim3((unsigned)n), dim3(256), 0, stream>>>(c, kept, pitch, part, R);
     return hipGetLastError();
 }
-hipError_t launch_ce_rows_f32(const CeRows& r, long long row0, long long rows, float* scores, long long ld, int V, const float* b, float* loss,
+hipError_t launch_ce_rows_f32(const CeRows& r, long long row0, long long rows, float* scores, long long ld, int V, const Bias& b, float* loss,
                               bool grads, hipStream_t stream) {
     k_ce_rows_f32<<<dim3((unsigned)rows), dim3(256), 0, stream>>>(r, row0, scores, ld, V, b, loss, grads);
     return hipGetLastError();

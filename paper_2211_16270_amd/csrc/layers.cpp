@@ -66,7 +66,7 @@ rnnt_status check_linear(const rnnt_linear_desc* d, bool backward) {
     if (d->M < 0 || d->M > MAX_ROWS || d->K < 1 || d->K > MAX_WIDTH || d->N < 1 || d->N > MAX_WIDTH) return RNNT_ERR_SHAPE;
     if (d->dtype != RNNT_F32 && d->dtype != RNNT_BF16) return RNNT_ERR_UNSUPPORTED;
     if (d->activation < 0 || d->activation >= ACT_COUNT) return RNNT_ERR_UNSUPPORTED;
-    if (!(d->dropout >= 0.0f && d->dropout < 1.0f)) return RNNT_ERR_SHAPE;
+    if (!(d->dropout >= 0.0f && d->dropout < 1.0f) || d->bias_bf16 < 0 || d->bias_bf16 > 1) return RNNT_ERR_SHAPE;
     if (backward) {
         if (d->accumulate_params < 0 || d->accumulate_params > 1 || d->param_grads_bf16 < 0 || d->param_grads_bf16 > 3) return RNNT_ERR_SHAPE;
         if (d->param_grads_bf16 != 0 && (d->dtype != RNNT_BF16 || d->accumulate_params)) return RNNT_ERR_UNSUPPORTED;
@@ -151,10 +151,10 @@ LinearPlan plan_linear(const rnnt_linear_desc& d, bool backward) {
     return p;
 }
 
-rnnt_status linear_fwd_bf16(const rnnt_linear_desc& d, const LinearPlan& p, const void* x, const void* W, const float* b, const void* residual,
-                            const Dropout& drop, void* y, void* saved, unsigned char* ws, hipStream_t stream) {
+rnnt_status linear_fwd_bf16(const rnnt_linear_desc& d, const LinearPlan& p, const void* x, const void* W, const Bias& b, const void* residual,
+                            const Dropout& drop, uint64_t* rng_used, void* y, void* saved, unsigned char* ws, hipStream_t stream) {
     const long long M = d.M, K = d.K, N = d.N;
-    const LinearEpilogue e{b, residual, y, saved, d.activation, drop, M, d.N};
+    const LinearEpilogue e{b, residual, y, saved, d.activation, drop, (unsigned long long*)rng_used, M, d.N};
     if (p.few) {
         LAYER_HIP(launch_few_linear(FewJob{x, W, (int)M, d.K, d.N}, p.few_splits, (float*)(ws + p.off_slots), e, stream));
         return RNNT_OK;
@@ -219,15 +219,16 @@ rnnt_status linear_bwd_bf16(const rnnt_linear_desc& d, const LinearPlan& p, cons
     return RNNT_OK;
 }
 
-rnnt_status linear_fwd_f32(const rnnt_linear_desc& d, const LinearPlan& p, const float* x, const float* W, const float* b, const float* residual,
-                           const Dropout& drop, float* y, float* saved, unsigned char* ws, hipStream_t stream) {
+rnnt_status linear_fwd_f32(const rnnt_linear_desc& d, const LinearPlan& p, const float* x, const float* W, const Bias& b, const float* residual,
+                           const Dropout& drop, uint64_t* rng_used, float* y, float* saved, unsigned char* ws, hipStream_t stream) {
     const long long M = d.M, K = d.K, N = d.N;
     if (p.copy_x) LAYER_HIP(launch_pad(x, 4, M, K, 0, ws + p.off_x, M, p.Kp, stream));
     if (p.copy_w) LAYER_HIP(launch_pad(W, 4, K, N, 0, ws + p.off_w, p.Kp, p.Np, stream));
     float* z = p.y32 > 1 || N % 4 != 0 ? (float*)(ws + p.off_slots) : saved ? saved : y;
     LAYER_HIP(launch_gemm_f32_split(0, 1, p.copy_x ? (const float*)(ws + p.off_x) : x, p.Kp, p.copy_w ? (const float*)(ws + p.off_w) : W, p.Np, z, p.Np, M,
                                     p.Np, p.Kp, p.y32, M * p.Np, stream));
-    LAYER_HIP(launch_linear_rows_f32(z, p.Np, p.y32, M * p.Np, b, residual, y, saved, M, d.N, d.activation, drop, stream));
+    LAYER_HIP(launch_linear_rows_f32(z, p.Np, p.y32, M * p.Np, b, residual, y, saved, M, d.N, d.activation, drop,
+                                     (unsigned long long*)rng_used, stream));
     return RNNT_OK;
 }
 
@@ -266,6 +267,7 @@ rnnt_status linear_bwd_f32(const rnnt_linear_desc& d, const LinearPlan& p, const
 rnnt_status check_ce(const rnnt_ce_desc* d, bool grads) {
     if (!d) return RNNT_ERR_NULL;
     if (d->R < 0 || d->R > MAX_ROWS || d->D < 1 || d->D > MAX_WIDTH || d->V < 1 || d->V > MAX_WIDTH) return RNNT_ERR_SHAPE;
+    if (d->bias_bf16 < 0 || d->bias_bf16 > 1) return RNNT_ERR_SHAPE;
     if (d->dtype != RNNT_F32 && d->dtype != RNNT_BF16) return RNNT_ERR_UNSUPPORTED;
     if (grads) {
         if (d->accumulate_params < 0 || d->accumulate_params > 1 || d->param_grads_bf16 < 0 || d->param_grads_bf16 > 3) return RNNT_ERR_SHAPE;
@@ -373,9 +375,10 @@ CePlan plan_ce(const rnnt_ce_desc& d, bool grads, size_t budget) {
     return best;
 }
 
-rnnt_status run_ce(const rnnt_ce_desc& d, const CePlan& p, const void* x, const void* W, const float* b, const int32_t* label, const float* row_weight,
+rnnt_status run_ce(const rnnt_ce_desc& d, const CePlan& p, const void* x, const void* W, const void* b_ptr, const int32_t* label, const float* row_weight,
                    float* loss, void* dx, void* dW, void* db, unsigned char* ws, hipStream_t stream) {
     const long long D = d.D, V = d.V;
+    const Bias b{b_ptr, d.bias_bf16 != 0};
     const CeRows rows{(int*)(ws + p.off_count), (int*)(ws + p.off_index), (int*)(ws + p.off_label), (float*)(ws + p.off_weight)};
     const int size = p.bf16 ? 2 : 4;
     if (p.identity) {
@@ -491,20 +494,22 @@ extern "C" size_t rnnt_linear_workspace_bytes(const rnnt_linear_desc* desc, int3
     return plan_linear(*desc, backward != 0).bytes;
 }
 
-extern "C" rnnt_status rnnt_linear_fwd(const rnnt_linear_desc* desc, const void* x, const void* W, const float* b, const void* residual,
-                                       const uint64_t* rng, void* y, void* saved, void* workspace, size_t workspace_bytes, void* hip_stream) {
+extern "C" rnnt_status rnnt_linear_fwd(const rnnt_linear_desc* desc, const void* x, const void* W, const void* b, const void* residual,
+                                       const uint64_t* rng, uint64_t* rng_used, void* y, void* saved, void* workspace, size_t workspace_bytes, void* hip_stream) {
     const rnnt_status st = check_linear(desc, false);
     if (st != RNNT_OK) return st;
     if (!W || (desc->M > 0 && (!x || !y))) return RNNT_ERR_NULL;
     const Dropout drop = make_dropout(*desc, rng);
     if (drop.cut != 0 && !rng) return RNNT_ERR_NULL;
-    if (!aligned({x, W, b, residual, y, saved}) || (uintptr_t)rng % 8 != 0) return RNNT_ERR_UNSUPPORTED;
+    if (!aligned({x, W, b, residual, y, saved}) || (((uintptr_t)rng | (uintptr_t)rng_used) % 8) != 0) return RNNT_ERR_UNSUPPORTED;
+    if (rng_used && !rng) return RNNT_ERR_NULL;
     const LinearPlan p = plan_linear(*desc, false);
     if (!workspace_ok(workspace, workspace_bytes, p.bytes)) return RNNT_ERR_WORKSPACE;
     if (desc->M == 0) return RNNT_OK;
     unsigned char* ws = (unsigned char*)workspace;
-    if (p.bf16) return linear_fwd_bf16(*desc, p, x, W, b, residual, drop, y, saved, ws, (hipStream_t)hip_stream);
-    return linear_fwd_f32(*desc, p, (const float*)x, (const float*)W, b, (const float*)residual, drop, (float*)y, (float*)saved, ws,
+    const Bias bias{b, desc->bias_bf16 != 0};
+    if (p.bf16) return linear_fwd_bf16(*desc, p, x, W, bias, residual, drop, rng_used, y, saved, ws, (hipStream_t)hip_stream);
+    return linear_fwd_f32(*desc, p, (const float*)x, (const float*)W, bias, (const float*)residual, drop, rng_used, (float*)y, (float*)saved, ws,
                           (hipStream_t)hip_stream);
 }
 
@@ -529,7 +534,7 @@ extern "C" size_t rnnt_ce_loss_workspace_bytes(const rnnt_ce_desc* desc, int32_t
     return plan_ce(*desc, grads != 0, budget_bytes).bytes;
 }
 
-static rnnt_status ce_loss(const rnnt_ce_desc* desc, bool grads, const void* x, const void* W, const float* b, const int32_t* label,
+static rnnt_status ce_loss(const rnnt_ce_desc* desc, bool grads, const void* x, const void* W, const void* b, const int32_t* label,
                            const float* row_weight, float* loss, void* dx, void* dW, void* db, void* workspace, size_t workspace_bytes,
                            void* hip_stream) {
     const rnnt_status st = check_ce(desc, grads);
@@ -546,11 +551,11 @@ static rnnt_status ce_loss(const rnnt_ce_desc* desc, bool grads, const void* x, 
     return run_ce(*desc, p, x, W, b, label, row_weight, loss, dx, dW, db, (unsigned char*)workspace, (hipStream_t)hip_stream);
 }
 
-extern "C" rnnt_status rnnt_ce_loss_fwd(const rnnt_ce_desc* desc, const void* x, const void* W, const float* b, const int32_t* label, float* loss,
+extern "C" rnnt_status rnnt_ce_loss_fwd(const rnnt_ce_desc* desc, const void* x, const void* W, const void* b, const int32_t* label, float* loss,
                                         void* workspace, size_t workspace_bytes, void* hip_stream) {
     return ce_loss(desc, false, x, W, b, label, nullptr, loss, nullptr, nullptr, nullptr, workspace, workspace_bytes, hip_stream);
 }
-extern "C" rnnt_status rnnt_ce_loss_fwd_bwd(const rnnt_ce_desc* desc, const void* x, const void* W, const float* b, const int32_t* label,
+extern "C" rnnt_status rnnt_ce_loss_fwd_bwd(const rnnt_ce_desc* desc, const void* x, const void* W, const void* b, const int32_t* label,
                                             const float* row_weight, float* loss, void* dx, void* dW, void* db, void* workspace,
                                             size_t workspace_bytes, void* hip_stream) {
     return ce_loss(desc, true, x, W, b, label, row_weight, loss, dx, dW, db, workspace, workspace_bytes, hip_stream);

@@ -17,6 +17,17 @@ struct Dropout {
     float scale;
 };
 
+// float or bfloat16, or none (p null: zeros)
+struct Bias {
+    const void* p;
+    bool bf16;
+#ifdef __HIPCC__
+    __device__ __forceinline__ float at(int n) const {
+        return p == nullptr ? 0.0f : bf16 ? (float)((const __bf16*)p)[n] : ((const float*)p)[n];
+    }
+#endif
+};
+
 // ---- bf16 matrix products ---------------------------------------------------------------------------------------------
 struct GemmOperand {
     const void* p;
@@ -50,12 +61,13 @@ inline size_t gemm_slot_bytes(const GemmPlan& p, long long M, long long N) {
 
 // y = residual + dropout(act(z + bias)), z rounded to fp16 into saved
 struct LinearEpilogue {
-    const float* bias;                   // or null
+    Bias bias;
     const void* residual;                // bf16, or null
     void* y;                             // bf16
     void* saved;                         // fp16, or null
     int act;
     Dropout drop;
+    unsigned long long* rng_used;        // drop.state as the kernels saw it, or null
     long long M;
     int N;
 };
@@ -73,7 +85,7 @@ struct StoreEpilogue {
 // Scores h = v + bias of a tile row -> their maximum m and S = sum 2^15 e^{h - m} (stats[row * tiles_n + tile]), the label's score, and, where kept is
 // not null, 2^15 e^{h - m} as fp16.
 struct CeEpilogue {
-    const float* bias;
+    Bias bias;
     int V;
     const int* label;
     float* label_score;
@@ -158,8 +170,8 @@ hipError_t launch_dz(bool bf16, const DzArgs& a, hipStream_t stream);
 hipError_t launch_sum_parts(const SumJob& j, hipStream_t stream);
 // fp32: z (the sum of `splits` arrays of pitch ld, `stride` apart; one may be saved or y) + bias -> saved (or null), y = residual + dropout(act(z + bias)); all
 // but z dense [M, N]
-hipError_t launch_linear_rows_f32(const float* z, long long ld, int splits, long long stride, const float* bias, const float* residual, float* y,
-                                  float* saved, long long M, int N, int act, const Dropout& drop, hipStream_t stream);
+hipError_t launch_linear_rows_f32(const float* z, long long ld, int splits, long long stride, const Bias& bias, const float* residual, float* y,
+                                  float* saved, long long M, int N, int act, const Dropout& drop, unsigned long long* rng_used, hipStream_t stream);
 // dst [.., N] (+)= the sum of `splits` arrays of pitch ld, `stride` apart, rows as they are or row i to row_map[i] (those < 0 nowhere)
 hipError_t launch_reduce_f32(const float* src, long long ld, int splits, long long stride, const int* row_map, float* dst, long long rows, int N, bool add,
                              hipStream_t stream);
@@ -195,7 +207,7 @@ hipError_t launch_ce_finish(const CeChunk& c, hipStream_t stream);
 inline bool ce_grad_finishes(int tiles_n) { return tiles_n <= 16; }
 hipError_t launch_ce_grad(const CeChunk& c, void* kept, long long pitch, float* part, hipStream_t stream);
 // fp32: scores [rows, V] (pitch ld, without the bias) -> loss and, with grads, score gradients in place (zeros in rows behind the last)
-hipError_t launch_ce_rows_f32(const CeRows& r, long long row0, long long rows, float* scores, long long ld, int V, const float* b, float* loss,
+hipError_t launch_ce_rows_f32(const CeRows& r, long long row0, long long rows, float* scores, long long ld, int V, const Bias& b, float* loss,
                               bool grads, hipStream_t stream);
 // total = sum of weight[r] loss[r] over the rows whose weight is not 0 (null: ones)
 hipError_t launch_ce_total(const float* loss, const float* weight, long long R, float* total, hipStream_t stream);

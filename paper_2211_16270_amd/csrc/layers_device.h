@@ -190,10 +190,15 @@ __device__ __forceinline__ float for_f16(float z) {
 }
 
 // ---- what becomes of columns n .. n + 7 (n a multiple of 8) of row m of a product --------------------------------------
-__device__ __forceinline__ void load_bias8(const float* bias, int n, int N, float (&b)[8]) {
+__device__ __forceinline__ void load_bias8(const Bias& bias, int n, int N, float (&b)[8]) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) b[j] = bias != nullptr ? bias[n + j < N ? n + j : N - 1] : 0.0f;
+    for (int j = 0; j < 8; ++j) b[j] = bias.at(n + j < N ? n + j : N - 1);
 }
+// (by one workgroup of a launch whose epilogue it is)
+__device__ __forceinline__ void pass_rng(const LinearEpilogue& e) {
+    if (e.rng_used != nullptr && threadIdx.x < 2) e.rng_used[threadIdx.x] = e.drop.state[threadIdx.x];
+}
+__device__ __forceinline__ void pass_rng(const StoreEpilogue&) {}
 struct LinearStore {
     __device__ static __forceinline__ void store(const LinearEpilogue& e, int, long long m, int n, float (&v)[8], const float (&b)[8]) {
         if (m >= e.M || n >= e.N) return;
@@ -252,8 +257,18 @@ __device__ __forceinline__ void sum_parts(const SumJob& j, int blocks, int R, in
         blocks = r < blocks ? (int)r : blocks;
     }
     float s = 0.0f;
-    if (n < j.N)
-        for (int b = row; b < blocks; b += 8) s += j.part[(size_t)b * j.ld + n];
+    if (n < j.N) {
+        const float* p = j.part + n;
+        int b = row;
+        for (; b + 56 < blocks; b += 64) {                         // (eight loads at once: one by one their latency is all there is)
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = p[(size_t)(b + 8 * k) * j.ld];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s += v[k];
+        }
+        for (; b < blocks; b += 8) s += p[(size_t)b * j.ld];
+    }
     red[row][c] = s;
     __syncthreads();
     if (row == 0 && n < j.N) {
