@@ -122,6 +122,58 @@ struct TileShape {
     static constexpr unsigned B_AT = 3 * OPER;
 };
 
+// Zeros, or the bias of columns n .. n + 63 (n the same for all lanes) with `beyond` from N on, as they stand in a lane's registers.  Scalar loads: a vector
+// load's wait would wait for all the copies sent before it (CE, 1632 rows: 12.9 us, 14.9 with such loads).
+struct NoBias {
+    __device__ __forceinline__ void operator()(int, int, float (&b)[2][16]) const {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) b[j][q] = 0.0f;
+    }
+};
+struct ColumnBias {
+    Bias bias;
+    int N;
+    float beyond;
+    __device__ __forceinline__ void operator()(int n, int hb, float (&b)[2][16]) const {
+        if (n + 64 > N) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int q = 0; q < 16; ++q) {
+                    const int c = n + 32 * j + 8 * (q >> 2) + 4 * hb + (q & 3);
+                    const float v = bias.at(c < N ? c : N - 1);
+                    b[j][q] = c < N ? v : beyond;
+                }
+        } else if (bias.p == nullptr) {
+            NoBias{}(n, hb, b);
+        } else if (!bias.bf16) {
+            const float __attribute__((address_space(4)))* p = (const float __attribute__((address_space(4)))*)((const float*)bias.p + n);
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int q = 0; q < 16; ++q) {
+                    const int c = 32 * j + 8 * (q >> 2) + (q & 3);
+                    const float lo = p[c], hi = p[c + 4];
+                    b[j][q] = hb ? hi : lo;
+                }
+        } else {
+            const unsigned __attribute__((address_space(4)))* p =
+                (const unsigned __attribute__((address_space(4)))*)((const unsigned short*)bias.p + n);
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int q = 0; q < 16; q += 2) {
+                    const int c = (32 * j + 8 * (q >> 2) + (q & 3)) / 2;
+                    const unsigned lo = p[c], hi = p[c + 2], w = hb ? hi : lo;
+                    b[j][q] = __uint_as_float(w << 16);
+                    b[j][q + 1] = __uint_as_float(w & 0xffff0000u);
+                }
+        }
+    }
+};
+
 // acc[i][j] = the tile's product over the stages [s0, s1): block of 32 rows i of the wave's part, block of 32 columns j.  The matrix instruction takes B's
 // fragment first, so lane l holds row l % 32 and register 4 q + r column 8 q + 4 (l / 32) + r.
 // LDS holds three stages of A and two of B.  A stage is four k16-steps; the fragments of the next step are read behind the MFMAs of the present one.
@@ -129,9 +181,10 @@ struct TileShape {
 // go out in the first two steps (their buffer became free a stage ago), those of B in the fourth, into the buffer that has just become free.  (Two stages of
 // both, all copies in the fourth step: 8192^3 1250 to 1280 TFLOP/s, now 1335; without any copies 1470 to 1510.  The rest of the loss is the prologue and
 // the epilogue, which nothing hides: K = 1024 940 TFLOP/s.)  A wave has priority while it sends MFMAs (K = 1024: 874 without).
-template <class TS, bool AKS, bool BKS>
+// init: what the sums of the columns start from.
+template <class TS, bool AKS, bool BKS, class INIT>
 __device__ __forceinline__ void gemm_tile(f32x16 (&acc)[TS::MT][TS::NT], const GemmOperand& ga, const GemmOperand& gb, long long m0, long long n0,
-                                          long long M, long long N, int s0, int s1, unsigned char* smem) {
+                                          long long M, long long N, int s0, int s1, unsigned char* smem, const INIT& init) {
     constexpr int MT = TS::MT, NT = TS::NT;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int wm = wave / TS::WN, wn = wave % TS::WN;
@@ -148,11 +201,17 @@ __device__ __forceinline__ void gemm_tile(f32x16 (&acc)[TS::MT][TS::NT], const G
     const unsigned base = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem;
     const unsigned dst_a = base + (unsigned)(wave * LA::PW) * 1024u, dst_b = base + TS::B_AT + (unsigned)(wave * LB::PW) * 1024u;
 
+    auto start = [&] {
+        float b[NT][16];
+        init((int)n0 + wn * NT * 32, lane >> 5, b);
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = f32x16{0};
-    if (s0 >= s1) return;
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int q = 0; q < 16; ++q) acc[i][j][q] = b[j][q];
+    };
+    if (s0 >= s1) return start();
     const int last = s1 - 1;
     auto issue_a = [&](int s, unsigned buf) {
         const unsigned char* p = la.stage(s);
@@ -167,6 +226,7 @@ __device__ __forceinline__ void gemm_tile(f32x16 (&acc)[TS::MT][TS::NT], const G
     issue_b(s0, 0u);
     issue_a(s0 < last ? s0 + 1 : last, TS::OPER);
     issue_b(s0 < last ? s0 + 1 : last, TS::OPER);
+    start();
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LA::PW + LB::PW) : "memory");
     __syncthreads();
     static_for<0, MT>([&](auto i) { fa[0][decltype(i)::value] = ra.template read<0, decltype(i)::value>(smem); });
@@ -231,29 +291,49 @@ __device__ __forceinline__ void gemm_tile(f32x16 (&acc)[TS::MT][TS::NT], const G
     __syncthreads();
 }
 
-// A 32 x 32 block of results through 4 KiB of LDS of the wave's own: lane l comes away with eight consecutive columns 8 (l % 4) .. + 7 of rows l / 4 and
-// 16 + l / 4, so that what follows touches 64 bytes of a row in one piece.  (16-byte pieces of a row at their place xor (row % 8): all banks.)
+// Eight columns of the lane's row: granule p of block j of accumulator d, columns 16 p + 8 (l / 32) .. + 7 of the block
+__device__ __forceinline__ void granule8(const f32x16& d, int p, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        unsigned x = __float_as_uint(d[8 * p + i]), y = __float_as_uint(d[8 * p + 4 + i]);
+        swap_halves(x, y);
+        v[i] = __uint_as_float(x);
+        v[4 + i] = __uint_as_float(y);
+    }
+}
+// 32 rows x 64 columns of 16-bit results through 4 KiB of LDS of the wave's own, so that a store covers whole lines: lane l brings granule (j, p) of row
+// l % 32 and takes, for t = 0 .. 3, the eight columns 8 (l % 8) .. + 7 of row 8 t + l / 8.  (Granule c of row r at place c xor (r % 8): all banks.)
 constexpr unsigned TURN_BYTES = 4096;
-__device__ __forceinline__ void turn_block(const f32x16& d, unsigned char* area, int lane) {
-    const int row = lane & 31, hb = lane >> 5;
+__device__ __forceinline__ void turn_put(unsigned char* area, int j, int p, int lane, const u32x4& x) {
+    const int row = lane & 31, c = 4 * j + 2 * p + (lane >> 5);
+    *reinterpret_cast<u32x4*>(area + row * 128 + ((c ^ (row & 7)) << 4)) = x;
+}
+__device__ __forceinline__ u32x4 turn_take(const unsigned char* area, int t, int lane) {
+    const int row = 8 * t + (lane >> 3);
+    return *reinterpret_cast<const u32x4*>(area + row * 128 + (((lane & 7) ^ (row & 7)) << 4));
+}
+// The same with 32 x 64 fp32 results and 8 KiB: what is done with them is done once per row piece, in a loop.  (16-byte piece c of row r at place
+// c xor (r % 16).)
+constexpr unsigned TURN32_BYTES = 8192;
+__device__ __forceinline__ void turn32_put(unsigned char* area, int j, const f32x16& d, int lane) {
+    const int row = lane & 31;
 #pragma unroll
     for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<f32x4*>(area + row * 128 + (((2 * q + hb) ^ (row & 7)) << 4)) = f32x4{d[4 * q], d[4 * q + 1], d[4 * q + 2], d[4 * q + 3]};
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        *reinterpret_cast<f32x4*>(area + row * 256 + (((8 * j + 2 * q + (lane >> 5)) ^ (row & 15)) << 4)) =
+            f32x4{d[4 * q], d[4 * q + 1], d[4 * q + 2], d[4 * q + 3]};
 }
-__device__ __forceinline__ void turned8(const unsigned char* area, int half, int lane, float (&v)[8]) {
-    const int row = 16 * half + (lane >> 2), g = lane & 3;
-    const f32x4 a = *reinterpret_cast<const f32x4*>(area + row * 128 + (((2 * g) ^ (row & 7)) << 4));
-    const f32x4 b = *reinterpret_cast<const f32x4*>(area + row * 128 + (((2 * g + 1) ^ (row & 7)) << 4));
+__device__ __forceinline__ void turn32_take(const unsigned char* area, int t, int lane, float (&v)[8]) {
+    const int row = 8 * t + (lane >> 3), c = 2 * (lane & 7);
+    const f32x4 a = *reinterpret_cast<const f32x4*>(area + row * 256 + ((c ^ (row & 15)) << 4));
+    const f32x4 b = *reinterpret_cast<const f32x4*>(area + row * 256 + (((c + 1) ^ (row & 15)) << 4));
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         v[j] = a[j];
         v[4 + j] = b[j];
     }
 }
-__device__ __forceinline__ void turn_done() {
+// between the two, and before the area is written again
+__device__ __forceinline__ void turn_fence() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");

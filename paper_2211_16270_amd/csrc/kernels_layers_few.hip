@@ -30,7 +30,9 @@ struct FewLinear {
     __device__ __forceinline__ void operator()(int m, int n, int, float (&v)[8]) const {
         float b[8];
         LinearStore::bias(e, n, b);
-        LinearStore::store(e, 0, m, n, v, b);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] += b[k];
+        LinearStore::store(e, m, n, v, LinearStore::fetch(e, m, n));
     }
 };
 // Statistics of the 32 columns of a row (four neighbouring lanes hold them), as k_ce_scores leaves them for its tiles
@@ -67,9 +69,11 @@ struct FewCe {
 // rows x 32 columns of x W per workgroup, MT blocks of 16 rows.  A wave brings its steps (32 of k) of W through registers into LDS of its own, where the
 // transposing read makes MFMA fragments of them; x comes as fragments from memory.  The eight waves' sums meet in LDS.  Neighbouring column blocks share
 // lines of W: they go to one XCD.  What bounds it: latency (one token, K = 640, N = 2560: the launch, two trips to memory, the reduction).
+// WHOLE: K and N are multiples of 32, no piece has an end in it (the code for ends, eight loads under eight conditions for each load, takes longer to fetch
+// than to run).
 // A long sum is split over workgroups too (gridDim.y > 1), whose results go to slots [split][M][N up to 8]: 64 rows, K = 2560, N = 640 19.8 us in 20
 // workgroups, half of it x, which each of them reads whole.
-template <int MT, class E>
+template <int MT, bool WHOLE, class E>
 __global__ __launch_bounds__(64 * FW) void k_few_rows(FewJob j, E e, int blocks, float* __restrict__ slots, int per_split) {
     __shared__ __align__(16) unsigned char smem[FW * MT * 16 * FC * 4];
     static_assert(MT * 16 * FC * 4 >= 2048, "a step of W per wave");
@@ -98,10 +102,15 @@ __global__ __launch_bounds__(64 * FW) void k_few_rows(FewJob j, E e, int blocks,
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const int k = k0 + 16 * u + wk;
-            w[s][u] = raw8(W + (size_t)(k < K ? k : 0) * N, k < K ? wlive : 0);
+            if constexpr (WHOLE) w[s][u] = *reinterpret_cast<const bf16x8*>(W + (size_t)(k < K ? k : 0) * N);
+            else w[s][u] = raw8(W + (size_t)(k < K ? k : 0) * N, k < K ? wlive : 0);
         }
 #pragma unroll
-        for (int i = 0; i < MT; ++i) a[s][i] = raw8(x[i] + (k0 + xk < K ? k0 + xk : 0), row_ok[i] ? K - (k0 + xk) : 0);
+        for (int i = 0; i < MT; ++i) {
+            const bf16_t* p = x[i] + (k0 + xk < K ? k0 + xk : 0);
+            if constexpr (WHOLE) a[s][i] = *reinterpret_cast<const bf16x8*>(p);
+            else a[s][i] = raw8(p, row_ok[i] ? K - (k0 + xk) : 0);
+        }
     };
     const int fj = (lane >> 2) & 3, fc = lane & 3, fg = lane >> 4;
     auto step = [&](auto slot_tag) {
@@ -172,10 +181,14 @@ hipError_t launch_few(const FewJob& j, const E& e, int splits, float* slots, hip
     if (j.M <= 0 || j.M > FEW_ROWS) return j.M <= 0 ? hipSuccess : hipErrorInvalidValue;
     const int blocks = (j.N + FC - 1) / FC, per = ((j.K + 31) / 32 + splits - 1) / splits;
     const dim3 grid((unsigned)((blocks + 7) / 8 * 8), (unsigned)splits);
-    if (j.M <= 16) k_few_rows<1, E><<<grid, dim3(64 * FW), 0, stream>>>(j, e, blocks, slots, per);
-    else if (j.M <= 32) k_few_rows<2, E><<<grid, dim3(64 * FW), 0, stream>>>(j, e, blocks, slots, per);
-    else k_few_rows<4, E><<<grid, dim3(64 * FW), 0, stream>>>(j, e, blocks, slots, per);
-    return hipGetLastError();
+    const bool whole = j.K % 32 == 0 && j.N % FC == 0;
+    auto go = [&](auto mt) {
+        constexpr int MT = decltype(mt)::value;
+        if (whole) k_few_rows<MT, true, E><<<grid, dim3(64 * FW), 0, stream>>>(j, e, blocks, slots, per);
+        else k_few_rows<MT, false, E><<<grid, dim3(64 * FW), 0, stream>>>(j, e, blocks, slots, per);
+        return hipGetLastError();
+    };
+    return j.M <= 16 ? go(std::integral_constant<int, 1>{}) : j.M <= 32 ? go(std::integral_constant<int, 2>{}) : go(std::integral_constant<int, 4>{});
 }
 
 }  // namespace

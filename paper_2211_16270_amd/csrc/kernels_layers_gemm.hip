@@ -37,27 +37,32 @@ __device__ __forceinline__ void gemm_workgroup(const GemmJob& g, const E& e, int
     if (m0 >= x.M) return;
     const int s0 = t.split * per_split, s1 = s0 + per_split < x.stages ? s0 + per_split : x.stages;
     f32x16 acc[TS::MT][TS::NT];
-    gemm_tile<TS, AKS, BKS>(acc, g.A, g.B, m0, n0, g.a_rows, g.b_rows, s0, s1, smem);
+    constexpr bool LINEAR = std::is_same_v<E, LinearEpilogue>;
+    if constexpr (LINEAR) gemm_tile<TS, AKS, BKS>(acc, g.A, g.B, m0, n0, g.a_rows, g.b_rows, s0, s1, smem, ColumnBias{e.bias, e.N, 0.0f});
+    else gemm_tile<TS, AKS, BKS>(acc, g.A, g.B, m0, n0, g.a_rows, g.b_rows, s0, s1, smem, NoBias{});
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-    const int wm = wave / TS::WN, wn = wave % TS::WN;
+    const int wm = wave / TS::WN, wn = wave % TS::WN, n = (int)n0 + wn * TS::NT * 32 + 8 * (lane & 7);
+    unsigned char* area = smem + wave * TURN32_BYTES;
+    static_assert(TS::NT == 2 && TS::WAVES * TURN32_BYTES <= TS::SMEM, "a wave's 64 columns");
     typedef typename EpilogueOf<E>::type Store;
-    unsigned char* area = smem + wave * TURN_BYTES;
 #pragma unroll
-    for (int j = 0; j < TS::NT; ++j) {
-        const int n = (int)n0 + (wn * TS::NT + j) * 32 + 8 * (lane & 3);
-        float b[8];
-        Store::bias(e, n, b);
+    for (int i = 0; i < TS::MT; ++i) {
+        typename Store::Extra x[4];
 #pragma unroll
-        for (int i = 0; i < TS::MT; ++i) {
-            turn_block(acc[i][j], area, lane);
+        for (int k = 0; k < 4; ++k) x[k] = Store::fetch(e, m0 + (wm * TS::MT + i) * 32 + 8 * k + (lane >> 3), n);
+        turn32_put(area, 0, acc[i][0], lane);
+        turn32_put(area, 1, acc[i][1], lane);
+        turn_fence();
 #pragma unroll 1
-            for (int half = 0; half < 2; ++half) {
-                float v[8];
-                turned8(area, half, lane, v);
-                Store::store(e, t.split, m0 + (wm * TS::MT + i) * 32 + 16 * half + (lane >> 2), n, v, b);
-            }
-            turn_done();
+        for (int k = 0; k < 4; ++k) {
+            const long long m = m0 + (wm * TS::MT + i) * 32 + 8 * k + (lane >> 3);
+            float v[8];
+            turn32_take(area, k, lane, v);
+            // (a register array indexed by the loop's counter would lie in memory)
+            const typename Store::Extra r = k & 2 ? (k & 1 ? x[3] : x[2]) : (k & 1 ? x[1] : x[0]);
+            Store::store(e, m, n, v, r, t.split);
         }
+        turn_fence();
     }
 }
 
@@ -75,13 +80,15 @@ __global__ __launch_bounds__(TS::THREADS, 2) void k_layer_gemm(TileJob<E> j) {
     if (blockIdx.x == 0) pass_rng(j.e);
     gemm_workgroup<TS, AKS, BKS, E>(j.g, j.e, blockIdx.x, j.mt, j.nt, j.splits, j.per_split, smem);
 }
-// dx and dW
+// dx and dW; the product whose workgroups take longer goes first (CE, 9288 x 1024 x 32768, dx in 148 workgroups of 512 stages: behind dW's 512 of 146 the
+// two took 1200 us, in front of them xxx).
 template <class TS>
-__global__ __launch_bounds__(TS::THREADS, 2) void k_layer_grads(TileJob<StoreEpilogue> x, TileJob<StoreEpilogue> w, int wgs_w) {
+__global__ __launch_bounds__(TS::THREADS, 2) void k_layer_grads(TileJob<StoreEpilogue> x, TileJob<StoreEpilogue> w, int wgs_x, int wgs_w) {
     extern __shared__ __align__(16) unsigned char smem[];
-    const int L = blockIdx.x;
-    if (L < wgs_w) gemm_workgroup<TS, true, true, StoreEpilogue>(w.g, w.e, L, w.mt, w.nt, w.splits, w.per_split, smem);
-    else gemm_workgroup<TS, false, false, StoreEpilogue>(x.g, x.e, L - wgs_w, x.mt, x.nt, x.splits, x.per_split, smem);
+    const bool x_first = x.per_split > w.per_split;
+    const int L = blockIdx.x, is_x = x_first ? L < wgs_x : L >= wgs_w;
+    if (is_x) gemm_workgroup<TS, false, false, StoreEpilogue>(x.g, x.e, x_first ? L : L - wgs_w, x.mt, x.nt, x.splits, x.per_split, smem);
+    else gemm_workgroup<TS, true, true, StoreEpilogue>(w.g, w.e, x_first ? L - wgs_x : L, w.mt, w.nt, w.splits, w.per_split, smem);
 }
 
 // The sum of the splits' results, in order, and the epilogue.  One thread per eight columns.
@@ -101,6 +108,8 @@ __device__ __forceinline__ void reduce_workgroup(const ReduceJob<E>& r, unsigned
     const long long per = r.Np / 8, m = i / per;
     const int n = (int)(i - m * per) * 8;
     if (m >= job_extent(r.g).M) return;
+    typedef typename EpilogueOf<E>::type Store;
+    const typename Store::Extra x = Store::fetch(r.e, m, n);
     const float* s = r.slots + (size_t)m * r.Np + n;
     f32x4 a = f32x4{0}, b = f32x4{0};
 #pragma unroll 4
@@ -109,9 +118,10 @@ __device__ __forceinline__ void reduce_workgroup(const ReduceJob<E>& r, unsigned
         b += *reinterpret_cast<const f32x4*>(s + 4);
     }
     float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}, bias[8];
-    typedef typename EpilogueOf<E>::type Store;
     Store::bias(r.e, n, bias);
-    Store::store(r.e, 0, m, n, v, bias);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] += bias[k];
+    Store::store(r.e, m, n, v, x);
 }
 template <class E>
 __global__ __launch_bounds__(256) void k_layer_reduce(ReduceJob<E> r) {
@@ -139,23 +149,12 @@ __global__ __launch_bounds__(TS::THREADS, 2) void k_ce_scores(GemmJob g, CeEpilo
     const long long m0 = (long long)t.m * TS::BM, n0 = (long long)t.n * TS::BN;
     if (m0 >= x.M) return;
     f32x16 acc[TS::MT][TS::NT];
-    gemm_tile<TS, false, true>(acc, g.A, g.B, m0, n0, g.a_rows, g.b_rows, 0, g.stages, smem);
+    // (entries beyond the vocabulary are -inf)
+    gemm_tile<TS, false, true>(acc, g.A, g.B, m0, n0, g.a_rows, g.b_rows, 0, g.stages, smem, ColumnBias{e.bias, e.V, RNNT_NEG_INF});
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l32 = lane & 31, hb = lane >> 5;
     const int wm = wave / TS::WN, wn = wave % TS::WN;
     float* top = reinterpret_cast<float*>(smem);                  // [WN][BM]
     float* sum = top + TS::WN * TS::BM;                           // [WN][BM]
-    // scores; entries beyond the vocabulary are -inf
-#pragma unroll
-    for (int j = 0; j < TS::NT; ++j)
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int n = (int)n0 + (wn * TS::NT + j) * 32 + 8 * q + 4 * hb + r;
-                const float b = e.bias.at(n < e.V ? n : e.V - 1);
-#pragma unroll
-                for (int i = 0; i < TS::MT; ++i) acc[i][j][4 * q + r] = n < e.V ? acc[i][j][4 * q + r] + b : RNNT_NEG_INF;
-            }
 #pragma unroll
     for (int i = 0; i < TS::MT; ++i) {
         const int row = (wm * TS::MT + i) * 32 + l32;
@@ -199,20 +198,20 @@ __global__ __launch_bounds__(TS::THREADS, 2) void k_ce_scores(GemmJob g, CeEpilo
         if constexpr (KEEP) {
             unsigned char* area = smem + 2 * TS::WN * TS::BM * 4 + wave * TURN_BYTES;
 #pragma unroll
-            for (int j = 0; j < TS::NT; ++j) {
-                turn_block(acc[i][j], area, lane);
+            for (int k = 0; k < 4; ++k) {
+                float v[8];
+                granule8(acc[i][k >> 1], k & 1, v);
+                f16x8 h;
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    float v[8];
-                    turned8(area, half, lane, v);
-                    f16x8 h;
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) h[k] = (_Float16)v[k];
-                    *reinterpret_cast<f16x8*>((_Float16*)e.kept + (size_t)(m0 + (wm * TS::MT + i) * 32 + 16 * half + (lane >> 2)) * e.pitch + n0 +
-                                              (wn * TS::NT + j) * 32 + 8 * (lane & 3)) = h;
-                }
-                turn_done();
+                for (int x = 0; x < 8; ++x) h[x] = (_Float16)v[x];
+                turn_put(area, k >> 1, k & 1, lane, __builtin_bit_cast(u32x4, h));
             }
+            turn_fence();
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                *reinterpret_cast<u32x4*>((_Float16*)e.kept + (size_t)(m0 + (wm * TS::MT + i) * 32 + 8 * k + (lane >> 3)) * e.pitch + n0 +
+                                          wn * TS::NT * 32 + 8 * (lane & 7)) = turn_take(area, k, lane);
+            turn_fence();
         }
         if (wn == 0 && hb == 0) e.stats[(size_t)(m0 + row) * e.tiles_n + t.n].x = m;
     }
@@ -279,7 +278,7 @@ hipError_t grad_gemms(const GradGemm& dx, const GradGemm& dw, hipStream_t stream
     if (dw.g.M > 0) w = tile_job<TS>(dw.g, dw.splits > 1 ? slot_epilogue(dw.g, dw.slots) : dw.e, dw.splits, dw.splits > 1 ? dw.per_split : dw.g.stages);
     const long long nx = x.workgroups(), nw = w.workgroups();
     if (nx + nw > 0x7ffffff0LL) return hipErrorInvalidValue;
-    return launch_tiles<&k_layer_grads<TS>, TS>(nx + nw, stream, x, w, (int)nw);
+    return launch_tiles<&k_layer_grads<TS>, TS>(nx + nw, stream, x, w, (int)nx, (int)nw);
 }
 
 }  // namespace

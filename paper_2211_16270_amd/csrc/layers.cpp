@@ -177,7 +177,7 @@ rnnt_status linear_bwd_bf16(const rnnt_linear_desc& d, const LinearPlan& p, cons
     const long long M = d.M, K = d.K, N = d.N;
     float* part = (float*)(ws + p.off_part);
     if (M > 0 && (db || (p.own_dz && (dx || dW)))) {
-        const DzArgs a{dy, d.activation == ACT_NONE ? nullptr : saved, p.own_dz ? ws + p.off_dz : nullptr, db ? part : nullptr, M,
+        const DzArgs a{dy, d.activation == ACT_NONE ? nullptr : saved, p.own_dz && (dx || dW) ? ws + p.off_dz : nullptr, db ? part : nullptr, M,
                        p.own_dz ? p.Mp : M, d.N, p.Np, d.activation, drop};
         LAYER_HIP(launch_dz(true, a, stream));
     }
@@ -237,7 +237,7 @@ rnnt_status linear_bwd_f32(const rnnt_linear_desc& d, const LinearPlan& p, const
     const long long M = d.M, K = d.K, N = d.N;
     float* part = (float*)(ws + p.off_part);
     if (M > 0 && (db || (p.own_dz && (dx || dW)))) {
-        const DzArgs a{dy, d.activation == ACT_NONE ? nullptr : saved, p.own_dz ? ws + p.off_dz : nullptr, db ? part : nullptr, M, M, d.N, p.Np,
+        const DzArgs a{dy, d.activation == ACT_NONE ? nullptr : saved, p.own_dz && (dx || dW) ? ws + p.off_dz : nullptr, db ? part : nullptr, M, M, d.N, p.Np,
                        d.activation, drop};
         LAYER_HIP(launch_dz(false, a, stream));
     }

@@ -64,6 +64,26 @@ __device__ __forceinline__ void store8(T* p, int live, const float (&v)[8]) {
     }
 }
 
+// Eight packed 16-bit values, zeros from `live` on
+template <typename T>
+__device__ __forceinline__ typename Vec8<T>::type take8(const T* p, int live) {
+    if (live >= 8) return *reinterpret_cast<const typename Vec8<T>::any*>(p);
+    typename Vec8<T>::type x = {};
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (j < live) x[j] = p[j];
+    return x;
+}
+// The first `live` of eight packed 16-bit values
+template <typename T, typename V>
+__device__ __forceinline__ void put8(T* p, int live, const V& x) {
+    if (live >= 8) *reinterpret_cast<typename Vec8<T>::any*>(p) = x;
+    else
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < live) p[j] = x[j];
+}
+
 // Philox4x32-10 (Salmon, Moraes, Dror, Shaw: Parallel random numbers, as easy as 1, 2, 3; 2011) with key {seed} on the counter {column / 8, row, offset}:
 // the 128 bits of eight columns, 16 for each.
 struct RandomBits8 {
@@ -181,12 +201,20 @@ __device__ __forceinline__ void act_grad8(int act, const float (&z)[8], float (&
 }
 
 // A saved pre-activation: fp16 (11 bits, where bf16's eight would add as much to the gradient's error as its own rounding does), beyond the largest
-// one that largest one (there act' has its limit), and a nonzero one stays nonzero (its sign is relu's derivative).
-__device__ __forceinline__ float for_f16(float z) {
-    float c = z > 65504.0f ? 65504.0f : z < -65504.0f ? -65504.0f : z;             // (NaN stays)
-    if (c > 0.0f && c < 5.9604644775390625e-8f) c = 5.9604644775390625e-8f;
-    if (c < 0.0f && c > -5.9604644775390625e-8f) c = -5.9604644775390625e-8f;
-    return c;
+// one that largest one (there act' has its limit).  relu's derivative is its sign: a nonzero one stays nonzero.
+__device__ __forceinline__ f16x8 saved8(int act, const float (&z)[8]) {
+    f16x8 s;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float c = __builtin_amdgcn_fmed3f(z[j], -65504.0f, 65504.0f);
+        s[j] = (_Float16)(z[j] == z[j] ? c : z[j]);
+    }
+    if (act == ACT_RELU) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (s[j] == (_Float16)0.0f && z[j] != 0.0f) s[j] = z[j] > 0.0f ? (_Float16)5.9604644775390625e-8f : (_Float16)-5.9604644775390625e-8f;
+    }
+    return s;
 }
 
 // ---- what becomes of columns n .. n + 7 (n a multiple of 8) of row m of a product --------------------------------------
@@ -199,40 +227,35 @@ __device__ __forceinline__ void pass_rng(const LinearEpilogue& e) {
     if (e.rng_used != nullptr && threadIdx.x < 2) e.rng_used[threadIdx.x] = e.drop.state[threadIdx.x];
 }
 __device__ __forceinline__ void pass_rng(const StoreEpilogue&) {}
+// v: columns n .. n + 7 of row m of the product, with the bias.  fetch: what of memory the epilogue needs (sent ahead of the work on v).
 struct LinearStore {
-    __device__ static __forceinline__ void store(const LinearEpilogue& e, int, long long m, int n, float (&v)[8], const float (&b)[8]) {
+    typedef bf16x8 Extra;
+    __device__ static __forceinline__ Extra fetch(const LinearEpilogue& e, long long m, int n) {
+        Extra r = bf16x8{0};
+        if (e.residual != nullptr && m < e.M && n < e.N) r = take8((const bf16_t*)e.residual + (size_t)m * e.N + n, e.N - n);
+        return r;
+    }
+    __device__ static __forceinline__ void store(const LinearEpilogue& e, long long m, int n, float (&v)[8], const Extra& r, int = 0) {
         if (m >= e.M || n >= e.N) return;
         const size_t at = (size_t)m * e.N + n;
-        const int live = e.N - n;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += b[j];
-        if (e.saved != nullptr) {
-            float h[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) h[j] = for_f16(v[j]);
-            store8((_Float16*)e.saved + at, live, h);
-        }
+        if (e.saved != nullptr) put8((_Float16*)e.saved + at, e.N - n, saved8(e.act, v));
         act8<true>(e.act, v);
         drop8(e.drop, m, n, v);
-        if (e.residual != nullptr) {
-            float r[8];
-            load8((const bf16_t*)e.residual + at, live, r);
+        bf16x8 y;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] += r[j];
-        }
-        store8((bf16_t*)e.y + at, live, v);
+        for (int j = 0; j < 8; ++j) y[j] = (bf16_t)(v[j] + (float)r[j]);
+        put8((bf16_t*)e.y + at, e.N - n, y);
     }
     __device__ static __forceinline__ void bias(const LinearEpilogue& e, int n, float (&b)[8]) { load_bias8(e.bias, n < e.N ? n : e.N - 1, e.N, b); }
 };
 struct PlainStore {
-    __device__ static __forceinline__ void store(const StoreEpilogue& e, int split, long long m, int n, float (&v)[8], const float (&)[8]) {
-        if (m >= e.M || n >= e.N) return;
-        long long row = m;
-        if (e.row_map != nullptr) {
-            row = e.row_map[m];
-            if (row < 0) return;
-        }
-        const size_t at = (size_t)split * e.split_stride + (size_t)row * e.ld + n;
+    typedef long long Extra;             // the output's row, -1: nowhere
+    __device__ static __forceinline__ Extra fetch(const StoreEpilogue& e, long long m, int n) {
+        return m >= e.M || n >= e.N ? -1 : e.row_map != nullptr ? (long long)e.row_map[m] : m;
+    }
+    __device__ static __forceinline__ void store(const StoreEpilogue& e, long long, int n, float (&v)[8], const Extra& x, int split = 0) {
+        if (x < 0) return;
+        const size_t at = (size_t)split * e.split_stride + (size_t)x * e.ld + n;
         const int live = e.N - n;
         if (e.prev != nullptr) {
             float p[8];
