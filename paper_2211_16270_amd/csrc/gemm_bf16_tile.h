@@ -20,7 +20,8 @@ constexpr int GK = 64;
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x8_t __attribute__((ext_vector_type(8)));
 
-template <int R, bool KS, int WAVES>
+// SIDE: 0 A, 1 B of a product of parts (which part a stage takes), -1 a product of bf16 values
+template <int R, bool KS, int WAVES, int SIDE>
 struct TileLoader {
     static constexpr int BYTES = R * GK * 2;
     static constexpr int PW = BYTES / 1024 / WAVES;               // copies per wave and stage
@@ -30,12 +31,13 @@ struct TileLoader {
     static_assert(PW % 2 == 0, "the places of two rows of k repeat every second copy");
     const unsigned char* main;                                    // of this wave's first copy of stage 0
     const unsigned char* tail;
-    long long step, ld;                                           // bytes
+    long long step, ld, part;                                     // bytes
     int last;                                                     // the stage that is read from `tail`, or -1
     unsigned voff[NV];
 
     __device__ __forceinline__ void init(const GemmOperand& o, long long i0, long long n_i, int wave, int lane) {
         ld = o.ld * 2;
+        part = o.part * 2;
         last = o.tail != nullptr ? o.tail_stage : -1;
         if constexpr (KS) {
             const int per = R / 8, slot = lane & (per - 1);
@@ -68,7 +70,12 @@ struct TileLoader {
         else lds_dma16_s(st, voff[T], lds + T * 1024);
     }
     __device__ __forceinline__ const unsigned char* stage(int s) const {
-        const unsigned char* p = KS && s == last ? tail : main + s * step;
+        const unsigned char* p;
+        if constexpr (SIDE >= 0) {
+            // pairs (1, 3), (2, 2), (3, 1), (1, 2), (2, 1), (0, 0): parts as a table of four bits each
+            const int block = s / PAIRS, pair = s - block * PAIRS;
+            p = main + block * step + ((SIDE == 0 ? 0x021321u : 0x012123u) >> (4 * pair) & 15u) * part;
+        } else p = KS && s == last ? tail : main + s * step;
         // (uniform, and said so: the copies take it in scalar registers)
         const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)(size_t)p), hi = __builtin_amdgcn_readfirstlane((unsigned)((size_t)p >> 32));
         size_t u = ((size_t)hi << 32) | lo;
@@ -182,14 +189,16 @@ struct ColumnBias {
 // both, all copies in the fourth step: 8192^3 1250 to 1280 TFLOP/s, now 1335; without any copies 1470 to 1510.  The rest of the loss is the prologue and
 // the epilogue, which nothing hides: K = 1024 940 TFLOP/s.)  A wave has priority while it sends MFMAs (K = 1024: 874 without).
 // init: what the sums of the columns start from.
-template <class TS, bool AKS, bool BKS, class INIT>
+// F32: a product of parts.  The matrix instruction's accumulation rounds towards minus infinity, alike for all results: 5e-11 of a result's size per unit of
+// depth, which sums over many of them would show.  So every 1024 of depth the sum changes its sign, and B enters with the other one.
+template <class TS, bool AKS, bool BKS, bool F32, class INIT>
 __device__ __forceinline__ void gemm_tile(f32x16 (&acc)[TS::MT][TS::NT], const GemmOperand& ga, const GemmOperand& gb, long long m0, long long n0,
                                           long long M, long long N, int s0, int s1, unsigned char* smem, const INIT& init) {
     constexpr int MT = TS::MT, NT = TS::NT;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int wm = wave / TS::WN, wn = wave % TS::WN;
-    typedef TileLoader<TS::BM, AKS, TS::WAVES> LA;
-    typedef TileLoader<TS::BN, BKS, TS::WAVES> LB;
+    typedef TileLoader<TS::BM, AKS, TS::WAVES, F32 ? 0 : -1> LA;
+    typedef TileLoader<TS::BN, BKS, TS::WAVES, F32 ? 1 : -1> LB;
     LA la;
     LB lb;
     la.init(ga, m0, M, wave, lane);
@@ -261,21 +270,45 @@ __device__ __forceinline__ void gemm_tile(f32x16 (&acc)[TS::MT][TS::NT], const G
             __builtin_amdgcn_sched_barrier(0);
         });
     };
+    unsigned sign = 0;                                            // of B's entries, twice per register
+    auto turn_signs = [&](int s) {
+        if constexpr (F32) {
+            const unsigned now = (s / PAIRS) & (1024 / GK) ? 0x80008000u : 0u;
+            if (now != sign) {
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) acc[i][j] = -acc[i][j];
+                sign = now;
+            }
+        }
+    };
+    auto signed_b = [&](int set) {
+        if constexpr (F32) {
+#pragma unroll
+            for (int j = 0; j < NT; ++j) fb[set][j] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, fb[set][j]) ^ sign);
+        }
+    };
     unsigned a0 = 0, a1 = TS::OPER, a2 = 2 * TS::OPER, b0 = 0;    // A's buffers of this stage, the next, the one after; B's of this stage
     for (int s = s0; s < s1; ++s) {
         // (past the end: the last stage again, into buffers nobody reads any more)
         const int ahead = s + 2 < s1 ? s + 2 : last;
         const unsigned char *pa = smem + a0, *pb = smem + TS::B_AT + b0;
+        turn_signs(s);
         __builtin_amdgcn_s_waitcnt(WAIT_LGKM0);
+        signed_b(0);
         __builtin_amdgcn_sched_barrier(0);
         multiply(std::integral_constant<int, 0>{}, pa, pb, ahead, a2);
         __builtin_amdgcn_s_waitcnt(WAIT_LGKM0);
+        signed_b(1);
         __builtin_amdgcn_sched_barrier(0);
         multiply(std::integral_constant<int, 1>{}, pa, pb, ahead, a2);
         __builtin_amdgcn_s_waitcnt(WAIT_LGKM0);
+        signed_b(0);
         __builtin_amdgcn_sched_barrier(0);
         multiply(std::integral_constant<int, 2>{}, pa, pb, 0, 0u);
         __builtin_amdgcn_s_waitcnt(WAIT_LGKM0);
+        signed_b(1);
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LA::PW) : "memory");       // the next stage has landed; A's after that may be in flight
         __syncthreads();
         __builtin_amdgcn_sched_barrier(0);
@@ -286,6 +319,13 @@ __device__ __forceinline__ void gemm_tile(f32x16 (&acc)[TS::MT][TS::NT], const G
         a2 = t;
         b0 ^= TS::OPER;
     }
+    if constexpr (F32)
+        if (sign != 0) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = -acc[i][j];
+        }
     __builtin_amdgcn_s_waitcnt(WAIT_LGKM0);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");              // no copy may land after this: the epilogue uses LDS
     __syncthreads();

@@ -243,11 +243,6 @@ hipError_t launch_gemm_f32_masked(int a_kslow, int b_kslow, const float* A, long
                                   const float* B, long long ldb, const RowMask& mb, float* C, long long ldc,
                                   const float* bias, int atomic, long long M, long long N, long long K, int splits,
                                   hipStream_t stream);
-// C without bias and masks; the sum over k in `splits` parts (as many as gemm_f32_split_count says: parts are multiples of the K-step), part z stored at
-// C + z * split_stride.
-int gemm_f32_split_count(long long K, int splits);
-hipError_t launch_gemm_f32_split(int a_kslow, int b_kslow, const float* A, long long lda, const float* B, long long ldb, float* C, long long ldc,
-                                 long long M, long long N, long long K, int splits, long long split_stride, hipStream_t stream);
 // out[c] += sum_r x[r,c]   (x fp32 [rows,cols])
 hipError_t launch_col_sum(const float* x, long long rows, int cols, float* out, hipStream_t stream);
 

@@ -478,12 +478,11 @@ struct OperandF32 {
 // 32 x 32, six MFMAs of depth 16 each per K-step; two LDS buffers, one barrier per K-step, global loads two K-steps ahead of their MFMAs in registers.
 // Two workgroups per compute unit (72 KiB of LDS and 256 registers each; three of 128 x 128): one's splitting stands beside the other's MFMAs.
 // grid (M/128, N/TN, splits); a split covers k_per_split (a multiple of 16) of K.  atomic != 0: the tile
-// is added to C with float atomics (split over K, or C accumulates over calls); else split z is stored at C + z * split_stride.
+// is added to C with float atomics (split over K, or C accumulates over calls).
 template <int TN, class OpA, class OpB>
 __global__ __launch_bounds__(256, TN == 256 ? 2 : 3) void k_gemm_f32(OpA A, OpB B, float* __restrict__ C, long long ldc,
                                                      const float* __restrict__ bias, int atomic, long long M,
-                                                     long long N, long long K, long long k_per_split,
-                                                     long long split_stride) {
+                                                     long long N, long long K, long long k_per_split) {
     constexpr int NT = TN / 64;                       // MFMA tiles of a wave along N
     constexpr unsigned A_BYTES = FT / 32 * 3072, BUF = A_BYTES + TN / 32 * 3072;
     __shared__ __align__(16) unsigned char smem[2 * BUF];
@@ -493,7 +492,6 @@ __global__ __launch_bounds__(256, TN == 256 ? 2 : 3) void k_gemm_f32(OpA A, OpB 
     const long long ks = (long long)blockIdx.z * k_per_split;
     const long long ke = ks + k_per_split < K ? ks + k_per_split : K;
     if (ks >= ke) return;
-    C += blockIdx.z * split_stride;
     f32x16 acc[2][NT];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -656,7 +654,6 @@ struct GemmF32 {
     int atomic;
     long long M, N, K;
     int splits;
-    long long split_stride;
 };
 
 template <bool AK, bool BK, bool EDGE, int TN>
@@ -668,7 +665,7 @@ hipError_t launch_gemm_f32_t(const GemmF32& g, hipStream_t stream) {
     const OperandF32<AK, EDGE, FT> a{g.A, g.lda, g.M, g.K, g.ma};
     const OperandF32<BK, EDGE, TN> b{g.B, g.ldb, g.N, g.K, g.mb};
     k_gemm_f32<TN><<<dim3((unsigned)gm, (unsigned)gn, (unsigned)nz), dim3(256), 0, stream>>>(a, b, g.C, g.ldc, g.bias, g.atomic, g.M, g.N,
-                                                                                        g.K, per, g.split_stride);
+                                                                                        g.K, per);
     return hipGetLastError();
 }
 
@@ -702,7 +699,7 @@ hipError_t launch_gemm_f32(const GemmF32& g, hipStream_t stream) {
     // 16-byte pieces along each operand's contiguous index
     const bool fits = g.lda % 4 == 0 && g.ldb % 4 == 0 && (AK ? g.M : g.K) % 4 == 0 && (BK ? g.N : g.K) % 4 == 0 &&
                       (uintptr_t)g.A % 16 == 0 && (uintptr_t)g.B % 16 == 0;
-    if (!fits || g.splits < 1 || (g.splits > 1 && !g.atomic && g.split_stride == 0)) return hipErrorInvalidValue;
+    if (!fits || g.splits < 1 || (g.splits > 1 && !g.atomic)) return hipErrorInvalidValue;
     const bool wide = wide_tiles_pay(g.M, g.N, g.splits);
     const bool edge = g.ma.len != nullptr || g.mb.len != nullptr || g.M % FT != 0 || g.N % (wide ? 256 : 128) != 0 || g.K % FK != 0;
     if (wide) return edge ? launch_gemm_f32_t<AK, BK, true, 256>(g, stream) : launch_gemm_f32_t<AK, BK, false, 256>(g, stream);
@@ -938,27 +935,15 @@ bool gemm_f32_edge_fits(const void* A, long long lda, const void* B, long long l
            (uintptr_t)A % 16 == 0 && (uintptr_t)B % 16 == 0;
 }
 
-static hipError_t launch_gemm_f32_any(int a_kslow, int b_kslow, const GemmF32& g, hipStream_t stream) {
-    if (!a_kslow && b_kslow) return launch_gemm_f32<false, true>(g, stream);
-    if (!a_kslow && !b_kslow) return launch_gemm_f32<false, false>(g, stream);
-    if (a_kslow && b_kslow) return launch_gemm_f32<true, true>(g, stream);
-    return hipErrorInvalidValue;
-}
-
 hipError_t launch_gemm_f32_masked(int a_kslow, int b_kslow, const float* A, long long lda, const RowMask& ma,
                                   const float* B, long long ldb, const RowMask& mb, float* C, long long ldc,
                                   const float* bias, int atomic, long long M, long long N, long long K, int splits,
                                   hipStream_t stream) {
-    return launch_gemm_f32_any(a_kslow, b_kslow, GemmF32{A, lda, ma, B, ldb, mb, C, ldc, bias, atomic, M, N, K, splits, 0}, stream);
-}
-int gemm_f32_split_count(long long K, int splits) {
-    const long long per = ((K + splits - 1) / splits + FK - 1) / FK * FK;
-    return (int)std::max(1LL, (K + per - 1) / per);
-}
-hipError_t launch_gemm_f32_split(int a_kslow, int b_kslow, const float* A, long long lda, const float* B, long long ldb, float* C, long long ldc,
-                                 long long M, long long N, long long K, int splits, long long split_stride, hipStream_t stream) {
-    const RowMask none{nullptr, 1, 0};
-    return launch_gemm_f32_any(a_kslow, b_kslow, GemmF32{A, lda, none, B, ldb, none, C, ldc, nullptr, 0, M, N, K, splits, split_stride}, stream);
+    const GemmF32 g{A, lda, ma, B, ldb, mb, C, ldc, bias, atomic, M, N, K, splits};
+    if (!a_kslow && b_kslow) return launch_gemm_f32<false, true>(g, stream);
+    if (!a_kslow && !b_kslow) return launch_gemm_f32<false, false>(g, stream);
+    if (a_kslow && b_kslow) return launch_gemm_f32<true, true>(g, stream);
+    return hipErrorInvalidValue;
 }
 
 namespace {
@@ -968,7 +953,7 @@ hipError_t joint_gemm_f32(const float* A, long long lda, const float* B, long lo
                           const float* bias, int atomic, long long M, long long N, long long K, int splits,
                           hipStream_t stream) {
     const RowMask none{nullptr, 1, 0};
-    return launch_gemm_f32<AK, BK>(GemmF32{A, lda, none, B, ldb, none, C, ldc, bias, atomic, M, N, K, splits, 0}, stream);
+    return launch_gemm_f32<AK, BK>(GemmF32{A, lda, none, B, ldb, none, C, ldc, bias, atomic, M, N, K, splits}, stream);
 }
 }  // namespace
 

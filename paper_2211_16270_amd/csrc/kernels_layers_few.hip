@@ -23,16 +23,17 @@ __device__ __forceinline__ bf16x8 raw8(const bf16_t* p, int live) {
     return __builtin_bit_cast(bf16x8, v);
 }
 
+template <class STORE>
 struct FewLinear {
     LinearEpilogue e;
     __device__ __forceinline__ void first() const { pass_rng(e); }
     // columns n .. n + 7 (granule g of the workgroup's 32) of row m
     __device__ __forceinline__ void operator()(int m, int n, int, float (&v)[8]) const {
         float b[8];
-        LinearStore::bias(e, n, b);
+        STORE::bias(e, n, b);
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] += b[k];
-        LinearStore::store(e, m, n, v, LinearStore::fetch(e, m, n));
+        STORE::store(e, m, n, v, STORE::fetch(e, m, n));
     }
 };
 // Statistics of the 32 columns of a row (four neighbouring lanes hold them), as k_ce_scores leaves them for its tiles
@@ -65,6 +66,39 @@ struct FewCe {
         if (e.kept != nullptr) store8((_Float16*)e.kept + (size_t)m * e.pitch + n, 8, v);
     }
 };
+
+// The eight waves' sums -> the epilogue, or this split's slot
+template <int MT, class E>
+__device__ __forceinline__ void few_finish(const FewJob& j, const E& e, const f32x4 (&acc)[MT][2], unsigned char* smem, float* __restrict__ slots, int block,
+                                           int n0) {
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    __syncthreads();
+    // register r of lane l: column 4 (l / 16) + r of its 16, row l % 16
+    float* part = reinterpret_cast<float*>(smem);
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+            *reinterpret_cast<f32x4*>(part + ((wave * MT + i) * 16 + (lane & 15)) * FC + c * 16 + 4 * (lane >> 4)) = acc[i][c];
+    __syncthreads();
+    if (tid < MT * 64) {
+        const int m = tid >> 2, g = tid & 3;
+        f32x4 p = f32x4{0}, q = f32x4{0};
+#pragma unroll
+        for (int k = 0; k < FW; ++k) {
+            const float* s = part + ((size_t)k * MT * 16 + m) * FC + g * 8;
+            p += *reinterpret_cast<const f32x4*>(s);
+            q += *reinterpret_cast<const f32x4*>(s + 4);
+        }
+        float v[8] = {p[0], p[1], p[2], p[3], q[0], q[1], q[2], q[3]};
+        if (m >= j.M) return;
+        if (slots == nullptr) e(m, n0 + g * 8, block, v);
+        else {
+            const int Np = (j.N + 7) / 8 * 8;
+            if (n0 + g * 8 < Np) store8(slots + ((size_t)blockIdx.y * j.M + m) * Np + n0 + g * 8, 8, v);
+        }
+    }
+}
 
 // rows x 32 columns of x W per workgroup, MT blocks of 16 rows.  A wave brings its steps (32 of k) of W through registers into LDS of its own, where the
 // transposing read makes MFMA fragments of them; x comes as fragments from memory.  The eight waves' sums meet in LDS.  Neighbouring column blocks share
@@ -148,35 +182,73 @@ __global__ __launch_bounds__(64 * FW) void k_few_rows(FewJob j, E e, int blocks,
                 fetch(s, 32 * (t + FW * (q + FD)));
             }
         });
-    __syncthreads();
-    // register r of lane l: column 4 (l / 16) + r of its 16, row l % 16
-    float* part = reinterpret_cast<float*>(smem);
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-            *reinterpret_cast<f32x4*>(part + ((wave * MT + i) * 16 + (lane & 15)) * FC + c * 16 + 4 * (lane >> 4)) = acc[i][c];
-    __syncthreads();
-    if (tid < MT * 64) {
-        const int m = tid >> 2, g = tid & 3;
-        f32x4 p = f32x4{0}, q = f32x4{0};
-#pragma unroll
-        for (int k = 0; k < FW; ++k) {
-            const float* s = part + ((size_t)k * MT * 16 + m) * FC + g * 8;
-            p += *reinterpret_cast<const f32x4*>(s);
-            q += *reinterpret_cast<const f32x4*>(s + 4);
-        }
-        float v[8] = {p[0], p[1], p[2], p[3], q[0], q[1], q[2], q[3]};
-        if (m >= j.M) return;
-        if (slots == nullptr) e(m, n0 + g * 8, block, v);
-        else {
-            const int Np = (N + 7) / 8 * 8;
-            if (n0 + g * 8 < Np) store8(slots + ((size_t)blockIdx.y * j.M + m) * Np + n0 + g * 8, 8, v);
-        }
-    }
+    few_finish<MT>(j, e, acc, smem, slots, block, n0);
 }
 
-template <class E>
+// The same in fp32 on the fp32 matrix instruction (16 x 16 x 4), which takes its operands as they lie: a wave's step of 32 along k is eight of them, the
+// i-th with k = 8 g + i in the lanes of group g = l / 16, so that a lane's eight values of x are one piece.
+template <int MT, bool WHOLE, class E>
+__global__ __launch_bounds__(64 * FW) void k_few_rows_f32(FewJob j, E e, int blocks, float* __restrict__ slots, int per_split) {
+    __shared__ __align__(16) unsigned char smem[FW * MT * 16 * FC * 4];
+    const int per = (blocks + 7) >> 3, block = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    if ((int)(blockIdx.x >> 3) >= per || block >= blocks) return;
+    if (block == 0 && slots == nullptr) e.first();
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, n0 = block * FC, g = lane >> 4, l16 = lane & 15;
+    const int K = j.K, N = j.N;
+    const float* W = (const float*)j.W;
+    const float* x[MT];
+    bool row_ok[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int row = 16 * i + l16;
+        row_ok[i] = row < j.M;
+        x[i] = (const float*)j.x + (size_t)(row_ok[i] ? row : 0) * K;
+    }
+    f32x4 acc[MT][2];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) acc[i][0] = acc[i][1] = f32x4{0};
+    constexpr int D = MT == 4 ? 1 : 2;                            // steps in flight
+    float w[D][2][8], a[D][MT][8];
+    auto fetch = [&](auto slot_tag, int k0) {
+        constexpr int s = decltype(slot_tag)::value;
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int k = k0 + 8 * g + i, n = n0 + 16 * c + l16;
+                const bool ok = k < K && (WHOLE || n < N);
+                const float v = W[ok ? (size_t)k * N + n : 0];
+                w[s][c][i] = ok ? v : 0.0f;
+            }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const int k = k0 + 8 * g;
+            load8(x[i] + (k < K ? k : 0), WHOLE ? 8 : row_ok[i] ? (K - k < 0 ? 0 : K - k) : 0, a[s][i]);
+        }
+    };
+    auto step = [&](auto slot_tag) {
+        constexpr int s = decltype(slot_tag)::value;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) acc[m][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[s][c][i], a[s][m][i], acc[m][c], 0, 0, 0);
+    };
+    const int all = (K + 31) / 32, first = blockIdx.y * per_split, steps = first + per_split < all ? first + per_split : all;
+    static_for<0, D>([&](auto s) { fetch(s, 32 * (first + wave + FW * decltype(s)::value)); });
+    for (int t = first + wave; t < steps; t += FW * D)
+        static_for<0, D>([&](auto s) {
+            constexpr int q = decltype(s)::value;
+            if (t + FW * q < steps) {
+                step(s);
+                fetch(s, 32 * (t + FW * (q + D)));
+            }
+        });
+    few_finish<MT>(j, e, acc, smem, slots, block, n0);
+}
+
+template <bool F32, class E>
 hipError_t launch_few(const FewJob& j, const E& e, int splits, float* slots, hipStream_t stream) {
     if (j.M <= 0 || j.M > FEW_ROWS) return j.M <= 0 ? hipSuccess : hipErrorInvalidValue;
     const int blocks = (j.N + FC - 1) / FC, per = ((j.K + 31) / 32 + splits - 1) / splits;
@@ -184,7 +256,10 @@ hipError_t launch_few(const FewJob& j, const E& e, int splits, float* slots, hip
     const bool whole = j.K % 32 == 0 && j.N % FC == 0;
     auto go = [&](auto mt) {
         constexpr int MT = decltype(mt)::value;
-        if (whole) k_few_rows<MT, true, E><<<grid, dim3(64 * FW), 0, stream>>>(j, e, blocks, slots, per);
+        if constexpr (F32) {
+            if (whole) k_few_rows_f32<MT, true, E><<<grid, dim3(64 * FW), 0, stream>>>(j, e, blocks, slots, per);
+            else k_few_rows_f32<MT, false, E><<<grid, dim3(64 * FW), 0, stream>>>(j, e, blocks, slots, per);
+        } else if (whole) k_few_rows<MT, true, E><<<grid, dim3(64 * FW), 0, stream>>>(j, e, blocks, slots, per);
         else k_few_rows<MT, false, E><<<grid, dim3(64 * FW), 0, stream>>>(j, e, blocks, slots, per);
         return hipGetLastError();
     };
@@ -201,9 +276,12 @@ int few_splits(long long M, int K, int N) {
     return (steps + per - 1) / per;
 }
 hipError_t launch_few_linear(const FewJob& j, int splits, float* slots, const LinearEpilogue& e, hipStream_t stream) {
-    const hipError_t err = launch_few(j, FewLinear{e}, splits, splits > 1 ? slots : nullptr, stream);
-    return err != hipSuccess || splits <= 1 ? err : launch_linear_reduce(j.M, j.N, splits, slots, e, stream);
+    const hipError_t err = j.f32 ? launch_few<true>(j, FewLinear<LinearStore32>{e}, splits, splits > 1 ? slots : nullptr, stream)
+                                 : launch_few<false>(j, FewLinear<LinearStore>{e}, splits, splits > 1 ? slots : nullptr, stream);
+    return err != hipSuccess || splits <= 1 ? err : launch_linear_reduce(j.f32, j.M, j.N, splits, slots, e, stream);
 }
-hipError_t launch_few_ce(const FewJob& j, const CeEpilogue& e, hipStream_t stream) { return launch_few(j, FewCe{e}, 1, nullptr, stream); }
+hipError_t launch_few_ce(const FewJob& j, const CeEpilogue& e, hipStream_t stream) {
+    return j.f32 ? launch_few<true>(j, FewCe{e}, 1, nullptr, stream) : launch_few<false>(j, FewCe{e}, 1, nullptr, stream);
+}
 
 }  // namespace rnnt

@@ -21,14 +21,14 @@ __device__ __forceinline__ JobExtent job_extent(const GemmJob& g) {
         n = n < 0 ? 0 : n;
         if (g.limit == GEMM_ROWS_M) x.M = n < x.M ? n : x.M;
         else {
-            const long long s = (n + GK - 1) / GK;
+            const long long s = (n + GK - 1) / GK * g.per_block;
             x.stages = s < x.stages ? (int)s : x.stages;
         }
     }
     return x;
 }
 
-template <class TS, bool AKS, bool BKS, class E>
+template <class TS, bool AKS, bool BKS, bool F32, class E>
 __device__ __forceinline__ void gemm_workgroup(const GemmJob& g, const E& e, int L, int mt, int nt, int splits, int per_split, unsigned char* smem) {
     TilePlace t;
     if (!place_tile(L, mt, nt, splits, t)) return;
@@ -37,9 +37,11 @@ __device__ __forceinline__ void gemm_workgroup(const GemmJob& g, const E& e, int
     if (m0 >= x.M) return;
     const int s0 = t.split * per_split, s1 = s0 + per_split < x.stages ? s0 + per_split : x.stages;
     f32x16 acc[TS::MT][TS::NT];
-    constexpr bool LINEAR = std::is_same_v<E, LinearEpilogue>;
-    if constexpr (LINEAR) gemm_tile<TS, AKS, BKS>(acc, g.A, g.B, m0, n0, g.a_rows, g.b_rows, s0, s1, smem, ColumnBias{e.bias, e.N, 0.0f});
-    else gemm_tile<TS, AKS, BKS>(acc, g.A, g.B, m0, n0, g.a_rows, g.b_rows, s0, s1, smem, NoBias{});
+    constexpr bool LINEAR = std::is_base_of_v<LinearEpilogue, E>;
+    // (scores in fp32 are the only other results with a bias)
+    if constexpr (LINEAR || (F32 && !AKS && BKS))
+        gemm_tile<TS, AKS, BKS, F32>(acc, g.A, g.B, m0, n0, g.a_rows, g.b_rows, s0, s1, smem, ColumnBias{e.bias, e.N, 0.0f});
+    else gemm_tile<TS, AKS, BKS, F32>(acc, g.A, g.B, m0, n0, g.a_rows, g.b_rows, s0, s1, smem, NoBias{});
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int wm = wave / TS::WN, wn = wave % TS::WN, n = (int)n0 + wn * TS::NT * 32 + 8 * (lane & 7);
     unsigned char* area = smem + wave * TURN32_BYTES;
@@ -74,21 +76,21 @@ struct TileJob {
     int mt, nt, splits, per_split;
     __host__ __device__ long long workgroups() const { return ((long long)mt * nt * splits + 7) / 8 * 8; }
 };
-template <class TS, bool AKS, bool BKS, class E>
+template <class TS, bool AKS, bool BKS, bool F32, class E>
 __global__ __launch_bounds__(TS::THREADS, 2) void k_layer_gemm(TileJob<E> j) {
     extern __shared__ __align__(16) unsigned char smem[];
     if (blockIdx.x == 0) pass_rng(j.e);
-    gemm_workgroup<TS, AKS, BKS, E>(j.g, j.e, blockIdx.x, j.mt, j.nt, j.splits, j.per_split, smem);
+    gemm_workgroup<TS, AKS, BKS, F32, E>(j.g, j.e, blockIdx.x, j.mt, j.nt, j.splits, j.per_split, smem);
 }
 // dx and dW; the product whose workgroups take longer goes first (CE, 9288 x 1024 x 32768, dx in 148 workgroups of 512 stages: behind dW's 512 of 146 the
 // two took 1200 us, in front of them xxx).
-template <class TS>
+template <class TS, bool F32>
 __global__ __launch_bounds__(TS::THREADS, 2) void k_layer_grads(TileJob<StoreEpilogue> x, TileJob<StoreEpilogue> w, int wgs_x, int wgs_w) {
     extern __shared__ __align__(16) unsigned char smem[];
     const bool x_first = x.per_split > w.per_split;
     const int L = blockIdx.x, is_x = x_first ? L < wgs_x : L >= wgs_w;
-    if (is_x) gemm_workgroup<TS, false, false, StoreEpilogue>(x.g, x.e, x_first ? L : L - wgs_w, x.mt, x.nt, x.splits, x.per_split, smem);
-    else gemm_workgroup<TS, true, true, StoreEpilogue>(w.g, w.e, x_first ? L - wgs_x : L, w.mt, w.nt, w.splits, w.per_split, smem);
+    if (is_x) gemm_workgroup<TS, false, false, F32, StoreEpilogue>(x.g, x.e, x_first ? L : L - wgs_w, x.mt, x.nt, x.splits, x.per_split, smem);
+    else gemm_workgroup<TS, true, true, F32, StoreEpilogue>(w.g, w.e, x_first ? L - wgs_x : L, w.mt, w.nt, w.splits, w.per_split, smem);
 }
 
 // The sum of the splits' results, in order, and the epilogue.  One thread per eight columns.
@@ -150,7 +152,7 @@ __global__ __launch_bounds__(TS::THREADS, 2) void k_ce_scores(GemmJob g, CeEpilo
     if (m0 >= x.M) return;
     f32x16 acc[TS::MT][TS::NT];
     // (entries beyond the vocabulary are -inf)
-    gemm_tile<TS, false, true>(acc, g.A, g.B, m0, n0, g.a_rows, g.b_rows, 0, g.stages, smem, ColumnBias{e.bias, e.V, RNNT_NEG_INF});
+    gemm_tile<TS, false, true, false>(acc, g.A, g.B, m0, n0, g.a_rows, g.b_rows, 0, g.stages, smem, ColumnBias{e.bias, e.V, RNNT_NEG_INF});
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l32 = lane & 31, hb = lane >> 5;
     const int wm = wave / TS::WN, wn = wave % TS::WN;
     float* top = reinterpret_cast<float*>(smem);                  // [WN][BM]
@@ -249,36 +251,41 @@ TileJob<E> tile_job(const GemmJob& g, const E& e, int splits, int per_split) {
 }
 inline long long padded8(long long n) { return (n + 7) / 8 * 8; }
 StoreEpilogue slot_epilogue(const GemmJob& g, float* slots) {
-    return StoreEpilogue{slots, nullptr, nullptr, padded8(g.N), g.M * padded8(g.N), g.M, (int)padded8(g.N), false};
+    return StoreEpilogue{slots, nullptr, nullptr, padded8(g.N), g.M * padded8(g.N), Bias{}, g.M, (int)padded8(g.N), false};
 }
 template <class E>
 ReduceJob<E> reduce_job(const GemmJob& g, const E& e, const float* slots, int splits) {
     return ReduceJob<E>{g, e, slots, splits, padded8(g.N), g.M * padded8(g.N), g.M * (padded8(g.N) / 8)};
 }
 
-template <class TS, bool AKS, bool BKS, class E>
+template <class TS, bool F32, class E>
 hipError_t gemm_of(const GemmJob& g, const GemmPlan& p, float* slots, const E& e, hipStream_t stream) {
     if (p.splits <= 1) {
         const TileJob<E> j = tile_job<TS>(g, e, 1, g.stages);
-        return launch_tiles<&k_layer_gemm<TS, AKS, BKS, E>, TS>(j.workgroups(), stream, j);
+        return launch_tiles<&k_layer_gemm<TS, false, true, F32, E>, TS>(j.workgroups(), stream, j);
     }
     const TileJob<StoreEpilogue> j = tile_job<TS>(g, slot_epilogue(g, slots), p.splits, p.per_split);
-    hipError_t err = launch_tiles<&k_layer_gemm<TS, AKS, BKS, StoreEpilogue>, TS>(j.workgroups(), stream, j);
+    hipError_t err = launch_tiles<&k_layer_gemm<TS, false, true, F32, StoreEpilogue>, TS>(j.workgroups(), stream, j);
     if (err != hipSuccess) return err;
     const ReduceJob<E> r = reduce_job(g, e, slots, p.splits);
     if ((r.total + 255) / 256 > 0x7fffffffLL) return hipErrorInvalidValue;
     k_layer_reduce<E><<<dim3(r.workgroups()), dim3(256), 0, stream>>>(r);
     return hipGetLastError();
 }
+template <bool F32, class E>
+hipError_t gemm_of(const GemmJob& g, const GemmPlan& p, float* slots, const E& e, hipStream_t stream) {
+    if (g.M <= 0 || g.N <= 0) return hipSuccess;
+    return p.tile == 256 ? gemm_of<TileShape<256>, F32>(g, p, slots, e, stream) : gemm_of<TileShape<128>, F32>(g, p, slots, e, stream);
+}
 
-template <class TS>
+template <class TS, bool F32>
 hipError_t grad_gemms(const GradGemm& dx, const GradGemm& dw, hipStream_t stream) {
     TileJob<StoreEpilogue> x{}, w{};
     if (dx.g.M > 0) x = tile_job<TS>(dx.g, dx.splits > 1 ? slot_epilogue(dx.g, dx.slots) : dx.e, dx.splits, dx.splits > 1 ? dx.per_split : dx.g.stages);
     if (dw.g.M > 0) w = tile_job<TS>(dw.g, dw.splits > 1 ? slot_epilogue(dw.g, dw.slots) : dw.e, dw.splits, dw.splits > 1 ? dw.per_split : dw.g.stages);
     const long long nx = x.workgroups(), nw = w.workgroups();
     if (nx + nw > 0x7ffffff0LL) return hipErrorInvalidValue;
-    return launch_tiles<&k_layer_grads<TS>, TS>(nx + nw, stream, x, w, (int)nx, (int)nw);
+    return launch_tiles<&k_layer_grads<TS, F32>, TS>(nx + nw, stream, x, w, (int)nx, (int)nw);
 }
 
 }  // namespace
@@ -347,21 +354,31 @@ PairPlan plan_pair(long long Mx, long long Nx, int stages_x, long long Mw, long 
 }
 
 hipError_t launch_linear_gemm(const GemmJob& g, const GemmPlan& p, float* slots, const LinearEpilogue& e, hipStream_t stream) {
-    if (g.M <= 0 || g.N <= 0) return hipSuccess;
-    return p.tile == 256 ? gemm_of<TileShape<256>, false, true, LinearEpilogue>(g, p, slots, e, stream)
-                         : gemm_of<TileShape<128>, false, true, LinearEpilogue>(g, p, slots, e, stream);
+    return gemm_of<false>(g, p, slots, e, stream);
 }
-hipError_t launch_linear_reduce(long long M, int N, int splits, const float* slots, const LinearEpilogue& e, hipStream_t stream) {
+hipError_t launch_linear_gemm(const GemmJob& g, const GemmPlan& p, float* slots, const LinearEpilogue32& e, hipStream_t stream) {
+    return gemm_of<true>(g, p, slots, e, stream);
+}
+hipError_t launch_scores_f32(const GemmJob& g, int tile, const StoreEpilogue& e, hipStream_t stream) {
+    return gemm_of<true>(g, GemmPlan{tile, 1, g.stages}, nullptr, e, stream);
+}
+hipError_t launch_linear_reduce(bool f32, long long M, int N, int splits, const float* slots, const LinearEpilogue& e, hipStream_t stream) {
     GemmJob g{};
     g.M = M;
     g.N = N;
     const ReduceJob<LinearEpilogue> r = reduce_job(g, e, slots, splits);
-    k_layer_reduce<LinearEpilogue><<<dim3(r.workgroups()), dim3(256), 0, stream>>>(r);
+    if (f32) {
+        const ReduceJob<LinearEpilogue32> q = reduce_job(g, LinearEpilogue32{e}, slots, splits);
+        k_layer_reduce<LinearEpilogue32><<<dim3(q.workgroups()), dim3(256), 0, stream>>>(q);
+    } else k_layer_reduce<LinearEpilogue><<<dim3(r.workgroups()), dim3(256), 0, stream>>>(r);
     return hipGetLastError();
 }
-hipError_t launch_grad_gemms(int tile, const GradGemm& dx, const GradGemm& dw, const SumJob& db, hipStream_t stream) {
+hipError_t launch_grad_gemms(bool parts, int tile, const GradGemm& dx, const GradGemm& dw, const SumJob& db, hipStream_t stream) {
     if (dx.g.M > 0 || dw.g.M > 0) {
-        const hipError_t e = tile == 256 ? grad_gemms<TileShape<256>>(dx, dw, stream) : grad_gemms<TileShape<128>>(dx, dw, stream);
+        typedef TileShape<256> L;
+        typedef TileShape<128> S;
+        const hipError_t e = tile == 256 ? (parts ? grad_gemms<L, true>(dx, dw, stream) : grad_gemms<L, false>(dx, dw, stream))
+                                         : (parts ? grad_gemms<S, true>(dx, dw, stream) : grad_gemms<S, false>(dx, dw, stream));
         if (e != hipSuccess) return e;
     }
     ReduceJob<StoreEpilogue> x{}, w{};

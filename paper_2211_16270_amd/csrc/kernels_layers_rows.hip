@@ -11,12 +11,25 @@ namespace {
 inline unsigned blocks_of(long long n, long long per) { return (unsigned)((n + per - 1) / per); }
 inline bool grid_fits(long long n) { return n <= 0x7fffffffLL; }
 
-template <typename T>
-__global__ __launch_bounds__(256) void k_layer_pad(const T* __restrict__ src, long long rows, long long cols, long long r0, T* __restrict__ dst,
-                                                   long long ld_to, long long total) {
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
-        const long long r = i / ld_to, c = i - r * ld_to;
-        dst[i] = r0 + r < rows && c < cols ? src[(r0 + r) * cols + c] : (T)0;
+// One thread per eight values
+__global__ __launch_bounds__(256) void k_layer_pads(PadJobs jobs, unsigned first1, unsigned first2) {
+    const int k = blockIdx.x >= first2 ? 2 : blockIdx.x >= first1 ? 1 : 0;
+    const PadJob& j = jobs.job[k];
+    const unsigned first = k == 2 ? first2 : k == 1 ? first1 : 0, wgs = (k == 0 ? first1 : k == 1 ? first2 : gridDim.x) - first;
+    const long long groups = j.ld_to / 8, total = j.rows_to * groups;
+    for (long long i = (long long)(blockIdx.x - first) * 256 + threadIdx.x; i < total; i += (long long)wgs * 256) {
+        const long long r = i / groups, c = (i - r * groups) * 8;
+        const long long left = j.r0 + r < j.rows ? j.cols - c : 0;
+        const int live = left < 0 ? 0 : left < 8 ? (int)left : 8;
+        const size_t from = (size_t)(j.r0 + r) * j.cols + c, to = (size_t)i * 8;
+        if (j.kind == PAD_16) {
+            *reinterpret_cast<bf16x8*>((bf16_t*)j.dst + to) = take8((const bf16_t*)j.src + (live ? from : 0), live);
+        } else {
+            float v[8];
+            load8((const float*)j.src + (live ? from : 0), live, v);
+            if (j.kind == PAD_PARTS) put_parts8((bf16_t*)j.dst + to, j.rows_to * j.ld_to, v);
+            else store8((float*)j.dst + to, 8, v);
+        }
     }
 }
 
@@ -63,16 +76,13 @@ __global__ __launch_bounds__(256) void k_layer_dz(DzArgs a, int R) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[j] += v[j];
         if (a.dz != nullptr) {
-            T* o = (T*)a.dz + (size_t)m * a.ld + n;               // (ld is a multiple of 64, fp32: of 4)
+            bf16_t* o = (bf16_t*)a.dz + (size_t)m * a.ld + n;     // (ld is a multiple of 64)
             if constexpr (sizeof(T) == 2) {
                 bf16x8 x;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) x[j] = (bf16_t)v[j];
                 *reinterpret_cast<bf16x8*>(o) = x;
-            } else {
-                *reinterpret_cast<f32x4*>(o) = f32x4{v[0], v[1], v[2], v[3]};
-                if (n + 4 < a.ld) *reinterpret_cast<f32x4*>(o + 4) = f32x4{v[4], v[5], v[6], v[7]};
-            }
+            } else put_parts8(o, a.rows_to * a.ld, v);
         }
     }
     if (a.part != nullptr && r0 < a.M) fold_columns(sum, red, a.part + (size_t)rb * a.ld, n0, a.N, tid);
@@ -81,65 +91,6 @@ __global__ __launch_bounds__(256) void k_layer_dz(DzArgs a, int R) {
 __global__ __launch_bounds__(256) void k_layer_sum_parts(SumJob j, int blocks, int R) {
     __shared__ float red[8][32];
     sum_parts(j, blocks, R, blockIdx.x, red);
-}
-
-// The splits' sum, in order
-__device__ __forceinline__ void load8_sum(const float* p, int splits, long long stride, int live, float (&v)[8]) {
-    load8(p, live, v);
-    for (int k = 1; k < splits; ++k) {
-        float x[8];
-        load8(p + k * stride, live, x);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += x[j];
-    }
-}
-
-// z (pitch ld, may be saved or y) + bias -> saved, y; one thread per eight columns
-__global__ __launch_bounds__(256) void k_linear_rows_f32(const float* z, long long ld, int splits, long long stride, Bias bias, const float* __restrict__ residual,
-                                                         float* y, float* saved, long long M, int N, int act, Dropout drop,
-                                                         unsigned long long* rng_used, long long groups, long long total) {
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (rng_used != nullptr && i < 2) rng_used[i] = drop.state[i];
-    if (i >= total) return;
-    const long long m = i / groups;
-    const int n = (int)(i - m * groups) * 8, live = N - n < 8 ? N - n : 8;
-    const size_t at = (size_t)m * N + n;
-    float v[8], b[8];
-    load8_sum(z + (size_t)m * ld + n, splits, stride, live, v);
-    load_bias8(bias, n, N, b);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] += b[j];
-    if (saved != nullptr) store8(saved + at, live, v);
-    act8<false>(act, v);
-    drop8(drop, m, n, v);
-    if (residual != nullptr) {
-        float r[8];
-        load8(residual + at, live, r);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += r[j];
-    }
-    store8(y + at, live, v);
-}
-
-__global__ __launch_bounds__(256) void k_layer_reduce_f32(const float* __restrict__ src, long long ld, int splits, long long stride,
-                                                          const int* __restrict__ row_map, float* __restrict__ dst, int N, bool add, long long groups,
-                                                          long long total) {
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (i >= total) return;
-    const long long m = i / groups;
-    const int n = (int)(i - m * groups) * 8, live = N - n < 8 ? N - n : 8;
-    const long long row = row_map != nullptr ? row_map[m] : m;
-    if (row < 0) return;
-    float v[8];
-    load8_sum(src + (size_t)m * ld + n, splits, stride, live, v);
-    float* to = dst + (size_t)row * N + n;
-    if (add) {
-        float p[8];
-        load8(to, live, p);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += p[j];
-    }
-    store8(to, live, v);
 }
 
 // ---- cross entropy --------------------------------------------------------------------------------------------------
@@ -206,11 +157,11 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_ce_rows(const int* __restrict_
 // SCAN: a workgroup counts the real rows before its own itself (the labels come from the L2), which saves a launch; else k_ce_rows has left `place`.
 constexpr int GATHER_ROWS = 16;
 typedef int i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+// T: bf16, or float, whose rows go to xp as parts of cap rows.
 template <typename T, bool SCAN>
 __global__ __launch_bounds__(256) void k_ce_gather(const T* __restrict__ x, long long R, int D, const int* __restrict__ labels,
                                                    const float* __restrict__ weight, int ignore, long long cap, const int* __restrict__ place, CeRows r,
-                                                   T* __restrict__ xp, long long ld, long long fill_to, float* __restrict__ loss, T* __restrict__ dx,
-                                                   int row_wgs) {
+                                                   bf16_t* __restrict__ xp, long long ld, float* __restrict__ loss, T* __restrict__ dx, int row_wgs) {
     __shared__ int wave_count[4], at_row[GATHER_ROWS];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const long long first = (long long)blockIdx.x * GATHER_ROWS;
@@ -245,10 +196,7 @@ __global__ __launch_bounds__(256) void k_ce_gather(const T* __restrict__ x, long
         }
         __syncthreads();
     } else if (fill) n = *r.count;
-    constexpr int E = 16 / sizeof(T);
-    typedef T piece __attribute__((ext_vector_type(E)));
     if (!fill) {
-        const bool vec = D % E == 0;
 #pragma unroll
         for (int k = 0; k < GATHER_ROWS / 4; ++k) {
             const long long row = first + wave * (GATHER_ROWS / 4) + k;
@@ -258,24 +206,29 @@ __global__ __launch_bounds__(256) void k_ce_gather(const T* __restrict__ x, long
             if (to < 0) {
                 if (lane == 0) loss[row] = 0.0f;
                 if (dx != nullptr)
-                    for (int c = lane; c < D; c += 64) dx[(size_t)row * D + c] = (T)0;
+                    for (int c = lane; c < D; c += 64) dx[(size_t)row * D + c] = (T)0.0f;
                 continue;
             }
-            T* dst = xp + (size_t)to * ld;
-            if (vec) {
-                for (int c = lane * E; c < D; c += 64 * E) *reinterpret_cast<piece*>(dst + c) = *reinterpret_cast<const piece*>(src + c);
-                for (int c = D + lane; c < ld; c += 64) dst[c] = (T)0;
-            } else {
-                for (int c = lane; c < ld; c += 64) dst[c] = c < D ? src[c] : (T)0;
+            bf16_t* dst = xp + (size_t)to * ld;
+            for (int c = lane * 8; c < ld; c += 512) {
+                const int live = D - c < 0 ? 0 : D - c;
+                if constexpr (sizeof(T) == 2) *reinterpret_cast<bf16x8*>(dst + c) = take8(src + (live ? c : 0), live);
+                else {
+                    float v[8];
+                    load8(src + (live ? c : 0), live, v);
+                    put_parts8(dst + c, cap * ld, v);
+                }
             }
         }
         return;
     }
-    // zeros behind the last row, up to fill_to (0: the next multiple of 256)
+    // zeros behind the last row up to the next multiple of 256
     const int wg = blockIdx.x - row_wgs, wgs = gridDim.x - row_wgs;
-    const long long end = fill_to != 0 ? fill_to : (n + 255) / 256 * 256;
+    const long long end = (n + 255) / 256 * 256;
     for (long long at = n + wg * 4 + wave; at < end; at += wgs * 4)
-        for (int c = lane; c < ld; c += 64) xp[(size_t)at * ld + c] = (T)0;
+        for (int c = lane * 8; c < ld; c += 512)
+#pragma unroll
+            for (int q = 0; q < (sizeof(T) == 2 ? 1 : PARTS); ++q) *reinterpret_cast<bf16x8*>(xp + q * cap * ld + (size_t)at * ld + c) = bf16x8{0};
     if constexpr (SCAN) {
         if (wg == 0 && tid == 0) *r.count = (int)n;
         for (long long i = n + wg * 256 + tid; i < cap; i += wgs * 256) {
@@ -388,61 +341,86 @@ __global__ __launch_bounds__(256) void k_ce_grad(CeChunk c, void* __restrict__ k
     if (part != nullptr) fold_columns(sum, red, part + (size_t)rb * pitch, n0, c.V, tid);
 }
 
-// fp32: a workgroup per row of scores: maximum and sum of the exponentials in one pass, the gradient in a second one
-__global__ __launch_bounds__(256) void k_ce_rows_f32(CeRows r, long long row0, float* __restrict__ scores, long long ld, int V,
-                                                     Bias b, float* __restrict__ loss, bool grads) {
-    __shared__ float2 part[4];
-    const long long i = blockIdx.x;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, at = r.index[row0 + i];
-    float* h = scores + (size_t)i * ld;
-    f32x4* h4 = reinterpret_cast<f32x4*>(h);
-    if (at < 0) {
-        if (grads)
-            for (int v = tid; v < ld / 4; v += 256) h4[v] = f32x4{0};
+// fp32: a workgroup per row of scores: maximum, sum of the exponentials, then the gradient as parts (the row stays in the caches)
+__global__ __launch_bounds__(256) void k_ce_rows_f32(CeRows r, long long row0, const float* __restrict__ scores, long long ld, int V,
+                                                     float* __restrict__ loss, bf16_t* __restrict__ grad, long long part) {
+    __shared__ float2 red[4];
+    const long long i = blockIdx.x, count = (long long)*r.count - row0;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    bf16_t* g = grad + (size_t)i * ld;
+    if (i >= count) {
+        if (grad != nullptr && i < (count + 63) / 64 * 64)
+            for (int v = tid * 8; v < ld; v += 2048)
+#pragma unroll
+                for (int q = 0; q < PARTS; ++q) *reinterpret_cast<bf16x8*>(g + q * part + v) = bf16x8{0};
         return;
     }
-    const int y = r.label[row0 + i];
+    const float* h = scores + (size_t)i * ld;
+    const int at = r.index[row0 + i], y = r.label[row0 + i];
     const bool known = (unsigned)y < (unsigned)V;
-    auto score = [&](int v) { return h[v] + b.at(v); };
-    const float hy = known ? score(y) : 0.0f;
+    const float hy = known ? h[y] : 0.0f;
+    auto each = [&](auto&& f) {                                    // (ld, and with it every row, is a multiple of 64 floats)
+#pragma unroll 2
+        for (int v = tid * 8; v < V; v += 2048) {
+            float x[8];
+            load8(h + v, 8, x);
+            if (v + 8 > V)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] = v + k < V ? x[k] : RNNT_NEG_INF;
+            f(v, x);
+        }
+    };
     float m = RNNT_NEG_INF, s = 0.0f;
-    for (int v = tid; v < V; v += 256) m = fmaxf(m, score(v));
+    each([&](int, const float (&x)[8]) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) m = fmaxf(m, x[k]);
+    });
     m = wave_max(m);
-    if (lane == 0) part[wave].x = m;
+    if (lane == 0) red[wave].x = m;
     __syncthreads();
-    const float M = fmaxf(fmaxf(part[0].x, part[1].x), fmaxf(part[2].x, part[3].x)), c = M == RNNT_NEG_INF ? 0.0f : M;
-    for (int v = tid; v < V; v += 256) s += expf(score(v) - c);
+    const float M = fmaxf(fmaxf(red[0].x, red[1].x), fmaxf(red[2].x, red[3].x)), c = M == RNNT_NEG_INF ? 0.0f : M;
+    each([&](int, const float (&x)[8]) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s += expf(x[k] - c);
+    });
     s = wave_sum(s);
-    if (lane == 0) part[wave].y = s;
+    if (lane == 0) red[wave].y = s;
     __syncthreads();
-    const float S = (part[0].y + part[1].y) + (part[2].y + part[3].y);
+    const float S = (red[0].y + red[1].y) + (red[2].y + red[3].y);
     if (tid == 0) loss[at] = S == 0.0f || !known ? -RNNT_NEG_INF : (c - hy) + logf(S);
-    if (!grads) return;
+    if (grad == nullptr) return;
     const float w = r.weight[row0 + i], f = S == 0.0f ? 0.0f : w / S;
-    for (int v = tid; v < ld; v += 256) {
-        float d = v < V && S != 0.0f ? expf(score(v) - c) * f : 0.0f;
-        if (v == y && known) d -= w;
-        h[v] = d;
-    }
+    each([&](int v, float (&x)[8]) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            x[k] = S == 0.0f ? 0.0f : expf(x[k] - c) * f;
+            if (v + k == y) x[k] -= w;
+        }
+        put_parts8(g + v, part, x);
+    });
+    for (int v = (V + 7) / 8 * 8 + tid * 8; v < ld; v += 2048)
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q) *reinterpret_cast<bf16x8*>(g + q * part + v) = bf16x8{0};
 }
 
-__global__ __launch_bounds__(256) void k_layer_col_sums_f32(const float* __restrict__ x, long long rows, long long ld, int N, float* __restrict__ part,
-                                                            int R) {
+__global__ __launch_bounds__(256) void k_layer_col_sums_f32(const bf16_t* __restrict__ x, long long rows, long long ld, int N, const int* __restrict__ count,
+                                                            long long row0, float* __restrict__ part, int R) {
     __shared__ __align__(16) float red[8][256];
     const int nb = (N + 255) / 256, rb = blockIdx.x / nb;
     const int tid = threadIdx.x, n0 = (blockIdx.x - rb * nb) * 256, n = n0 + (tid & 31) * 8;
-    const int live = ld - n < 8 ? (int)(ld - n) : 8;
-    const long long r0 = (long long)rb * R;
+    const long long r0 = (long long)rb * R, live = (long long)*count - row0;
+    if (r0 >= live) return;
     float sum[8] = {};
     if (n < ld)
 #pragma unroll 4
         for (int i = 0; i < R / 8; ++i) {
             const long long m = r0 + i * 8 + (tid >> 5);
-            if (m >= rows) break;
-            float v[8];
-            load8(x + (size_t)m * ld + n, live, v);
+            if (m >= live) break;
+            const bf16_t* p = x + (size_t)m * ld + n;
+            const bf16x8 h = *reinterpret_cast<const bf16x8*>(p), q = *reinterpret_cast<const bf16x8*>(p + 2 * rows * ld),
+                         l = *reinterpret_cast<const bf16x8*>(p + 3 * rows * ld);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum[j] += v[j];
+            for (int j = 0; j < 8; ++j) sum[j] += (float)h[j] + ((float)q[j] + (float)l[j]);
         }
     fold_columns(sum, red, part + (size_t)rb * ld, n0, N, tid);
 }
@@ -509,14 +487,12 @@ hipError_t launch_scale(const float* factor, void* const (&p)[3], const long lon
     return hipGetLastError();
 }
 
-hipError_t launch_pad(const void* src, int size, long long rows, long long cols, long long r0, void* dst, long long rows_to, long long ld_to,
-                      hipStream_t stream) {
-    const long long total = rows_to * ld_to;
-    if (total <= 0) return hipSuccess;
-    const unsigned grid = (unsigned)std::min<long long>((total + 255) / 256, 16384);
-    if (size == 2)
-        k_layer_pad<unsigned short><<<dim3(grid), dim3(256), 0, stream>>>((const unsigned short*)src, rows, cols, r0, (unsigned short*)dst, ld_to, total);
-    else k_layer_pad<unsigned><<<dim3(grid), dim3(256), 0, stream>>>((const unsigned*)src, rows, cols, r0, (unsigned*)dst, ld_to, total);
+hipError_t launch_pads(const PadJobs& j, hipStream_t stream) {
+    unsigned wgs[3] = {};
+    for (int k = 0; k < j.n; ++k) wgs[k] = (unsigned)std::min<long long>((j.job[k].rows_to * (j.job[k].ld_to / 8) + 255) / 256, 8192);
+    const unsigned total = wgs[0] + wgs[1] + wgs[2];
+    if (total == 0) return hipSuccess;
+    k_layer_pads<<<dim3(total), dim3(256), 0, stream>>>(j, wgs[0], wgs[0] + wgs[1]);
     return hipGetLastError();
 }
 
@@ -536,47 +512,29 @@ hipError_t launch_sum_parts(const SumJob& j, hipStream_t stream) {
     return hipGetLastError();
 }
 
-hipError_t launch_linear_rows_f32(const float* z, long long ld, int splits, long long stride, const Bias& bias, const float* residual, float* y,
-                                  float* saved, long long M, int N, int act, const Dropout& drop, unsigned long long* rng_used, hipStream_t stream) {
-    const long long groups = (N + 7) / 8, total = M * groups;
-    if (total <= 0) return hipSuccess;
-    if (!grid_fits((total + 255) / 256)) return hipErrorInvalidValue;
-    k_linear_rows_f32<<<dim3(blocks_of(total, 256)), dim3(256), 0, stream>>>(z, ld, splits, stride, bias, residual, y, saved, M, N, act, drop,
-                                                                             rng_used, groups, total);
-    return hipGetLastError();
-}
-hipError_t launch_reduce_f32(const float* src, long long ld, int splits, long long stride, const int* row_map, float* dst, long long rows, int N, bool add,
-                             hipStream_t stream) {
-    const long long groups = (N + 7) / 8, total = rows * groups;
-    if (total <= 0) return hipSuccess;
-    if (!grid_fits((total + 255) / 256)) return hipErrorInvalidValue;
-    k_layer_reduce_f32<<<dim3(blocks_of(total, 256)), dim3(256), 0, stream>>>(src, ld, splits, stride, row_map, dst, N, add, groups, total);
-    return hipGetLastError();
-}
-
 namespace {
 template <typename T>
 hipError_t gather(const void* x, long long R, int D, const int* labels, const float* weight, int ignore, long long cap, int* place, const CeRows& r, void* xp,
-                  long long ld, long long fill_to, float* loss, void* dx, hipStream_t stream) {
-    const unsigned row_wgs = blocks_of(R, GATHER_ROWS), fill_wgs = (unsigned)std::min<long long>(256, blocks_of(std::max(256LL, fill_to), 16));
-    const dim3 grid(row_wgs + fill_wgs);
+                  long long ld, float* loss, void* dx, hipStream_t stream) {
+    const unsigned row_wgs = blocks_of(R, GATHER_ROWS);
+    const dim3 grid(row_wgs + 16);
     if (R <= GATHER_SCAN) {
-        k_ce_gather<T, true><<<grid, dim3(256), 0, stream>>>((const T*)x, R, D, labels, weight, ignore, cap, nullptr, r, (T*)xp, ld, fill_to, loss, (T*)dx,
+        k_ce_gather<T, true><<<grid, dim3(256), 0, stream>>>((const T*)x, R, D, labels, weight, ignore, cap, nullptr, r, (bf16_t*)xp, ld, loss, (T*)dx,
                                                              (int)row_wgs);
     } else {
         k_ce_rows<<<dim3(blocks_of(R, SCAN_ROWS)), dim3(SCAN_THREADS), 0, stream>>>(labels, weight, R, ignore, cap, place, r);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        k_ce_gather<T, false><<<grid, dim3(256), 0, stream>>>((const T*)x, R, D, labels, weight, ignore, cap, place, r, (T*)xp, ld, fill_to, loss, (T*)dx,
+        k_ce_gather<T, false><<<grid, dim3(256), 0, stream>>>((const T*)x, R, D, labels, weight, ignore, cap, place, r, (bf16_t*)xp, ld, loss, (T*)dx,
                                                               (int)row_wgs);
     }
     return hipGetLastError();
 }
 }  // namespace
-hipError_t launch_ce_gather(const void* x, int size, long long R, int D, const int* labels, const float* weight, int ignore, long long cap, int* place,
-                            const CeRows& r, void* xp, long long ld, long long fill_to, float* loss, void* dx, hipStream_t stream) {
-    return size == 2 ? gather<unsigned short>(x, R, D, labels, weight, ignore, cap, place, r, xp, ld, fill_to, loss, dx, stream)
-                     : gather<unsigned>(x, R, D, labels, weight, ignore, cap, place, r, xp, ld, fill_to, loss, dx, stream);
+hipError_t launch_ce_gather(const void* x, bool f32, long long R, int D, const int* labels, const float* weight, int ignore, long long cap, int* place,
+                            const CeRows& r, void* xp, long long ld, float* loss, void* dx, hipStream_t stream) {
+    return f32 ? gather<float>(x, R, D, labels, weight, ignore, cap, place, r, xp, ld, loss, dx, stream)
+               : gather<bf16_t>(x, R, D, labels, weight, ignore, cap, place, r, xp, ld, loss, dx, stream);
 }
 hipError_t launch_ce_finish(const CeChunk& c, hipStream_t stream) {
     k_ce_finish<<<dim3(blocks_of(c.rows, 4)), dim3(256), 0, stream>>>(c);
@@ -590,17 +548,17 @@ hipError_t launch_ce_grad(const CeChunk& c, void* kept, long long pitch, float* 
     else k_ce_grad<false><<<dim3((unsigned)n), dim3(256), 0, stream>>>(c, kept, pitch, part, R);
     return hipGetLastError();
 }
-hipError_t launch_ce_rows_f32(const CeRows& r, long long row0, long long rows, float* scores, long long ld, int V, const Bias& b, float* loss,
-                              bool grads, hipStream_t stream) {
-    k_ce_rows_f32<<<dim3((unsigned)rows), dim3(256), 0, stream>>>(r, row0, scores, ld, V, b, loss, grads);
+hipError_t launch_ce_rows_f32(const CeRows& r, long long row0, long long rows, const float* scores, long long ld, int V, float* loss, void* grad,
+                              hipStream_t stream) {
+    k_ce_rows_f32<<<dim3((unsigned)rows), dim3(256), 0, stream>>>(r, row0, scores, ld, V, loss, (bf16_t*)grad, rows * ld);
     return hipGetLastError();
 }
-hipError_t launch_col_sums_f32(const float* x, long long rows, long long ld, int N, float* part, hipStream_t stream) {
+hipError_t launch_col_sums_f32(const void* x, long long rows, long long ld, int N, const int* count, long long row0, float* part, hipStream_t stream) {
     const int R = sum_rows(rows, N);
     const long long n = (long long)blocks_of(N, 256) * sum_blocks(rows, N);
     if (!grid_fits(n)) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)n);
-    k_layer_col_sums_f32<<<grid, dim3(256), 0, stream>>>(x, rows, ld, N, part, R);
+    k_layer_col_sums_f32<<<dim3((unsigned)n), dim3(256), 0, stream>>>((const bf16_t*)x, rows, ld, N, count, row0, part, R);
     return hipGetLastError();
 }
+
 }  // namespace rnnt

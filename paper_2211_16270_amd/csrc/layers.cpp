@@ -47,19 +47,6 @@ struct Carver {
 };
 bool workspace_ok(const void* ws, size_t have, size_t need) { return need == 0 || (ws != nullptr && (uintptr_t)ws % 256 == 0 && have >= need); }
 
-// fp32 products: two workgroups of 128 x 128 per compute unit, so a sum over k is cut into as many parts as make 512 of them, each at least 64 deep
-// (2048 x 512 out of a depth of 4096: 180 us in one part, 64 workgroups); at most 16384 deep, so that its rounding does not grow with it.  Parts are
-// stored apart and added in order.
-int splits_f32(long long M, long long N, long long K) {
-    const double tiles = (double)((M + 127) / 128) * (double)((N + 127) / 128);
-    long long s = tiles >= 512.0 ? 1 : (long long)(512.0 / std::max(1.0, tiles));
-    s = std::min(s, std::max(1LL, K / 64));
-    while (s > 1 && (double)s * (double)M * (double)N * 4.0 > (double)SLOT_CAP) --s;
-    s = std::max(s, (K + 16383) / 16384);
-    return K > 0 ? gemm_f32_split_count(K, (int)s) : 1;
-}
-size_t slots_f32(int splits, long long rows, long long ld) { return (size_t)splits * (size_t)rows * (size_t)ld * 4; }
-
 // ---- linear -------------------------------------------------------------------------------------------------------------
 rnnt_status check_linear(const rnnt_linear_desc* d, bool backward) {
     if (!d) return RNNT_ERR_NULL;
@@ -79,187 +66,138 @@ Dropout make_dropout(const rnnt_linear_desc& d, const uint64_t* rng) {
     return Dropout{(const unsigned long long*)rng, cut, (float)(65536.0 / (65536.0 - cut))};
 }
 
-// Where the operands of the products lie.  bf16: rows of 64 elements' multiples along a contiguous contraction, 8 along the other index, else a padded copy.
+// Where the operands of the products lie.  bf16: as the caller has them where rows are multiples of 64 elements along a contiguous contraction and of 8 along the
+// other index, else in a padded copy.  fp32: in a padded copy as parts (layers.h).
 struct LinearPlan {
-    bool bf16, backward;
-    bool few;                             // forward pass of at most FEW_ROWS rows: one launch on the arrays as they are
+    bool f32, few;                        // few: forward pass of at most FEW_ROWS rows, one launch on the arrays as they are
     int few_splits;
     bool copy_x, copy_w, own_dz;
-    long long Kp, Np, Mp;                 // pitches of the copies and of dz; rows of dz
+    long long Kp, Np, Mp;                 // multiples of 64
     size_t off_x, off_w, off_dz, off_xt, off_dyt, off_part, off_slots, off_slots_w, bytes;
     GemmPlan y;
     PairPlan grads;
-    int y32, dx32, dw32;                  // fp32: parts of the three sums
 };
 LinearPlan plan_linear(const rnnt_linear_desc& d, bool backward) {
     LinearPlan p{};
-    p.bf16 = d.dtype == RNNT_BF16;
-    p.backward = backward;
+    p.f32 = d.dtype == RNNT_F32;
     const long long M = d.M, K = d.K, N = d.N;
-    const size_t e = p.bf16 ? 2 : 4;
-    Carver c;
+    const int per = p.f32 ? PAIRS : 1;    // stages per 64 of depth
+    const size_t e = p.f32 ? PARTS * 2 : 2;
     const bool plain = d.activation == ACT_NONE && dropout_cut(d.dropout) == 0;
-    if (p.bf16) {
-        p.Kp = up(K, 64);
-        p.Np = up(N, 64);
-        p.Mp = up(M, 64);
-        if (!backward && M <= FEW_ROWS) {
-            p.few = true;
-            p.few_splits = few_splits(M, d.K, d.N);
-            p.off_slots = c.take(p.few_splits > 1 ? (size_t)p.few_splits * M * up(N, 8) * 4 : 0);
-        } else if (!backward) {
-            p.copy_x = K % 64 != 0;
-            p.copy_w = K % 64 != 0 || N % 8 != 0;
-            p.y = plan_gemm(M, N, (int)(p.Kp / 64), SLOT_CAP);
-            p.off_x = c.take(p.copy_x ? (size_t)M * p.Kp * 2 : 0);
-            p.off_w = c.take(p.copy_w ? (size_t)p.Kp * p.Np * 2 : 0);
-            p.off_slots = c.take(gemm_slot_bytes(p.y, M, N));
-        } else {
-            p.own_dz = !plain || N % 64 != 0;
-            p.copy_x = K % 8 != 0;
-            p.copy_w = N % 64 != 0;
-            p.grads = plan_pair(M, K, (int)(p.Np / 64), K, N, (int)(p.Mp / 64), SLOT_CAP);
-            p.off_dz = c.take(p.own_dz ? (size_t)p.Mp * p.Np * 2 : 0);
-            p.off_x = c.take(p.copy_x ? (size_t)p.Mp * p.Kp * 2 : 0);
-            p.off_w = c.take(p.copy_w ? (size_t)K * p.Np * 2 : 0);
-            p.off_xt = c.take(!p.copy_x && M % 64 != 0 ? (size_t)64 * K * 2 : 0);
-            p.off_dyt = c.take(!p.own_dz && M % 64 != 0 ? (size_t)64 * N * 2 : 0);
-            p.off_part = c.take((size_t)sum_capacity(M, N) * p.Np * 4);
-            p.off_slots = c.take(gemm_slot_bytes(p.grads.dx, M, K));
-            p.off_slots_w = c.take(gemm_slot_bytes(p.grads.dw, K, N));
-        }
-    } else {
-        p.Kp = up(K, 4);
-        p.Np = up(N, 4);
-        p.copy_x = K % 4 != 0;
-        p.copy_w = K % 4 != 0 || N % 4 != 0;
+    Carver c;
+    p.Kp = up(K, 64);
+    p.Np = up(N, 64);
+    p.Mp = up(M, 64);
+    if (!backward && M <= FEW_ROWS) {
+        p.few = true;
+        p.few_splits = few_splits(M, d.K, d.N);
+        p.off_slots = c.take(p.few_splits > 1 ? (size_t)p.few_splits * M * up(N, 8) * 4 : 0);
+    } else if (!backward) {
+        p.copy_x = p.f32 || K % 64 != 0;
+        p.copy_w = p.f32 || K % 64 != 0 || N % 8 != 0;
+        p.y = plan_gemm(M, N, (int)(p.Kp / 64) * per, SLOT_CAP);
         p.off_x = c.take(p.copy_x ? (size_t)M * p.Kp * e : 0);
         p.off_w = c.take(p.copy_w ? (size_t)p.Kp * p.Np * e : 0);
-        if (!backward) {
-            p.y32 = splits_f32(M, p.Np, p.Kp);
-            p.off_slots = c.take(p.y32 > 1 || N % 4 != 0 ? slots_f32(p.y32, M, p.Np) : 0);
-        } else {
-            p.own_dz = !plain || N % 4 != 0;
-            p.off_dz = c.take(p.own_dz ? (size_t)M * p.Np * e : 0);
-            p.off_part = c.take((size_t)sum_capacity(M, N) * p.Np * 4);
-            p.dx32 = splits_f32(M, K, p.Np);
-            p.dw32 = splits_f32(p.Kp, p.Np, M);
-            p.off_slots = c.take(std::max(p.dx32 > 1 ? slots_f32(p.dx32, M, K) : 0, slots_f32(p.dw32, p.Kp, p.Np)));
-        }
+        p.off_slots = c.take(gemm_slot_bytes(p.y, M, N));
+    } else {
+        p.own_dz = p.f32 || !plain || N % 64 != 0;
+        p.copy_x = p.f32 || K % 8 != 0;
+        p.copy_w = p.f32 || N % 64 != 0;
+        p.grads = plan_pair(M, K, (int)(p.Np / 64) * per, K, N, (int)(p.Mp / 64) * per, SLOT_CAP);
+        p.off_dz = c.take(p.own_dz ? (size_t)p.Mp * p.Np * e : 0);
+        p.off_x = c.take(p.copy_x ? (size_t)p.Mp * p.Kp * e : 0);
+        p.off_w = c.take(p.copy_w ? (size_t)K * p.Np * e : 0);
+        p.off_xt = c.take(!p.copy_x && M % 64 != 0 ? (size_t)64 * K * 2 : 0);
+        p.off_dyt = c.take(!p.own_dz && M % 64 != 0 ? (size_t)64 * N * 2 : 0);
+        p.off_part = c.take((size_t)sum_capacity(M, N) * p.Np * 4);
+        p.off_slots = c.take(gemm_slot_bytes(p.grads.dx, M, K));
+        p.off_slots_w = c.take(gemm_slot_bytes(p.grads.dw, K, N));
     }
     p.bytes = c.bytes;
     return p;
 }
 
-rnnt_status linear_fwd_bf16(const rnnt_linear_desc& d, const LinearPlan& p, const void* x, const void* W, const Bias& b, const void* residual,
-                            const Dropout& drop, uint64_t* rng_used, void* y, void* saved, unsigned char* ws, hipStream_t stream) {
+// An operand: the caller's array of pitch ld, or a copy of `rows` rows of pitch ld_copy
+GemmOperand operand(bool copied, bool f32, const void* own, long long ld, const void* copy, long long rows, long long ld_copy) {
+    return copied ? GemmOperand{copy, ld_copy, f32 ? rows * ld_copy : 0, nullptr, -1} : GemmOperand{own, ld, 0, nullptr, -1};
+}
+
+rnnt_status linear_fwd(const rnnt_linear_desc& d, const LinearPlan& p, const void* x, const void* W, const Bias& b, const void* residual,
+                       const Dropout& drop, uint64_t* rng_used, void* y, void* saved, unsigned char* ws, hipStream_t stream) {
     const long long M = d.M, K = d.K, N = d.N;
     const LinearEpilogue e{b, residual, y, saved, d.activation, drop, (unsigned long long*)rng_used, M, d.N};
+    float* slots = (float*)(ws + p.off_slots);
     if (p.few) {
-        LAYER_HIP(launch_few_linear(FewJob{x, W, (int)M, d.K, d.N}, p.few_splits, (float*)(ws + p.off_slots), e, stream));
+        LAYER_HIP(launch_few_linear(FewJob{x, W, (int)M, d.K, d.N, p.f32}, p.few_splits, slots, e, stream));
         return RNNT_OK;
     }
-    if (p.copy_x) LAYER_HIP(launch_pad(x, 2, M, K, 0, ws + p.off_x, M, p.Kp, stream));
-    if (p.copy_w) LAYER_HIP(launch_pad(W, 2, K, N, 0, ws + p.off_w, p.Kp, p.Np, stream));
+    const int kind = p.f32 ? PAD_PARTS : PAD_16;
+    PadJobs pads{};
+    if (p.copy_x) pads.add(kind, x, M, K, 0, ws + p.off_x, M, p.Kp);
+    if (p.copy_w) pads.add(kind, W, K, N, 0, ws + p.off_w, p.Kp, p.Np);
+    LAYER_HIP(launch_pads(pads, stream));
     GemmJob g{};
-    g.A = GemmOperand{p.copy_x ? ws + p.off_x : x, p.copy_x ? p.Kp : K, nullptr, -1};
-    g.B = GemmOperand{p.copy_w ? ws + p.off_w : W, p.copy_w ? p.Np : N, nullptr, -1};
+    g.A = operand(p.copy_x, p.f32, x, K, ws + p.off_x, M, p.Kp);
+    g.B = operand(p.copy_w, p.f32, W, N, ws + p.off_w, p.Kp, p.Np);
     g.M = g.a_rows = M;
     g.N = N;
     g.b_rows = p.copy_w ? p.Np : N;
-    g.stages = (int)(p.Kp / 64);
-    LAYER_HIP(launch_linear_gemm(g, p.y, (float*)(ws + p.off_slots), e, stream));
+    g.per_block = p.f32 ? PAIRS : 1;
+    g.stages = (int)(p.Kp / 64) * g.per_block;
+    LAYER_HIP(p.f32 ? launch_linear_gemm(g, p.y, slots, LinearEpilogue32{e}, stream) : launch_linear_gemm(g, p.y, slots, e, stream));
     return RNNT_OK;
 }
 
-rnnt_status linear_bwd_bf16(const rnnt_linear_desc& d, const LinearPlan& p, const void* x, const void* W, const void* saved, const Dropout& drop,
-                            const void* dy, void* dx, void* dW, void* db, unsigned char* ws, hipStream_t stream) {
-    const long long M = d.M, K = d.K, N = d.N;
+rnnt_status linear_bwd(const rnnt_linear_desc& d, const LinearPlan& p, const void* x, const void* W, const void* saved, const Dropout& drop, const void* dy,
+                       void* dx, void* dW, void* db, unsigned char* ws, hipStream_t stream) {
+    const long long M = d.M, K = d.K, N = d.N, whole = M / 64 * 64;
+    const bool ragged = M % 64 != 0;
     float* part = (float*)(ws + p.off_part);
+    if (M == 0) dx = nullptr;
     if (M > 0 && (db || (p.own_dz && (dx || dW)))) {
         const DzArgs a{dy, d.activation == ACT_NONE ? nullptr : saved, p.own_dz && (dx || dW) ? ws + p.off_dz : nullptr, db ? part : nullptr, M,
                        p.own_dz ? p.Mp : M, d.N, p.Np, d.activation, drop};
-        LAYER_HIP(launch_dz(true, a, stream));
+        LAYER_HIP(launch_dz(!p.f32, a, stream));
     }
-    const void* dz = p.own_dz ? ws + p.off_dz : dy;
-    const long long ld_dz = p.own_dz ? p.Np : N;
+    const int kind = p.f32 ? PAD_PARTS : PAD_16;
+    PadJobs pads{};
+    if (dx && p.copy_w) pads.add(kind, W, K, N, 0, ws + p.off_w, K, p.Np);
+    if (dW && p.copy_x) pads.add(kind, x, M, K, 0, ws + p.off_x, p.Mp, p.Kp);
+    else if (dW && ragged) pads.add(PAD_16, x, M, K, whole, ws + p.off_xt, 64, K);
+    if (dW && !p.own_dz && ragged) pads.add(PAD_16, dy, M, N, whole, ws + p.off_dyt, 64, N);
+    LAYER_HIP(launch_pads(pads, stream));
     GradGemm gx{}, gw{};
-    if (dx && M > 0) {
-        if (p.copy_w) LAYER_HIP(launch_pad(W, 2, K, N, 0, ws + p.off_w, K, p.Np, stream));
-        gx.g.A = GemmOperand{dz, ld_dz, nullptr, -1};
-        gx.g.B = GemmOperand{p.copy_w ? ws + p.off_w : W, p.copy_w ? p.Np : N, nullptr, -1};
+    gx.g.per_block = gw.g.per_block = p.f32 ? PAIRS : 1;
+    const GemmOperand dz = operand(p.own_dz, p.f32, dy, N, ws + p.off_dz, p.Mp, p.Np);
+    if (dx) {
+        gx.g.A = dz;
+        gx.g.B = operand(p.copy_w, p.f32, W, N, ws + p.off_w, K, p.Np);
         gx.g.M = gx.g.a_rows = M;
         gx.g.N = gx.g.b_rows = K;
-        gx.g.stages = (int)(p.Np / 64);
+        gx.g.stages = (int)(p.Np / 64) * gx.g.per_block;
         gx.splits = p.grads.dx.splits;
         gx.per_split = p.grads.dx.per_split;
         gx.slots = (float*)(ws + p.off_slots);
-        gx.e = StoreEpilogue{dx, nullptr, nullptr, K, 0, M, d.K, true};
+        gx.e = StoreEpilogue{dx, nullptr, nullptr, K, 0, Bias{}, M, d.K, !p.f32};
     }
     if (dW) {
-        const bool ragged = M % 64 != 0;
-        const long long whole = M / 64 * 64;
-        if (p.copy_x) LAYER_HIP(launch_pad(x, 2, M, K, 0, ws + p.off_x, p.Mp, p.Kp, stream));
-        else if (ragged) LAYER_HIP(launch_pad(x, 2, M, K, whole, ws + p.off_xt, 64, K, stream));
-        if (!p.own_dz && ragged) LAYER_HIP(launch_pad(dy, 2, M, N, whole, ws + p.off_dyt, 64, N, stream));
-        gw.g.A = GemmOperand{p.copy_x ? ws + p.off_x : x, p.copy_x ? p.Kp : K, !p.copy_x && ragged ? ws + p.off_xt : nullptr, (int)(whole / 64)};
-        gw.g.B = GemmOperand{dz, ld_dz, !p.own_dz && ragged ? ws + p.off_dyt : nullptr, (int)(whole / 64)};
+        gw.g.A = operand(p.copy_x, p.f32, x, K, ws + p.off_x, p.Mp, p.Kp);
+        gw.g.B = dz;
+        if (ragged && !p.copy_x) gw.g.A.tail = ws + p.off_xt;
+        if (ragged && !p.own_dz) gw.g.B.tail = ws + p.off_dyt;
+        gw.g.A.tail_stage = gw.g.B.tail_stage = (int)(whole / 64);
         gw.g.M = K;
         gw.g.a_rows = p.copy_x ? p.Kp : K;
         gw.g.N = N;
-        gw.g.b_rows = ld_dz;
-        gw.g.stages = (int)(p.Mp / 64);
+        gw.g.b_rows = p.own_dz ? p.Np : N;
+        gw.g.stages = (int)(p.Mp / 64) * gw.g.per_block;
         gw.splits = p.grads.dw.splits;
         gw.per_split = p.grads.dw.per_split;
         gw.slots = (float*)(ws + p.off_slots_w);
-        gw.e = StoreEpilogue{dW, d.accumulate_params ? (const float*)dW : nullptr, nullptr, N, 0, K, d.N, (d.param_grads_bf16 & 1) != 0};
+        gw.e = StoreEpilogue{dW, d.accumulate_params ? (const float*)dW : nullptr, nullptr, N, 0, Bias{}, K, d.N, (d.param_grads_bf16 & 1) != 0};
     }
     const SumJob sum{db ? part : nullptr, M, p.Np, d.N, nullptr, 0, d.accumulate_params ? (const float*)db : nullptr, db, (d.param_grads_bf16 & 2) != 0};
-    LAYER_HIP(launch_grad_gemms(p.grads.tile, gx, gw, sum, stream));
-    return RNNT_OK;
-}
-
-rnnt_status linear_fwd_f32(const rnnt_linear_desc& d, const LinearPlan& p, const float* x, const float* W, const Bias& b, const float* residual,
-                           const Dropout& drop, uint64_t* rng_used, float* y, float* saved, unsigned char* ws, hipStream_t stream) {
-    const long long M = d.M, K = d.K, N = d.N;
-    if (p.copy_x) LAYER_HIP(launch_pad(x, 4, M, K, 0, ws + p.off_x, M, p.Kp, stream));
-    if (p.copy_w) LAYER_HIP(launch_pad(W, 4, K, N, 0, ws + p.off_w, p.Kp, p.Np, stream));
-    float* z = p.y32 > 1 || N % 4 != 0 ? (float*)(ws + p.off_slots) : saved ? saved : y;
-    LAYER_HIP(launch_gemm_f32_split(0, 1, p.copy_x ? (const float*)(ws + p.off_x) : x, p.Kp, p.copy_w ? (const float*)(ws + p.off_w) : W, p.Np, z, p.Np, M,
-                                    p.Np, p.Kp, p.y32, M * p.Np, stream));
-    LAYER_HIP(launch_linear_rows_f32(z, p.Np, p.y32, M * p.Np, b, residual, y, saved, M, d.N, d.activation, drop,
-                                     (unsigned long long*)rng_used, stream));
-    return RNNT_OK;
-}
-
-rnnt_status linear_bwd_f32(const rnnt_linear_desc& d, const LinearPlan& p, const float* x, const float* W, const float* saved, const Dropout& drop,
-                           const float* dy, float* dx, float* dW, float* db, unsigned char* ws, hipStream_t stream) {
-    const long long M = d.M, K = d.K, N = d.N;
-    float* part = (float*)(ws + p.off_part);
-    if (M > 0 && (db || (p.own_dz && (dx || dW)))) {
-        const DzArgs a{dy, d.activation == ACT_NONE ? nullptr : saved, p.own_dz && (dx || dW) ? ws + p.off_dz : nullptr, db ? part : nullptr, M, M, d.N, p.Np,
-                       d.activation, drop};
-        LAYER_HIP(launch_dz(false, a, stream));
-    }
-    if (db)
-        LAYER_HIP(launch_sum_parts(SumJob{part, M, p.Np, d.N, nullptr, 0, d.accumulate_params ? db : nullptr, db, false}, stream));
-    const float* dz = p.own_dz ? (const float*)(ws + p.off_dz) : dy;
-    if (p.copy_w && dx && M > 0) LAYER_HIP(launch_pad(W, 4, K, N, 0, ws + p.off_w, p.Kp, p.Np, stream));
-    float* slots = (float*)(ws + p.off_slots);
-    if (dx && M > 0) {
-        LAYER_HIP(launch_gemm_f32_split(0, 0, dz, p.Np, p.copy_w ? (const float*)(ws + p.off_w) : W, p.Np, p.dx32 > 1 ? slots : dx, K, M, K, p.Np, p.dx32,
-                                        M * K, stream));
-        if (p.dx32 > 1) LAYER_HIP(launch_reduce_f32(slots, K, p.dx32, M * K, nullptr, dx, M, d.K, false, stream));
-    }
-    if (dW && M == 0) {
-        if (!d.accumulate_params) LAYER_HIP(launch_pad(nullptr, 4, 0, 0, 0, dW, K, N, stream));
-    } else if (dW) {
-        if (p.copy_x) LAYER_HIP(launch_pad(x, 4, M, K, 0, ws + p.off_x, M, p.Kp, stream));
-        const bool direct = p.dw32 == 1 && !p.copy_w && !d.accumulate_params;
-        LAYER_HIP(launch_gemm_f32_split(1, 1, p.copy_x ? (const float*)(ws + p.off_x) : x, p.Kp, dz, p.Np, direct ? dW : slots, p.Np, p.Kp, p.Np, M, p.dw32,
-                                        p.Kp * p.Np, stream));
-        if (!direct) LAYER_HIP(launch_reduce_f32(slots, p.Np, p.dw32, p.Kp * p.Np, nullptr, dW, K, d.N, d.accumulate_params != 0, stream));
-    }
+    LAYER_HIP(launch_grad_gemms(p.f32, p.grads.tile, gx, gw, sum, stream));
     return RNNT_OK;
 }
 
@@ -277,36 +215,36 @@ rnnt_status check_ce(const rnnt_ce_desc* d, bool grads) {
 }
 
 struct CePlan {
-    bool bf16, grads, copy_w;
-    bool few;                             // at most FEW_ROWS rows: scores by one launch on W as it is
+    bool f32, grads, copy_w;
+    bool few;                             // at most FEW_ROWS rows (fp32: without gradients): scores by one launch on W as it is
     bool identity;                        // ... and without gradients on x as it is
-    long long cap, chunk, Dp, Vp, pitch;  // rows (a multiple of 256) in all and per chunk; padded widths; elements of a chunk row
+    long long cap, chunk, Dp, Vp, pitch;  // rows (a multiple of 256) in all and per chunk; widths up to 64; elements of a chunk row
     int chunks, tile, tile_log2, tiles_n;
-    size_t off_count, off_index, off_label, off_weight, off_place, off_x, off_w, off_chunk, off_score, off_stats, off_scale, off_part, off_slots, off_slots_w, off_acc,
-        off_dbacc, bytes;
+    size_t off_count, off_index, off_label, off_weight, off_place, off_x, off_w, off_chunk, off_grad, off_score, off_stats, off_scale, off_part, off_slots,
+        off_slots_w, off_acc, off_dbacc, bytes;
     PairPlan pair;
-    int dx32, dw32;                       // fp32: parts of the gradients' sums
 };
 CePlan plan_ce_chunk(const rnnt_ce_desc& d, bool grads, long long chunk) {
     CePlan p{};
-    p.bf16 = d.dtype == RNNT_BF16;
+    p.f32 = d.dtype == RNNT_F32;
     p.grads = grads;
     const long long R = d.R, D = d.D, V = d.V;
+    const int per = p.f32 ? PAIRS : 1;
+    const size_t e = p.f32 ? PARTS * 2 : 2;
     p.cap = std::max(256LL, up(R, 256));
     p.chunk = std::min(chunk, p.cap);
     p.chunks = (int)((p.cap + p.chunk - 1) / p.chunk);
-    const size_t e = p.bf16 ? 2 : 4;
-    p.Dp = up(D, p.bf16 ? 64 : 4);
-    p.Vp = up(V, p.bf16 ? 64 : 4);
-    p.copy_w = p.Dp != D || p.Vp != V;
-    p.few = p.bf16 && R <= FEW_ROWS;
+    p.Dp = up(D, 64);
+    p.Vp = up(V, 64);
+    p.few = R <= FEW_ROWS && !(p.f32 && grads);
     p.identity = p.few && !grads;
+    p.copy_w = !p.identity && (p.f32 || p.Dp != D || p.Vp != V);
+    p.tile = p.few ? FEW_TILE : plan_gemm(p.chunk, V, (int)(p.Dp / 64) * per, 0).tile;
+    p.tile_log2 = p.few ? 5 : p.tile == 256 ? 8 : 7;
+    // (few: the columns of zeros up to Vp have parts of their own)
+    p.tiles_n = (int)(((p.few ? p.Vp : V) + p.tile - 1) / p.tile);
     Carver c;
     if (p.identity) {
-        p.copy_w = false;
-        p.tile = FEW_TILE;
-        p.tile_log2 = 5;
-        p.tiles_n = (int)((V + FEW_TILE - 1) / FEW_TILE);
         p.off_score = c.take((size_t)FEW_ROWS * 4);
         p.off_stats = c.take((size_t)R * p.tiles_n * 8);
         p.bytes = c.bytes;
@@ -319,36 +257,26 @@ CePlan plan_ce_chunk(const rnnt_ce_desc& d, bool grads, long long chunk) {
     p.off_place = c.take(R > GATHER_SCAN ? (size_t)p.cap * 4 : 0);
     p.off_x = c.take((size_t)p.cap * p.Dp * e);
     p.off_w = c.take(p.copy_w ? (size_t)p.Dp * p.Vp * e : 0);
-    if (p.bf16) {
+    if (p.f32) {
+        p.pitch = p.Vp;
+        p.off_chunk = c.take((size_t)p.chunk * p.pitch * 4);
+        p.off_grad = c.take(grads ? (size_t)p.chunk * p.pitch * e : 0);
+    } else {
         // (a row is 128 bytes longer than whole tiles: rows of a power-of-two length would all start in the same memory channel)
         p.pitch = up(V, 256) + 64;
-        p.tile = p.few ? FEW_TILE : plan_gemm(p.chunk, V, (int)(p.Dp / 64), 0).tile;
-        p.tile_log2 = p.few ? 5 : p.tile == 256 ? 8 : 7;
-        // (few: the columns of zeros up to Vp have parts of their own)
-        p.tiles_n = (int)(((p.few ? p.Vp : V) + p.tile - 1) / p.tile);
         p.off_score = c.take((size_t)p.chunk * 4);
         p.off_stats = c.take((size_t)p.chunk * p.tiles_n * 8);
         p.off_scale = c.take((size_t)p.chunk * 8);
-        if (grads) {
-            p.off_chunk = c.take((size_t)p.chunk * p.pitch * 2);
-            p.off_part = c.take((size_t)sum_capacity(p.chunk, V) * p.pitch * 4);
-            p.pair = plan_pair(p.chunk, D, (int)(p.Vp / 64), D, V, (int)(p.chunk / 64), SLOT_CAP);
-            p.off_slots = c.take(gemm_slot_bytes(p.pair.dx, p.chunk, D));
-            p.off_slots_w = c.take(gemm_slot_bytes(p.pair.dw, D, V));
-            // the weight gradient's sum over the chunks, where its output is bfloat16
-            p.off_acc = c.take(p.chunks > 1 && (d.param_grads_bf16 & 1) ? (size_t)D * V * 4 : 0);
-            p.off_dbacc = c.take(p.chunks > 1 ? (size_t)V * 4 : 0);
-        }
-    } else {
-        p.pitch = p.Vp;
-        p.off_chunk = c.take((size_t)p.chunk * p.pitch * 4);
-        if (grads) {
-            p.off_part = c.take((size_t)sum_capacity(p.chunk, V) * p.pitch * 4);
-            p.dx32 = splits_f32(p.chunk, D, p.Vp);
-            p.dw32 = splits_f32(p.Dp, p.Vp, p.chunk);
-            p.off_slots = c.take(std::max(slots_f32(p.dx32, p.chunk, D), slots_f32(p.dw32, p.Dp, p.Vp)));
-            p.off_dbacc = c.take(p.chunks > 1 ? (size_t)V * 4 : 0);
-        }
+        p.off_chunk = p.off_grad = c.take(grads ? (size_t)p.chunk * p.pitch * 2 : 0);
+    }
+    if (grads) {
+        p.off_part = c.take((size_t)sum_capacity(p.chunk, V) * p.pitch * 4);
+        p.pair = plan_pair(p.chunk, D, (int)(p.Vp / 64) * per, D, V, (int)(p.chunk / 64) * per, SLOT_CAP);
+        p.off_slots = c.take(gemm_slot_bytes(p.pair.dx, p.chunk, D));
+        p.off_slots_w = c.take(gemm_slot_bytes(p.pair.dw, D, V));
+        // the weight gradient's sum over the chunks, where its output is bfloat16
+        p.off_acc = c.take(p.chunks > 1 && (d.param_grads_bf16 & 1) ? (size_t)D * V * 4 : 0);
+        p.off_dbacc = c.take(p.chunks > 1 ? (size_t)V * 4 : 0);
     }
     p.bytes = c.bytes;
     return p;
@@ -356,7 +284,7 @@ CePlan plan_ce_chunk(const rnnt_ce_desc& d, bool grads, long long chunk) {
 // The largest chunks whose plan takes at most `budget` bytes (0: whose buffers take at most CE_CHUNK), at least 256 rows
 CePlan plan_ce(const rnnt_ce_desc& d, bool grads, size_t budget) {
     const long long all = std::max(256LL, up(d.R, 256));
-    const size_t row = d.dtype == RNNT_BF16 ? (size_t)(up(d.V, 256) + 64) * 2 : (size_t)up(d.V, 4) * 4;
+    const size_t row = d.dtype == RNNT_BF16 ? (size_t)(up(d.V, 256) + 64) * 2 : (size_t)up(d.V, 64) * (4 + (grads ? PARTS * 2 : 0));
     if (budget == 0) {
         // equal chunks
         const long long most = std::max(256LL, (long long)(CE_CHUNK / row) / 256 * 256), n = (all + most - 1) / most;
@@ -375,114 +303,93 @@ CePlan plan_ce(const rnnt_ce_desc& d, bool grads, size_t budget) {
     return best;
 }
 
-rnnt_status run_ce(const rnnt_ce_desc& d, const CePlan& p, const void* x, const void* W, const void* b_ptr, const int32_t* label, const float* row_weight,
+rnnt_status run_ce(const rnnt_ce_desc& d, const CePlan& p, const void* x, const void* W, const Bias& b, const int32_t* label, const float* row_weight,
                    float* loss, void* dx, void* dW, void* db, unsigned char* ws, hipStream_t stream) {
     const long long D = d.D, V = d.V;
-    const Bias b{b_ptr, d.bias_bf16 != 0};
-    const CeRows rows{(int*)(ws + p.off_count), (int*)(ws + p.off_index), (int*)(ws + p.off_label), (float*)(ws + p.off_weight)};
-    const int size = p.bf16 ? 2 : 4;
+    if (!p.grads && d.R == 0) return RNNT_OK;
     if (p.identity) {
-        if (d.R == 0) return RNNT_OK;
         CeRows own{};
         own.label = const_cast<int*>(label);
         const CeEpilogue e{b, d.V, label, (float*)(ws + p.off_score), (float2*)(ws + p.off_stats), p.tiles_n, nullptr, 0};
-        LAYER_HIP(launch_few_ce(FewJob{x, W, (int)d.R, d.D, d.V}, e, stream));
+        LAYER_HIP(launch_few_ce(FewJob{x, W, (int)d.R, d.D, d.V, p.f32}, e, stream));
         LAYER_HIP(launch_ce_finish(CeChunk{own, 0, d.R, e.label_score, e.stats, p.tiles_n, p.tile_log2, d.V, nullptr, loss, true, d.ignore_label}, stream));
         return RNNT_OK;
     }
-    void* xp = ws + p.off_x;
-    if (d.R > 0) {
-        LAYER_HIP(launch_ce_gather(x, size, d.R, d.D, label, row_weight, d.ignore_label, p.cap, (int*)(ws + p.off_place), rows, xp, p.Dp,
-                                   p.bf16 ? 0 : p.cap, loss, p.grads ? dx : nullptr, stream));
-    } else if (!p.grads) return RNNT_OK;
-    else LAYER_HIP(launch_pad(nullptr, 4, 0, 0, 0, rows.count, 1, 1, stream));       // (no rows: the gradients of an empty sum)
-    if (p.copy_w) LAYER_HIP(launch_pad(W, size, D, V, 0, ws + p.off_w, p.Dp, p.Vp, stream));
-    const void* Wu = p.copy_w ? ws + p.off_w : W;
-    unsigned char* chunk = ws + p.off_chunk;
+    const CeRows rows{(int*)(ws + p.off_count), (int*)(ws + p.off_index), (int*)(ws + p.off_label), (float*)(ws + p.off_weight)};
+    const int kind = p.f32 ? PAD_PARTS : PAD_16;
+    PadJobs pads{};
+    if (d.R > 0)
+        LAYER_HIP(launch_ce_gather(x, p.f32, d.R, d.D, label, row_weight, d.ignore_label, p.cap, (int*)(ws + p.off_place), rows, ws + p.off_x, p.Dp, loss,
+                                   p.grads ? dx : nullptr, stream));
+    else pads.add(PAD_32, nullptr, 0, 0, 0, rows.count, 1, 8);       // (no rows: the gradients of an empty sum; the part behind is 256 bytes away)
+    if (p.copy_w) pads.add(kind, W, D, V, 0, ws + p.off_w, p.Dp, p.Vp);
+    LAYER_HIP(launch_pads(pads, stream));
+    const GemmOperand w = operand(p.copy_w, p.f32, W, V, ws + p.off_w, p.Dp, p.Vp);
+    unsigned char *chunk = ws + p.off_chunk, *grad = ws + p.off_grad;
     float* part = (float*)(ws + p.off_part);
     for (int k = 0; k < p.chunks; ++k) {
         const long long row0 = (long long)k * p.chunk, n = std::min(p.chunk, p.cap - row0);
         const bool first = k == 0, last = k == p.chunks - 1;
-        const unsigned char* xc = (const unsigned char*)xp + (size_t)row0 * p.Dp * size;
-        if (p.bf16) {
-            GemmJob g{};
-            g.A = GemmOperand{xc, p.Dp, nullptr, -1};
-            g.B = GemmOperand{Wu, p.Vp, nullptr, -1};
-            g.M = g.a_rows = n;
-            g.N = V;
-            g.b_rows = p.Vp;
-            g.stages = (int)(p.Dp / 64);
-            g.limit = GEMM_ROWS_M;
-            g.count = rows.count;
-            g.row0 = row0;
+        GemmJob g{};
+        g.A = GemmOperand{ws + p.off_x + (size_t)row0 * p.Dp * 2, p.Dp, p.f32 ? p.cap * p.Dp : 0, nullptr, -1};
+        g.B = w;
+        g.M = g.a_rows = n;
+        g.N = V;
+        g.b_rows = p.Vp;
+        g.per_block = p.f32 ? PAIRS : 1;
+        g.stages = (int)(p.Dp / 64) * g.per_block;
+        g.limit = GEMM_ROWS_M;
+        g.count = rows.count;
+        g.row0 = row0;
+        if (d.R == 0) {
+        } else if (p.f32) {
+            const StoreEpilogue e{chunk, nullptr, nullptr, p.pitch, 0, b, n, d.V, false};
+            LAYER_HIP(launch_scores_f32(g, p.tile, e, stream));
+            LAYER_HIP(launch_ce_rows_f32(rows, row0, n, (const float*)chunk, p.pitch, d.V, loss, p.grads ? grad : nullptr, stream));
+            if (p.grads && db) LAYER_HIP(launch_col_sums_f32(grad, n, p.pitch, d.V, rows.count, row0, part, stream));
+        } else {
             const CeEpilogue e{b, d.V, rows.label + row0, (float*)(ws + p.off_score), (float2*)(ws + p.off_stats), p.tiles_n,
                                p.grads ? chunk : nullptr, p.pitch};
             const CeChunk c{rows, row0, n, e.label_score, e.stats, p.tiles_n, p.tile_log2, d.V, (float2*)(ws + p.off_scale), loss, false, 0};
-            if (d.R > 0) {
-                if (p.few) LAYER_HIP(launch_few_ce(FewJob{xc, Wu, (int)d.R, (int)p.Dp, (int)p.Vp}, e, stream));
-                else LAYER_HIP(launch_ce_gemm(g, p.tile, e, stream));
-                if (!p.grads || !ce_grad_finishes(p.tiles_n)) LAYER_HIP(launch_ce_finish(c, stream));
-            }
-            if (!p.grads) continue;
-            if (d.R > 0) LAYER_HIP(launch_ce_grad(c, chunk, p.pitch, db ? part : nullptr, stream));
-            GradGemm gx{}, gw{};
-            if (d.R > 0) {
-                gx.g = g;
-                gx.g.A = GemmOperand{chunk, p.pitch, nullptr, -1};
-                gx.g.N = gx.g.b_rows = D;
-                gx.g.stages = (int)(p.Vp / 64);
-                gx.splits = p.pair.dx.splits;
-                gx.per_split = p.pair.dx.per_split;
-                gx.slots = (float*)(ws + p.off_slots);
-                gx.e = StoreEpilogue{dx, nullptr, rows.index + row0, D, 0, n, d.D, true};
-            }
-            gw.g.A = GemmOperand{xc, p.Dp, nullptr, -1};
-            gw.g.B = GemmOperand{chunk, p.pitch, nullptr, -1};
-            gw.g.M = D;
-            gw.g.a_rows = p.Dp;
-            gw.g.N = V;
-            gw.g.b_rows = p.Vp;
-            gw.g.stages = (int)(n / 64);
-            gw.g.limit = GEMM_ROWS_K;
-            gw.g.count = rows.count;
-            gw.g.row0 = row0;
-            gw.splits = p.pair.dw.splits;
-            gw.per_split = p.pair.dw.per_split;
-            gw.slots = (float*)(ws + p.off_slots_w);
-            const bool w16 = (d.param_grads_bf16 & 1) != 0, b16 = (d.param_grads_bf16 & 2) != 0;
-            float* acc = w16 ? (float*)(ws + p.off_acc) : (float*)dW;
-            gw.e = StoreEpilogue{last ? dW : acc, !first || d.accumulate_params ? acc : nullptr, nullptr, V, 0, D, d.V, last && w16};
-            float* dba = (float*)(ws + p.off_dbacc);
-            const SumJob sum{db ? part : nullptr, n, p.pitch, d.V, rows.count, row0, first ? (d.accumulate_params ? (const float*)db : nullptr) : dba,
-                             last ? db : (void*)dba, last && b16};
-            LAYER_HIP(launch_grad_gemms(p.pair.tile, gx, gw, sum, stream));
-        } else {
-            float* S = (float*)chunk;
-            if (d.R > 0) {
-                LAYER_HIP(launch_gemm_f32_split(0, 1, (const float*)xc, p.Dp, (const float*)Wu, p.Vp, S, p.pitch, n, p.Vp, p.Dp, 1, 0, stream));
-                LAYER_HIP(launch_ce_rows_f32(rows, row0, n, S, p.pitch, d.V, b, loss, p.grads, stream));
-            }
-            if (!p.grads) continue;
-            if (d.R == 0) {
-                if (!d.accumulate_params) LAYER_HIP(launch_pad(nullptr, 4, 0, 0, 0, dW, D, V, stream));
-            } else {
-                float* slots = (float*)(ws + p.off_slots);
-                const int sx = gemm_f32_split_count(p.Vp, p.dx32), sw = gemm_f32_split_count(n, std::min<long long>(p.dw32, std::max(1LL, n / 64)));
-                LAYER_HIP(launch_gemm_f32_split(0, 0, S, p.pitch, (const float*)Wu, p.Vp, slots, D, n, D, p.Vp, sx, n * D, stream));
-                LAYER_HIP(launch_reduce_f32(slots, D, sx, n * D, rows.index + row0, (float*)dx, n, d.D, false, stream));
-                const bool add = !first || d.accumulate_params, direct = sw == 1 && !p.copy_w && !add;
-                LAYER_HIP(launch_gemm_f32_split(1, 1, (const float*)xc, p.Dp, S, p.pitch, direct ? (float*)dW : slots, p.Vp, p.Dp, p.Vp, n, sw,
-                                                p.Dp * p.Vp, stream));
-                if (!direct) LAYER_HIP(launch_reduce_f32(slots, p.Vp, sw, p.Dp * p.Vp, nullptr, (float*)dW, D, d.V, add, stream));
-                if (db) LAYER_HIP(launch_col_sums_f32(S, n, p.pitch, d.V, part, stream));
-            }
-            if (db) {
-                float* dba = (float*)(ws + p.off_dbacc);
-                LAYER_HIP(launch_sum_parts(SumJob{part, n, p.pitch, d.V, rows.count, row0,
-                                                  first ? (d.accumulate_params ? (const float*)db : nullptr) : dba, last ? db : (void*)dba, false},
-                                           stream));
-            }
+            if (p.few) LAYER_HIP(launch_few_ce(FewJob{g.A.p, w.p, (int)d.R, (int)p.Dp, (int)p.Vp, false}, e, stream));
+            else LAYER_HIP(launch_ce_gemm(g, p.tile, e, stream));
+            if (!p.grads || !ce_grad_finishes(p.tiles_n)) LAYER_HIP(launch_ce_finish(c, stream));
+            if (p.grads) LAYER_HIP(launch_ce_grad(c, chunk, p.pitch, db ? part : nullptr, stream));
         }
+        if (!p.grads) continue;
+        const GemmOperand dh{grad, p.pitch, p.f32 ? n * p.pitch : 0, nullptr, -1};
+        GradGemm gx{}, gw{};
+        gx.g.per_block = gw.g.per_block = g.per_block;
+        if (d.R > 0) {
+            gx.g = g;
+            gx.g.A = dh;
+            gx.g.N = gx.g.b_rows = D;
+            gx.g.stages = (int)(p.Vp / 64) * g.per_block;
+            gx.splits = p.pair.dx.splits;
+            gx.per_split = p.pair.dx.per_split;
+            gx.slots = (float*)(ws + p.off_slots);
+            gx.e = StoreEpilogue{dx, nullptr, rows.index + row0, D, 0, Bias{}, n, d.D, !p.f32};
+        }
+        gw.g.A = g.A;
+        gw.g.B = dh;
+        gw.g.M = D;
+        gw.g.a_rows = p.Dp;
+        gw.g.N = V;
+        gw.g.b_rows = p.Vp;
+        gw.g.stages = (int)(n / 64) * g.per_block;
+        gw.g.limit = GEMM_ROWS_K;
+        gw.g.count = rows.count;
+        gw.g.row0 = row0;
+        gw.splits = p.pair.dw.splits;
+        gw.per_split = p.pair.dw.per_split;
+        gw.slots = (float*)(ws + p.off_slots_w);
+        const bool w16 = (d.param_grads_bf16 & 1) != 0, b16 = (d.param_grads_bf16 & 2) != 0;
+        float* acc = w16 ? (float*)(ws + p.off_acc) : (float*)dW;
+        gw.e = StoreEpilogue{last ? dW : acc, !first || d.accumulate_params ? acc : nullptr, nullptr, V, 0, Bias{}, D, d.V, last && w16};
+        float* dba = (float*)(ws + p.off_dbacc);
+        const SumJob sum{db ? part : nullptr, n, p.pitch, d.V, rows.count, row0, first ? (d.accumulate_params ? (const float*)db : nullptr) : dba,
+                         last ? db : (void*)dba, last && b16};
+        LAYER_HIP(launch_grad_gemms(p.f32, p.pair.tile, gx, gw, sum, stream));
     }
     return RNNT_OK;
 }
@@ -508,9 +415,7 @@ extern "C" rnnt_status rnnt_linear_fwd(const rnnt_linear_desc* desc, const void*
     if (desc->M == 0) return RNNT_OK;
     unsigned char* ws = (unsigned char*)workspace;
     const Bias bias{b, desc->bias_bf16 != 0};
-    if (p.bf16) return linear_fwd_bf16(*desc, p, x, W, bias, residual, drop, rng_used, y, saved, ws, (hipStream_t)hip_stream);
-    return linear_fwd_f32(*desc, p, (const float*)x, (const float*)W, bias, (const float*)residual, drop, rng_used, (float*)y, (float*)saved, ws,
-                          (hipStream_t)hip_stream);
+    return linear_fwd(*desc, p, x, W, bias, residual, drop, rng_used, y, saved, ws, (hipStream_t)hip_stream);
 }
 
 extern "C" rnnt_status rnnt_linear_bwd(const rnnt_linear_desc* desc, const void* x, const void* W, const void* saved, const uint64_t* rng,
@@ -524,9 +429,7 @@ extern "C" rnnt_status rnnt_linear_bwd(const rnnt_linear_desc* desc, const void*
     const LinearPlan p = plan_linear(*desc, true);
     if (!workspace_ok(workspace, workspace_bytes, p.bytes)) return RNNT_ERR_WORKSPACE;
     unsigned char* ws = (unsigned char*)workspace;
-    if (p.bf16) return linear_bwd_bf16(*desc, p, x, W, saved, drop, dy, dx, dW, db, ws, (hipStream_t)hip_stream);
-    return linear_bwd_f32(*desc, p, (const float*)x, (const float*)W, (const float*)saved, drop, (const float*)dy, (float*)dx, (float*)dW, (float*)db, ws,
-                          (hipStream_t)hip_stream);
+    return linear_bwd(*desc, p, x, W, saved, drop, dy, dx, dW, db, ws, (hipStream_t)hip_stream);
 }
 
 extern "C" size_t rnnt_ce_loss_workspace_bytes(const rnnt_ce_desc* desc, int32_t grads, size_t budget_bytes) {
@@ -548,7 +451,7 @@ static rnnt_status ce_loss(const rnnt_ce_desc* desc, bool grads, const void* x, 
         if (workspace_bytes < p.bytes || q.chunk > p.chunk) p = q;
     }
     if (!workspace_ok(workspace, workspace_bytes, p.bytes)) return RNNT_ERR_WORKSPACE;
-    return run_ce(*desc, p, x, W, b, label, row_weight, loss, dx, dW, db, (unsigned char*)workspace, (hipStream_t)hip_stream);
+    return run_ce(*desc, p, x, W, Bias{b, desc->bias_bf16 != 0}, label, row_weight, loss, dx, dW, db, (unsigned char*)workspace, (hipStream_t)hip_stream);
 }
 
 extern "C" rnnt_status rnnt_ce_loss_fwd(const rnnt_ce_desc* desc, const void* x, const void* W, const void* b, const int32_t* label, float* loss,

@@ -29,9 +29,15 @@ struct Bias {
 };
 
 // ---- bf16 matrix products ---------------------------------------------------------------------------------------------
+// fp32 products: an fp32 value is the exact sum of three bf16 values, each the rounded rest of the ones before: x = h + m + l with |m| <= 2^-9 |x|, |l| <= 2^-18
+// |x|.  A matrix lies as four arrays of its shape, `part` elements apart: h, h where x is finite (else 0), m, l (0 where it is not).  A product
+// takes six pairs per 64 of k, the small ones first: h l, m m, l h, h m, m h, h h; what is left out is below 2^-26 of it.  Only the last takes the h that
+// may be infinite or NaN, so that those count as what they are.  (Below 2^-110 a value loses what lies under 2^-134.)
+constexpr int PARTS = 4, PAIRS = 6;
 struct GemmOperand {
     const void* p;
     long long ld;                        // elements
+    long long part;
     const void* tail;                    // k-slow operands whose K is no multiple of 64: the last stage's 64 rows, zeros from K on; else null
     int tail_stage;
 };
@@ -43,7 +49,8 @@ struct GemmJob {
     GemmOperand A, B;
     long long M, N;                      // tiles cover them; operands may be read up to a_rows, b_rows along their other index
     long long a_rows, b_rows;
-    int stages;                          // ceil(K / 64)
+    int per_block;                       // stages per 64 of k: 1, fp32 products: PAIRS
+    int stages;                          // ceil(K / 64) per_block
     int limit;
     const int* count;
     long long row0;
@@ -78,10 +85,13 @@ struct StoreEpilogue {
     const int* row_map;                  // or null
     long long ld;
     long long split_stride;              // elements between the results of two splits
+    Bias bias;
     long long M;
     int N;
     bool bf16;
 };
+// The same in fp32: residual, y, saved float
+struct LinearEpilogue32 : LinearEpilogue {};
 // Scores h = v + bias of a tile row -> their maximum m and S = sum 2^15 e^{h - m} (stats[row * tiles_n + tile]), the label's score, and, where kept is
 // not null, 2^15 e^{h - m} as fp16.
 struct CeEpilogue {
@@ -96,18 +106,22 @@ struct CeEpilogue {
 };
 // k-contiguous A, k-slow B
 hipError_t launch_linear_gemm(const GemmJob& g, const GemmPlan& p, float* slots, const LinearEpilogue& e, hipStream_t stream);
+hipError_t launch_linear_gemm(const GemmJob& g, const GemmPlan& p, float* slots, const LinearEpilogue32& e, hipStream_t stream);
 hipError_t launch_ce_gemm(const GemmJob& g, int tile, const CeEpilogue& e, hipStream_t stream);
+// scores in fp32 (out: float, with the bias)
+hipError_t launch_scores_f32(const GemmJob& g, int tile, const StoreEpilogue& e, hipStream_t stream);
 // The same two for at most FEW_ROWS rows, x [M, K] and W [K, N] dense, of any size and alignment; the statistics are of parts of FEW_TILE columns.
 constexpr int FEW_ROWS = 64, FEW_TILE = 32;
 struct FewJob {
     const void* x;
     const void* W;
     int M, K, N;
+    bool f32;                            // (results of the fp32 matrix instruction)
 };
 int few_splits(long long M, int K, int N);
 hipError_t launch_few_linear(const FewJob& j, int splits, float* slots, const LinearEpilogue& e, hipStream_t stream);
 // the epilogue on the sum of slots [splits][M][N up to 8]
-hipError_t launch_linear_reduce(long long M, int N, int splits, const float* slots, const LinearEpilogue& e, hipStream_t stream);
+hipError_t launch_linear_reduce(bool f32, long long M, int N, int splits, const float* slots, const LinearEpilogue& e, hipStream_t stream);
 hipError_t launch_few_ce(const FewJob& j, const CeEpilogue& e, hipStream_t stream);
 // The two gradients' products, dx (operands k-contiguous) and dW (operands k-slow), in one launch; then, in another, what remains: the sums of their splits
 // and the bias gradient's out of column sums.
@@ -132,12 +146,28 @@ struct SumJob {
     void* out;
     bool bf16;
 };
-hipError_t launch_grad_gemms(int tile, const GradGemm& dx, const GradGemm& dw, const SumJob& db, hipStream_t stream);
+// parts: fp32 products
+hipError_t launch_grad_gemms(bool parts, int tile, const GradGemm& dx, const GradGemm& dw, const SumJob& db, hipStream_t stream);
 
 // ---- passes over memory --------------------------------------------------------------------------------------------
-// dst[rows_to, ld_to] = src[rows, cols] (dense) from row r0 on, zeros elsewhere; element size 2 or 4
-hipError_t launch_pad(const void* src, int size, long long rows, long long cols, long long r0, void* dst, long long rows_to, long long ld_to,
-                      hipStream_t stream);
+// dst[rows_to, ld_to] = src[rows, cols] (dense) from row r0 on, zeros elsewhere, ld_to a multiple of 8: a copy of 16-bit values, of 32-bit ones, or of floats as
+// parts.  Up to three in one launch.
+enum PadKind { PAD_NONE = 0, PAD_16, PAD_32, PAD_PARTS };
+struct PadJob {
+    int kind;
+    const void* src;
+    long long rows, cols, r0;
+    void* dst;
+    long long rows_to, ld_to;
+};
+struct PadJobs {
+    PadJob job[3];
+    int n;
+    void add(int kind, const void* src, long long rows, long long cols, long long r0, void* dst, long long rows_to, long long ld_to) {
+        job[n++] = PadJob{kind, src, rows, cols, r0, dst, rows_to, ld_to};
+    }
+};
+hipError_t launch_pads(const PadJobs& j, hipStream_t stream);
 
 // Rows per workgroup of a pass over [rows, cols] that leaves column sums, and so per row of these partial sums: 128 where there are workgroups of
 // 128 x 256 enough, fewer for a small array (1632 x 640 in fp32, dz: 29.6 us with 128, 39 workgroups).
@@ -153,7 +183,7 @@ inline long long sum_capacity(long long rows, long long cols) {
     return few > many ? (few < most ? few : most) : many;
 }
 // dz = dy act'(z) mask / (1 - p) into dz [rows_to, ld] (zeros beyond [M, N]; null: not stored), column sums of blocks of sum_rows(M, N) rows into part
-// [sum_blocks(M, N), ld] (null: none).  bf16: saved fp16, dz bf16; else both float.
+// [sum_blocks(M, N), ld] (null: none).  bf16: saved fp16, dz bf16; else dy and saved float, dz as parts.
 struct DzArgs {
     const void* dy;
     const void* saved;
@@ -168,14 +198,6 @@ struct DzArgs {
 hipError_t launch_dz(bool bf16, const DzArgs& a, hipStream_t stream);
 // out[n] = prev[n] + sum of the partial sums
 hipError_t launch_sum_parts(const SumJob& j, hipStream_t stream);
-// fp32: z (the sum of `splits` arrays of pitch ld, `stride` apart; one may be saved or y) + bias -> saved (or null), y = residual + dropout(act(z + bias)); all
-// but z dense [M, N]
-hipError_t launch_linear_rows_f32(const float* z, long long ld, int splits, long long stride, const Bias& bias, const float* residual, float* y,
-                                  float* saved, long long M, int N, int act, const Dropout& drop, unsigned long long* rng_used, hipStream_t stream);
-// dst [.., N] (+)= the sum of `splits` arrays of pitch ld, `stride` apart, rows as they are or row i to row_map[i] (those < 0 nowhere)
-hipError_t launch_reduce_f32(const float* src, long long ld, int splits, long long stride, const int* row_map, float* dst, long long rows, int N, bool add,
-                             hipStream_t stream);
-
 // ---- cross entropy ---------------------------------------------------------------------------------------------------
 // Rows whose label is not `ignore`, in order: their number, places, labels, weights.  Arrays of `cap` entries (a multiple of 256).
 struct CeRows {
@@ -184,11 +206,11 @@ struct CeRows {
     int* label;
     float* weight;
 };
-// x's rows in that order into xp [.., ld] (zeros beyond D and in the rows behind the last up to fill_to, 0: up to a multiple of 256); loss and dx
+// x's rows in that order into xp [.., ld] (zeros beyond D and in the rows behind the last up to a multiple of 256; f32: as parts of cap rows); loss and dx
 // (null: no gradients) of the other rows = 0.  place: scratch of R ints for more than GATHER_SCAN rows.
 constexpr long long GATHER_SCAN = 16384;
-hipError_t launch_ce_gather(const void* x, int size, long long R, int D, const int* labels, const float* weight, int ignore, long long cap, int* place,
-                            const CeRows& r, void* xp, long long ld, long long fill_to, float* loss, void* dx, hipStream_t stream);
+hipError_t launch_ce_gather(const void* x, bool f32, long long R, int D, const int* labels, const float* weight, int ignore, long long cap, int* place,
+                            const CeRows& r, void* xp, long long ld, float* loss, void* dx, hipStream_t stream);
 // Rows [row0, row0 + rows) of that order and the statistics of their scores, tiles_n parts of 2^tile_log2 columns each (arrays: of the chunk)
 struct CeChunk {
     CeRows r;
@@ -206,12 +228,14 @@ hipError_t launch_ce_finish(const CeChunk& c, hipStream_t stream);
 // kept -> score gradients bf16, in place; their column sums (part: null: none).  Does launch_ce_finish's work too where ce_grad_finishes says so.
 inline bool ce_grad_finishes(int tiles_n) { return tiles_n <= 16; }
 hipError_t launch_ce_grad(const CeChunk& c, void* kept, long long pitch, float* part, hipStream_t stream);
-// fp32: scores [rows, V] (pitch ld, without the bias) -> loss and, with grads, score gradients in place (zeros in rows behind the last)
-hipError_t launch_ce_rows_f32(const CeRows& r, long long row0, long long rows, float* scores, long long ld, int V, const Bias& b, float* loss,
-                              bool grads, hipStream_t stream);
+// fp32: scores [rows, V] (pitch ld) of a chunk -> loss and, where grad is not null, the score gradients as parts (`rows` rows of pitch ld; zeros behind the
+// last up to a multiple of 64)
+hipError_t launch_ce_rows_f32(const CeRows& r, long long row0, long long rows, const float* scores, long long ld, int V, float* loss, void* grad,
+                              hipStream_t stream);
 // total = sum of weight[r] loss[r] over the rows whose weight is not 0 (null: ones)
 hipError_t launch_ce_total(const float* loss, const float* weight, long long R, float* total, hipStream_t stream);
 // three arrays (those of length 0: none) times *factor, in place; a factor of 1 moves nothing
 hipError_t launch_scale(const float* factor, void* const (&p)[3], const long long (&n)[3], const bool (&bf16)[3], hipStream_t stream);
-hipError_t launch_col_sums_f32(const float* x, long long rows, long long ld, int N, float* part, hipStream_t stream);
+// column sums of parts [rows, ld], of the rows below *count - row0
+hipError_t launch_col_sums_f32(const void* x, long long rows, long long ld, int N, const int* count, long long row0, float* part, hipStream_t stream);
 }  // namespace rnnt

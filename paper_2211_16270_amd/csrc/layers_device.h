@@ -12,6 +12,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef bf16x8 bf16x8_any __attribute__((aligned(2)));
 typedef f16x8 f16x8_any __attribute__((aligned(2)));
 typedef f32x4 f32x4_at4 __attribute__((aligned(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
 template <typename T>
 struct Vec8;
 template <>
@@ -82,6 +83,29 @@ __device__ __forceinline__ void put8(T* p, int live, const V& x) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (j < live) p[j] = x[j];
+}
+
+// Eight floats as parts (layers.h) into the four arrays at p.  A finite value that would round to infinity takes the largest bf16 value as its first part.
+__device__ __forceinline__ void put_parts8(bf16_t* p, long long part, const float (&v)[8]) {
+    bf16x8 h, f, m, l;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float x = v[j];
+        const bool finite = fabsf(x) < -RNNT_NEG_INF;
+        const float top = __uint_as_float(0x7f7f0000u);
+        float hf = (float)(bf16_t)x;
+        hf = finite ? __builtin_amdgcn_fmed3f(hf, -top, top) : 0.0f;
+        const float r = finite ? x - hf : 0.0f;
+        const bf16_t mb = (bf16_t)r;
+        h[j] = finite ? (bf16_t)hf : (bf16_t)x;
+        f[j] = (bf16_t)hf;
+        m[j] = mb;
+        l[j] = (bf16_t)(r - (float)mb);
+    }
+    *reinterpret_cast<bf16x8*>(p) = h;
+    *reinterpret_cast<bf16x8*>(p + part) = f;
+    *reinterpret_cast<bf16x8*>(p + 2 * part) = m;
+    *reinterpret_cast<bf16x8*>(p + 3 * part) = l;
 }
 
 // Philox4x32-10 (Salmon, Moraes, Dror, Shaw: Parallel random numbers, as easy as 1, 2, 3; 2011) with key {seed} on the counter {column / 8, row, offset}:
@@ -248,6 +272,25 @@ struct LinearStore {
     }
     __device__ static __forceinline__ void bias(const LinearEpilogue& e, int n, float (&b)[8]) { load_bias8(e.bias, n < e.N ? n : e.N - 1, e.N, b); }
 };
+struct LinearStore32 {
+    typedef f32x8 Extra;
+    __device__ static __forceinline__ Extra fetch(const LinearEpilogue& e, long long m, int n) {
+        float r[8] = {};
+        if (e.residual != nullptr && m < e.M && n < e.N) load8((const float*)e.residual + (size_t)m * e.N + n, e.N - n, r);
+        return f32x8{r[0], r[1], r[2], r[3], r[4], r[5], r[6], r[7]};
+    }
+    __device__ static __forceinline__ void store(const LinearEpilogue& e, long long m, int n, float (&v)[8], const Extra& r, int = 0) {
+        if (m >= e.M || n >= e.N) return;
+        const size_t at = (size_t)m * e.N + n;
+        if (e.saved != nullptr) store8((float*)e.saved + at, e.N - n, v);
+        act8<false>(e.act, v);
+        drop8(e.drop, m, n, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += r[j];
+        store8((float*)e.y + at, e.N - n, v);
+    }
+    __device__ static __forceinline__ void bias(const LinearEpilogue& e, int n, float (&b)[8]) { LinearStore::bias(e, n, b); }
+};
 struct PlainStore {
     typedef long long Extra;             // the output's row, -1: nowhere
     __device__ static __forceinline__ Extra fetch(const StoreEpilogue& e, long long m, int n) {
@@ -308,6 +351,10 @@ struct EpilogueOf;
 template <>
 struct EpilogueOf<LinearEpilogue> {
     typedef LinearStore type;
+};
+template <>
+struct EpilogueOf<LinearEpilogue32> {
+    typedef LinearStore32 type;
 };
 template <>
 struct EpilogueOf<StoreEpilogue> {
