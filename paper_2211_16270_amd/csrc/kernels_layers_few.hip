@@ -114,7 +114,7 @@ __global__ __launch_bounds__(64 * FW) void k_few_rows(FewJob j, E e, int blocks,
     const int per = (blocks + 7) >> 3, block = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
     if ((int)(blockIdx.x >> 3) >= per || block >= blocks) return;
     if (block == 0 && slots == nullptr) e.first();
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, n0 = block * FC;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n0 = block * FC;
     const int K = j.K, N = j.N;
     unsigned char* area = smem + wave * 2048;
     const bf16_t* W = (const bf16_t*)j.W + n0 + (lane & 3) * 8;
@@ -173,13 +173,16 @@ __global__ __launch_bounds__(64 * FW) void k_few_rows(FewJob j, E e, int blocks,
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     };
     const int all = (K + 31) / 32, first = blockIdx.y * per_split, steps = first + per_split < all ? first + per_split : all;
-    static_for<0, FD>([&](auto s) { fetch(s, 32 * (first + wave + FW * decltype(s)::value)); });
+    static_for<0, FD>([&](auto s) {
+        const int t = first + wave + FW * decltype(s)::value;
+        if (t < steps) fetch(s, 32 * t);
+    });
     for (int t = first + wave; t < steps; t += FW * FD)
         static_for<0, FD>([&](auto s) {
             constexpr int q = decltype(s)::value;
             if (t + FW * q < steps) {
                 step(s);
-                fetch(s, 32 * (t + FW * (q + FD)));
+                if (t + FW * (q + FD) < steps) fetch(s, 32 * (t + FW * (q + FD)));
             }
         });
     few_finish<MT>(j, e, acc, smem, slots, block, n0);
@@ -193,7 +196,7 @@ __global__ __launch_bounds__(64 * FW) void k_few_rows_f32(FewJob j, E e, int blo
     const int per = (blocks + 7) >> 3, block = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
     if ((int)(blockIdx.x >> 3) >= per || block >= blocks) return;
     if (block == 0 && slots == nullptr) e.first();
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, n0 = block * FC, g = lane >> 4, l16 = lane & 15;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n0 = block * FC, g = lane >> 4, l16 = lane & 15;
     const int K = j.K, N = j.N;
     const float* W = (const float*)j.W;
     const float* x[MT];
@@ -236,13 +239,16 @@ __global__ __launch_bounds__(64 * FW) void k_few_rows_f32(FewJob j, E e, int blo
                 for (int c = 0; c < 2; ++c) acc[m][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[s][c][i], a[s][m][i], acc[m][c], 0, 0, 0);
     };
     const int all = (K + 31) / 32, first = blockIdx.y * per_split, steps = first + per_split < all ? first + per_split : all;
-    static_for<0, D>([&](auto s) { fetch(s, 32 * (first + wave + FW * decltype(s)::value)); });
+    static_for<0, D>([&](auto s) {
+        const int t = first + wave + FW * decltype(s)::value;
+        if (t < steps) fetch(s, 32 * t);
+    });
     for (int t = first + wave; t < steps; t += FW * D)
         static_for<0, D>([&](auto s) {
             constexpr int q = decltype(s)::value;
             if (t + FW * q < steps) {
                 step(s);
-                fetch(s, 32 * (t + FW * (q + D)));
+                if (t + FW * (q + D) < steps) fetch(s, 32 * (t + FW * (q + D)));
             }
         });
     few_finish<MT>(j, e, acc, smem, slots, block, n0);
