@@ -20,8 +20,10 @@ constexpr int GK = 64;
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x8_t __attribute__((ext_vector_type(8)));
 
-// SIDE: 0 A, 1 B of a product of parts (which part a stage takes), -1 a product of bf16 values
-template <int R, bool KS, int WAVES, int SIDE>
+// How a product goes over its operands: once; twice, an operand being two bf16 values (GemmOperand::wrap); fp32 values as parts, in pairs.
+enum Passes { ONCE = 0, TWICE, IN_PARTS };
+// SIDE: 0 A, 1 B
+template <int R, bool KS, int WAVES, Passes HOW, int SIDE>
 struct TileLoader {
     static constexpr int BYTES = R * GK * 2;
     static constexpr int PW = BYTES / 1024 / WAVES;               // copies per wave and stage
@@ -33,12 +35,14 @@ struct TileLoader {
     const unsigned char* tail;
     long long step, ld, part;                                     // bytes
     int last;                                                     // the stage that is read from `tail`, or -1
+    int wrap;                                                     // the stage that is stage 0 again
     unsigned voff[NV];
 
     __device__ __forceinline__ void init(const GemmOperand& o, long long i0, long long n_i, int wave, int lane) {
         ld = o.ld * 2;
         part = o.part * 2;
         last = o.tail != nullptr ? o.tail_stage : -1;
+        wrap = o.wrap;
         if constexpr (KS) {
             const int per = R / 8, slot = lane & (per - 1);
             main = (const unsigned char*)o.p + i0 * 2 + (long long)(wave * PW * KR) * ld;
@@ -71,10 +75,14 @@ struct TileLoader {
     }
     __device__ __forceinline__ const unsigned char* stage(int s) const {
         const unsigned char* p;
-        if constexpr (SIDE >= 0) {
+        if constexpr (HOW == IN_PARTS) {
             // pairs (1, 3), (2, 2), (3, 1), (1, 2), (2, 1), (0, 0): parts as a table of four bits each
             const int block = s / PAIRS, pair = s - block * PAIRS;
             p = main + block * step + ((SIDE == 0 ? 0x021321u : 0x012123u) >> (4 * pair) & 15u) * part;
+        } else if constexpr (HOW == TWICE) {
+            const bool again = s >= wrap;
+            const int t = again ? s - wrap : s;
+            p = (KS && t == last ? tail : main + t * step) + (again ? part : 0);
         } else p = KS && s == last ? tail : main + s * step;
         // (uniform, and said so: the copies take it in scalar registers)
         const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)(size_t)p), hi = __builtin_amdgcn_readfirstlane((unsigned)((size_t)p >> 32));
@@ -189,16 +197,16 @@ struct ColumnBias {
 // both, all copies in the fourth step: 8192^3 1250 to 1280 TFLOP/s, now 1335; without any copies 1470 to 1510.  The rest of the loss is the prologue and
 // the epilogue, which nothing hides: K = 1024 940 TFLOP/s.)  A wave has priority while it sends MFMAs (K = 1024: 874 without).
 // init: what the sums of the columns start from.
-// F32: a product of parts.  The matrix instruction's accumulation rounds towards minus infinity, alike for all results: 5e-11 of a result's size per unit of
+// IN_PARTS: the matrix instruction's accumulation rounds towards minus infinity, alike for all results: 5e-11 of a result's size per unit of
 // depth, which sums over many of them would show.  So every 1024 of depth the sum changes its sign, and B enters with the other one.
-template <class TS, bool AKS, bool BKS, bool F32, class INIT>
+template <class TS, bool AKS, bool BKS, Passes HOW, class INIT>
 __device__ __forceinline__ void gemm_tile(f32x16 (&acc)[TS::MT][TS::NT], const GemmOperand& ga, const GemmOperand& gb, long long m0, long long n0,
                                           long long M, long long N, int s0, int s1, unsigned char* smem, const INIT& init) {
     constexpr int MT = TS::MT, NT = TS::NT;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int wm = wave / TS::WN, wn = wave % TS::WN;
-    typedef TileLoader<TS::BM, AKS, TS::WAVES, F32 ? 0 : -1> LA;
-    typedef TileLoader<TS::BN, BKS, TS::WAVES, F32 ? 1 : -1> LB;
+    typedef TileLoader<TS::BM, AKS, TS::WAVES, HOW, 0> LA;
+    typedef TileLoader<TS::BN, BKS, TS::WAVES, HOW, 1> LB;
     LA la;
     LB lb;
     la.init(ga, m0, M, wave, lane);
@@ -272,7 +280,7 @@ __device__ __forceinline__ void gemm_tile(f32x16 (&acc)[TS::MT][TS::NT], const G
     };
     unsigned sign = 0;                                            // of B's entries, twice per register
     auto turn_signs = [&](int s) {
-        if constexpr (F32) {
+        if constexpr (HOW == IN_PARTS) {
             const unsigned now = (s / PAIRS) & (1024 / GK) ? 0x80008000u : 0u;
             if (now != sign) {
 #pragma unroll
@@ -284,7 +292,7 @@ __device__ __forceinline__ void gemm_tile(f32x16 (&acc)[TS::MT][TS::NT], const G
         }
     };
     auto signed_b = [&](int set) {
-        if constexpr (F32) {
+        if constexpr (HOW == IN_PARTS) {
 #pragma unroll
             for (int j = 0; j < NT; ++j) fb[set][j] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, fb[set][j]) ^ sign);
         }
@@ -319,7 +327,7 @@ __device__ __forceinline__ void gemm_tile(f32x16 (&acc)[TS::MT][TS::NT], const G
         a2 = t;
         b0 ^= TS::OPER;
     }
-    if constexpr (F32)
+    if constexpr (HOW == IN_PARTS)
         if (sign != 0) {
 #pragma unroll
             for (int i = 0; i < MT; ++i)

@@ -28,7 +28,7 @@ __device__ __forceinline__ JobExtent job_extent(const GemmJob& g) {
     return x;
 }
 
-template <class TS, bool AKS, bool BKS, bool F32, class E>
+template <class TS, bool AKS, bool BKS, Passes HOW, class E>
 __device__ __forceinline__ void gemm_workgroup(const GemmJob& g, const E& e, int L, int mt, int nt, int splits, int per_split, unsigned char* smem) {
     TilePlace t;
     if (!place_tile(L, mt, nt, splits, t)) return;
@@ -39,14 +39,15 @@ __device__ __forceinline__ void gemm_workgroup(const GemmJob& g, const E& e, int
     f32x16 acc[TS::MT][TS::NT];
     constexpr bool LINEAR = std::is_base_of_v<LinearEpilogue, E>;
     // (scores in fp32 are the only other results with a bias)
-    if constexpr (LINEAR || (F32 && !AKS && BKS))
-        gemm_tile<TS, AKS, BKS, F32>(acc, g.A, g.B, m0, n0, g.a_rows, g.b_rows, s0, s1, smem, ColumnBias{e.bias, e.N, 0.0f});
-    else gemm_tile<TS, AKS, BKS, F32>(acc, g.A, g.B, m0, n0, g.a_rows, g.b_rows, s0, s1, smem, NoBias{});
+    if constexpr (LINEAR || (HOW == IN_PARTS && !AKS && BKS))
+        gemm_tile<TS, AKS, BKS, HOW>(acc, g.A, g.B, m0, n0, g.a_rows, g.b_rows, s0, s1, smem, ColumnBias{e.bias, e.N, 0.0f});
+    else gemm_tile<TS, AKS, BKS, HOW>(acc, g.A, g.B, m0, n0, g.a_rows, g.b_rows, s0, s1, smem, NoBias{});
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int wm = wave / TS::WN, wn = wave % TS::WN, n = (int)n0 + wn * TS::NT * 32 + 8 * (lane & 7);
     unsigned char* area = smem + wave * TURN32_BYTES;
     static_assert(TS::NT == 2 && TS::WAVES * TURN32_BYTES <= TS::SMEM, "a wave's 64 columns");
     typedef typename EpilogueOf<E>::type Store;
+    const float factor = Store::factor(e);
 #pragma unroll
     for (int i = 0; i < TS::MT; ++i) {
         typename Store::Extra x[4];
@@ -62,7 +63,7 @@ __device__ __forceinline__ void gemm_workgroup(const GemmJob& g, const E& e, int
             turn32_take(area, k, lane, v);
             // (a register array indexed by the loop's counter would lie in memory)
             const typename Store::Extra r = k & 2 ? (k & 1 ? x[3] : x[2]) : (k & 1 ? x[1] : x[0]);
-            Store::store(e, m, n, v, r, t.split);
+            Store::store(e, m, n, v, r, factor, t.split);
         }
         turn_fence();
     }
@@ -76,21 +77,20 @@ struct TileJob {
     int mt, nt, splits, per_split;
     __host__ __device__ long long workgroups() const { return ((long long)mt * nt * splits + 7) / 8 * 8; }
 };
-template <class TS, bool AKS, bool BKS, bool F32, class E>
+template <class TS, bool AKS, bool BKS, Passes HOW, class E>
 __global__ __launch_bounds__(TS::THREADS, 2) void k_layer_gemm(TileJob<E> j) {
     extern __shared__ __align__(16) unsigned char smem[];
     if (blockIdx.x == 0) pass_rng(j.e);
-    gemm_workgroup<TS, AKS, BKS, F32, E>(j.g, j.e, blockIdx.x, j.mt, j.nt, j.splits, j.per_split, smem);
+    gemm_workgroup<TS, AKS, BKS, HOW, E>(j.g, j.e, blockIdx.x, j.mt, j.nt, j.splits, j.per_split, smem);
 }
-// dx and dW; the product whose workgroups take longer goes first (CE, 9288 x 1024 x 32768, dx in 148 workgroups of 512 stages: behind dW's 512 of 146 the
-// two took 1200 us, in front of them xxx).
-template <class TS, bool F32>
+// dx and dW; the product whose workgroups take longer goes first (16000 x 1024 x 4096: 239 us, behind the other 308).
+template <class TS, Passes HOW>
 __global__ __launch_bounds__(TS::THREADS, 2) void k_layer_grads(TileJob<StoreEpilogue> x, TileJob<StoreEpilogue> w, int wgs_x, int wgs_w) {
     extern __shared__ __align__(16) unsigned char smem[];
     const bool x_first = x.per_split > w.per_split;
     const int L = blockIdx.x, is_x = x_first ? L < wgs_x : L >= wgs_w;
-    if (is_x) gemm_workgroup<TS, false, false, F32, StoreEpilogue>(x.g, x.e, x_first ? L : L - wgs_w, x.mt, x.nt, x.splits, x.per_split, smem);
-    else gemm_workgroup<TS, true, true, F32, StoreEpilogue>(w.g, w.e, x_first ? L - wgs_x : L, w.mt, w.nt, w.splits, w.per_split, smem);
+    if (is_x) gemm_workgroup<TS, false, false, HOW, StoreEpilogue>(x.g, x.e, x_first ? L : L - wgs_w, x.mt, x.nt, x.splits, x.per_split, smem);
+    else gemm_workgroup<TS, true, true, HOW, StoreEpilogue>(w.g, w.e, x_first ? L - wgs_x : L, w.mt, w.nt, w.splits, w.per_split, smem);
 }
 
 // The sum of the splits' results, in order, and the epilogue.  One thread per eight columns.
@@ -123,7 +123,7 @@ __device__ __forceinline__ void reduce_workgroup(const ReduceJob<E>& r, unsigned
     Store::bias(r.e, n, bias);
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] += bias[k];
-    Store::store(r.e, m, n, v, x);
+    Store::store(r.e, m, n, v, x, Store::factor(r.e));
 }
 template <class E>
 __global__ __launch_bounds__(256) void k_layer_reduce(ReduceJob<E> r) {
@@ -152,7 +152,7 @@ __global__ __launch_bounds__(TS::THREADS, 2) void k_ce_scores(GemmJob g, CeEpilo
     if (m0 >= x.M) return;
     f32x16 acc[TS::MT][TS::NT];
     // (entries beyond the vocabulary are -inf)
-    gemm_tile<TS, false, true, false>(acc, g.A, g.B, m0, n0, g.a_rows, g.b_rows, 0, g.stages, smem, ColumnBias{e.bias, e.V, RNNT_NEG_INF});
+    gemm_tile<TS, false, true, ONCE>(acc, g.A, g.B, m0, n0, g.a_rows, g.b_rows, 0, g.stages, smem, ColumnBias{e.bias, e.V, RNNT_NEG_INF});
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l32 = lane & 31, hb = lane >> 5;
     const int wm = wave / TS::WN, wn = wave % TS::WN;
     float* top = reinterpret_cast<float*>(smem);                  // [WN][BM]
@@ -251,41 +251,41 @@ TileJob<E> tile_job(const GemmJob& g, const E& e, int splits, int per_split) {
 }
 inline long long padded8(long long n) { return (n + 7) / 8 * 8; }
 StoreEpilogue slot_epilogue(const GemmJob& g, float* slots) {
-    return StoreEpilogue{slots, nullptr, nullptr, padded8(g.N), g.M * padded8(g.N), Bias{}, g.M, (int)padded8(g.N), false};
+    return StoreEpilogue{slots, nullptr, 1.0f, nullptr, nullptr, padded8(g.N), g.M * padded8(g.N), Bias{}, g.M, (int)padded8(g.N), false};
 }
 template <class E>
 ReduceJob<E> reduce_job(const GemmJob& g, const E& e, const float* slots, int splits) {
     return ReduceJob<E>{g, e, slots, splits, padded8(g.N), g.M * padded8(g.N), g.M * (padded8(g.N) / 8)};
 }
 
-template <class TS, bool F32, class E>
+template <class TS, Passes HOW, class E>
 hipError_t gemm_of(const GemmJob& g, const GemmPlan& p, float* slots, const E& e, hipStream_t stream) {
     if (p.splits <= 1) {
         const TileJob<E> j = tile_job<TS>(g, e, 1, g.stages);
-        return launch_tiles<&k_layer_gemm<TS, false, true, F32, E>, TS>(j.workgroups(), stream, j);
+        return launch_tiles<&k_layer_gemm<TS, false, true, HOW, E>, TS>(j.workgroups(), stream, j);
     }
     const TileJob<StoreEpilogue> j = tile_job<TS>(g, slot_epilogue(g, slots), p.splits, p.per_split);
-    hipError_t err = launch_tiles<&k_layer_gemm<TS, false, true, F32, StoreEpilogue>, TS>(j.workgroups(), stream, j);
+    hipError_t err = launch_tiles<&k_layer_gemm<TS, false, true, HOW, StoreEpilogue>, TS>(j.workgroups(), stream, j);
     if (err != hipSuccess) return err;
     const ReduceJob<E> r = reduce_job(g, e, slots, p.splits);
     if ((r.total + 255) / 256 > 0x7fffffffLL) return hipErrorInvalidValue;
     k_layer_reduce<E><<<dim3(r.workgroups()), dim3(256), 0, stream>>>(r);
     return hipGetLastError();
 }
-template <bool F32, class E>
+template <Passes HOW, class E>
 hipError_t gemm_of(const GemmJob& g, const GemmPlan& p, float* slots, const E& e, hipStream_t stream) {
     if (g.M <= 0 || g.N <= 0) return hipSuccess;
-    return p.tile == 256 ? gemm_of<TileShape<256>, F32>(g, p, slots, e, stream) : gemm_of<TileShape<128>, F32>(g, p, slots, e, stream);
+    return p.tile == 256 ? gemm_of<TileShape<256>, HOW>(g, p, slots, e, stream) : gemm_of<TileShape<128>, HOW>(g, p, slots, e, stream);
 }
 
-template <class TS, bool F32>
+template <class TS, Passes HOW>
 hipError_t grad_gemms(const GradGemm& dx, const GradGemm& dw, hipStream_t stream) {
     TileJob<StoreEpilogue> x{}, w{};
     if (dx.g.M > 0) x = tile_job<TS>(dx.g, dx.splits > 1 ? slot_epilogue(dx.g, dx.slots) : dx.e, dx.splits, dx.splits > 1 ? dx.per_split : dx.g.stages);
     if (dw.g.M > 0) w = tile_job<TS>(dw.g, dw.splits > 1 ? slot_epilogue(dw.g, dw.slots) : dw.e, dw.splits, dw.splits > 1 ? dw.per_split : dw.g.stages);
     const long long nx = x.workgroups(), nw = w.workgroups();
     if (nx + nw > 0x7ffffff0LL) return hipErrorInvalidValue;
-    return launch_tiles<&k_layer_grads<TS, F32>, TS>(nx + nw, stream, x, w, (int)nx, (int)nw);
+    return launch_tiles<&k_layer_grads<TS, HOW>, TS>(nx + nw, stream, x, w, (int)nx, (int)nw);
 }
 
 }  // namespace
@@ -354,13 +354,13 @@ PairPlan plan_pair(long long Mx, long long Nx, int stages_x, long long Mw, long 
 }
 
 hipError_t launch_linear_gemm(const GemmJob& g, const GemmPlan& p, float* slots, const LinearEpilogue& e, hipStream_t stream) {
-    return gemm_of<false>(g, p, slots, e, stream);
+    return gemm_of<ONCE>(g, p, slots, e, stream);
 }
 hipError_t launch_linear_gemm(const GemmJob& g, const GemmPlan& p, float* slots, const LinearEpilogue32& e, hipStream_t stream) {
-    return gemm_of<true>(g, p, slots, e, stream);
+    return gemm_of<IN_PARTS>(g, p, slots, e, stream);
 }
 hipError_t launch_scores_f32(const GemmJob& g, int tile, const StoreEpilogue& e, hipStream_t stream) {
-    return gemm_of<true>(g, GemmPlan{tile, 1, g.stages}, nullptr, e, stream);
+    return gemm_of<IN_PARTS>(g, GemmPlan{tile, 1, g.stages}, nullptr, e, stream);
 }
 hipError_t launch_linear_reduce(bool f32, long long M, int N, int splits, const float* slots, const LinearEpilogue& e, hipStream_t stream) {
     GemmJob g{};
@@ -377,8 +377,10 @@ hipError_t launch_grad_gemms(bool parts, int tile, const GradGemm& dx, const Gra
     if (dx.g.M > 0 || dw.g.M > 0) {
         typedef TileShape<256> L;
         typedef TileShape<128> S;
-        const hipError_t e = tile == 256 ? (parts ? grad_gemms<L, true>(dx, dw, stream) : grad_gemms<L, false>(dx, dw, stream))
-                                         : (parts ? grad_gemms<S, true>(dx, dw, stream) : grad_gemms<S, false>(dx, dw, stream));
+        const bool twice = dx.g.A.wrap > 0 || dw.g.B.wrap > 0;
+        const hipError_t e = parts   ? (tile == 256 ? grad_gemms<L, IN_PARTS>(dx, dw, stream) : grad_gemms<S, IN_PARTS>(dx, dw, stream))
+                             : twice ? grad_gemms<S, TWICE>(dx, dw, stream)
+                                     : (tile == 256 ? grad_gemms<L, ONCE>(dx, dw, stream) : grad_gemms<S, ONCE>(dx, dw, stream));
         if (e != hipSuccess) return e;
     }
     ReduceJob<StoreEpilogue> x{}, w{};

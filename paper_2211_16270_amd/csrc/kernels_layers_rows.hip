@@ -45,7 +45,7 @@ __device__ __forceinline__ void fold_columns(float (&sum)[8], float (*red)[256],
     if (n + tid < N) part[n + tid] = t;
 }
 
-// dz = dy act'(z) mask / (1 - p): a workgroup takes R rows x 256 columns, 8 thread rows x 32 granules of 8 columns.
+// dz = dy act'(z) mask: a workgroup takes R rows x 256 columns, 8 thread rows x 32 granules of 8 columns.
 template <typename T, typename S>
 __global__ __launch_bounds__(256) void k_layer_dz(DzArgs a, int R) {
     constexpr bool FAST = sizeof(T) == 2;
@@ -77,28 +77,26 @@ __global__ __launch_bounds__(256) void k_layer_dz(DzArgs a, int R) {
         for (int j = 0; j < 8; ++j) sum[j] += v[j];
         if (a.dz != nullptr) {
             bf16_t* o = (bf16_t*)a.dz + (size_t)m * a.ld + n;     // (ld is a multiple of 64)
-            if constexpr (sizeof(T) == 2) {
-                bf16x8 x;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = (bf16_t)v[j];
-                *reinterpret_cast<bf16x8*>(o) = x;
-            } else put_parts8(o, a.rows_to * a.ld, v);
+            if constexpr (sizeof(T) == 2) put_rounded8(o, a.rest, v);
+            else put_parts8(o, a.rows_to * a.ld, v);
         }
     }
     if (a.part != nullptr && r0 < a.M) fold_columns(sum, red, a.part + (size_t)rb * a.ld, n0, a.N, tid);
 }
 
-__global__ __launch_bounds__(256) void k_layer_sum_parts(SumJob j, int blocks, int R) {
-    __shared__ float red[8][32];
-    sum_parts(j, blocks, R, blockIdx.x, red);
-}
-
 // ---- cross entropy --------------------------------------------------------------------------------------------------
+// The unit of the score gradients: the mantissa of the largest weight.  The label's gradient is w (p - 1), by far the largest of a row, and its rounding to bf16
+// is off by up to 2^-8 where that lies just above a power of two, by the same for all rows where all have one weight and little p: a gradient's error was
+// 0.0029 of it with weights of 1.01 / 1024.  Relative to the unit it is p - 1, which has 2^-9 at most.
+__device__ __forceinline__ float unit_of(float largest) {
+    return largest > 0.0f && largest < -RNNT_NEG_INF ? __uint_as_float((__float_as_uint(largest) & 0x007fffffu) | 0x3f800000u) : 1.0f;
+}
 // Each workgroup counts the real rows before its own SCAN_ROWS (the labels come from the L2) and numbers its own.
 constexpr int SCAN_THREADS = 1024, SCAN_PER = 4, SCAN_ROWS = SCAN_THREADS * SCAN_PER;
 __global__ __launch_bounds__(SCAN_THREADS) void k_ce_rows(const int* __restrict__ labels, const float* __restrict__ weight, long long R, int ignore,
                                                           long long cap, int* __restrict__ place, CeRows r) {
     __shared__ int wave_sum[SCAN_THREADS / 64], wave_before[SCAN_THREADS / 64];
+    __shared__ float wave_most[SCAN_THREADS / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const long long first = (long long)blockIdx.x * SCAN_ROWS;
     int before = 0;
@@ -143,7 +141,21 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_ce_rows(const int* __restrict_
         }
     }
     if (blockIdx.x == gridDim.x - 1) {
-        if (tid == 0) *r.count = total;
+        float most = weight != nullptr ? 0.0f : 1.0f;
+        if (weight != nullptr)
+#pragma unroll 8
+            for (long long i = tid; i < R; i += SCAN_THREADS) {
+                const float w = weight[i];
+                most = labels[i] != ignore ? fmaxf(most, fabsf(w)) : most;
+            }
+        most = wave_max(most);
+        if (lane == 0) wave_most[wave] = most;
+        __syncthreads();
+        if (tid == 0) {
+            for (int w = 0; w < SCAN_THREADS / 64; ++w) most = fmaxf(most, wave_most[w]);
+            *r.count = total;
+            *const_cast<float*>(ce_unit(r)) = unit_of(most);
+        }
         // behind the last row: no label, no weight, up to the end of the arrays
         for (long long i = total + tid; i < cap; i += SCAN_THREADS) {
             r.index[i] = -1;
@@ -163,6 +175,7 @@ __global__ __launch_bounds__(256) void k_ce_gather(const T* __restrict__ x, long
                                                    const float* __restrict__ weight, int ignore, long long cap, const int* __restrict__ place, CeRows r,
                                                    bf16_t* __restrict__ xp, long long ld, float* __restrict__ loss, T* __restrict__ dx, int row_wgs) {
     __shared__ int wave_count[4], at_row[GATHER_ROWS];
+    __shared__ float wave_most[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const long long first = (long long)blockIdx.x * GATHER_ROWS;
     const bool fill = (int)blockIdx.x >= row_wgs;
@@ -230,7 +243,27 @@ __global__ __launch_bounds__(256) void k_ce_gather(const T* __restrict__ x, long
 #pragma unroll
             for (int q = 0; q < (sizeof(T) == 2 ? 1 : PARTS); ++q) *reinterpret_cast<bf16x8*>(xp + q * cap * ld + (size_t)at * ld + c) = bf16x8{0};
     if constexpr (SCAN) {
-        if (wg == 0 && tid == 0) *r.count = (int)n;
+        if (wg == 0) {
+            float most = weight != nullptr ? 0.0f : 1.0f;
+            if (weight != nullptr) {
+                long long i = tid * 4;
+#pragma unroll 4
+                for (; i + 4 <= R; i += 1024) {
+                    const i32x4_any y = *reinterpret_cast<const i32x4_any*>(labels + i);
+                    const f32x4_at4 w = *reinterpret_cast<const f32x4_at4*>(weight + i);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) most = y[j] != ignore ? fmaxf(most, fabsf(w[j])) : most;
+                }
+                for (; i < R; ++i) most = labels[i] != ignore ? fmaxf(most, fabsf(weight[i])) : most;
+            }
+            most = wave_max(most);
+            if (lane == 0) wave_most[wave] = most;
+            __syncthreads();
+            if (tid == 0) {
+                *r.count = (int)n;
+                *const_cast<float*>(ce_unit(r)) = unit_of(fmaxf(fmaxf(wave_most[0], wave_most[1]), fmaxf(wave_most[2], wave_most[3])));
+            }
+        }
         for (long long i = n + wg * 256 + tid; i < cap; i += wgs * 256) {
             r.index[i] = -1;
             r.label[i] = -1;
@@ -239,14 +272,17 @@ __global__ __launch_bounds__(256) void k_ce_gather(const T* __restrict__ x, long
     }
 }
 
-// Row i of a chunk: lse = M + ln(S / 2^15) out of the parts' statistics, loss = lse - score of the label (at < 0: not written); its scale.
-__device__ __forceinline__ float2 ce_finish_row(const CeChunk& c, long long i, int at, float M, float S) {
+// Row i of a chunk: lse = M + ln(S / 2^15) out of the parts' statistics, loss = lse - score of the label (at < 0: not written); its scale.  The label's gradient
+// w (p - 1) = w expm1(-loss): the difference would leave little of it where p is near 1.
+__device__ __forceinline__ float4 ce_finish_row(const CeChunk& c, long long i, int at, float M, float S) {
     const float m = M == RNNT_NEG_INF ? 0.0f : M;
     const int y = c.r.label[c.row0 + i];
     // (no entry of the vocabulary is possible, or the label is none of them: +inf)
     const bool none = S == 0.0f || (unsigned)y >= (unsigned)c.V;
-    if (at >= 0) c.loss[at] = none ? -RNNT_NEG_INF : (m - c.label_score[i]) + LN2_F * (__builtin_amdgcn_logf(S) - 15.0f);
-    return make_float2(m, S == 0.0f || c.identity ? 0.0f : c.r.weight[c.row0 + i] / S);
+    const float loss = none ? -RNNT_NEG_INF : (m - c.label_score[i]) + logf(S * 0x1p-15f);
+    if (at >= 0) c.loss[at] = loss;
+    const float w = c.identity ? 0.0f : c.r.weight[c.row0 + i] / *ce_unit(c.r);
+    return make_float4(m, S == 0.0f ? 0.0f : w / S, w * expm1f(-loss), 0.0f);
 }
 
 // One wavefront per row
@@ -273,16 +309,16 @@ __global__ __launch_bounds__(256) void k_ce_finish(CeChunk c) {
     for (int t = lane; t < c.tiles_n; t += 64) s += st[t].y * __builtin_amdgcn_exp2f((st[t].x - z) * LOG2E_F);
     const float S = wave_sum(s);
     if (lane == 0) {
-        const float2 f = ce_finish_row(c, i, at, M, S);
+        const float4 f = ce_finish_row(c, i, at, M, S);
         if (c.scale != nullptr) c.scale[i] = f;
     }
 }
 
 // A workgroup takes R rows x 256 columns.  FINISH: it also forms its rows' sums (those of the first columns write the losses).
 template <bool FINISH>
-__global__ __launch_bounds__(256) void k_ce_grad(CeChunk c, void* __restrict__ kept, long long pitch, float* __restrict__ part, int R) {
+__global__ __launch_bounds__(256) void k_ce_grad(CeChunk c, void* __restrict__ kept, long long pitch, long long rest, float* __restrict__ part, int R) {
     __shared__ __align__(16) float red[8][256];
-    __shared__ float2 scale[128];
+    __shared__ float4 scale[128];
     const int nb = (c.V + 255) / 256, rb = blockIdx.x / nb;
     const int tid = threadIdx.x, n0 = (blockIdx.x - rb * nb) * 256, n = n0 + (tid & 31) * 8;
     const long long r0 = (long long)rb * R;
@@ -292,7 +328,7 @@ __global__ __launch_bounds__(256) void k_ce_grad(CeChunk c, void* __restrict__ k
     const long long real_rows = (long long)*r.count - row0, live = (real_rows + 63) / 64 * 64;
     if (r0 >= live || real_rows <= 0) return;
     if (tid < R) {
-        float2 f = make_float2(0.0f, 0.0f);
+        float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (r0 + tid < real_rows) {
             if constexpr (FINISH) {
                 const float2* st = c.stats + (size_t)(r0 + tid) * c.tiles_n;
@@ -315,28 +351,20 @@ __global__ __launch_bounds__(256) void k_ce_grad(CeChunk c, void* __restrict__ k
             const long long m = r0 + in;
             if (m >= live) break;
             f16x8* at = reinterpret_cast<f16x8*>((_Float16*)kept + (size_t)m * pitch + n);
-            bf16x8 o = bf16x8{0};
+            float v[8] = {};
             if (m < real_rows) {
                 const f16x8 h = *at;
-                const float2 f = scale[in];
+                const float4 f = scale[in];
                 // (a row without a possible entry has f.y = 0 and parts of -inf; its exponentials are zeros)
                 const float k = f.y * __builtin_amdgcn_exp2f((c.stats[(size_t)m * c.tiles_n + t].x - f.x) * LOG2E_F);
-                const int y = r.label[row0 + m] - n;
-                float v[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = (float)h[j] * k;
-                if ((unsigned)y < 8u && n + y < c.V) {
-                    const float w = r.weight[row0 + m];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] -= y == j ? w : 0.0f;
-                }
+                const int label = r.label[row0 + m], y = label < c.V ? label - n : -1;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
+                    v[j] = y == j ? f.z : (float)h[j] * k;
                     sum[j] += v[j];
-                    o[j] = (bf16_t)v[j];
                 }
             }
-            *reinterpret_cast<bf16x8*>(at) = o;
+            put_rounded8(reinterpret_cast<bf16_t*>(at), rest, v);
         }
     if (part != nullptr) fold_columns(sum, red, part + (size_t)rb * pitch, n0, c.V, tid);
 }
@@ -387,15 +415,13 @@ __global__ __launch_bounds__(256) void k_ce_rows_f32(CeRows r, long long row0, c
     if (lane == 0) red[wave].y = s;
     __syncthreads();
     const float S = (red[0].y + red[1].y) + (red[2].y + red[3].y);
-    if (tid == 0) loss[at] = S == 0.0f || !known ? -RNNT_NEG_INF : (c - hy) + logf(S);
+    const float row_loss = S == 0.0f || !known ? -RNNT_NEG_INF : (c - hy) + logf(S);
+    if (tid == 0) loss[at] = row_loss;
     if (grad == nullptr) return;
-    const float w = r.weight[row0 + i], f = S == 0.0f ? 0.0f : w / S;
+    const float w = r.weight[row0 + i], f = S == 0.0f ? 0.0f : w / S, of_label = w * expm1f(-row_loss);      // (w (p - 1), see ce_finish_row)
     each([&](int v, float (&x)[8]) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            x[k] = S == 0.0f ? 0.0f : expf(x[k] - c) * f;
-            if (v + k == y) x[k] -= w;
-        }
+        for (int k = 0; k < 8; ++k) x[k] = v + k == y ? of_label : S == 0.0f ? 0.0f : expf(x[k] - c) * f;
         put_parts8(g + v, part, x);
     });
     for (int v = (V + 7) / 8 * 8 + tid * 8; v < ld; v += 2048)
@@ -506,12 +532,6 @@ hipError_t launch_dz(bool bf16, const DzArgs& a, hipStream_t stream) {
     return hipGetLastError();
 }
 
-hipError_t launch_sum_parts(const SumJob& j, hipStream_t stream) {
-    if (j.N <= 0 || j.part == nullptr) return hipSuccess;
-    k_layer_sum_parts<<<dim3(blocks_of(j.N, 32)), dim3(256), 0, stream>>>(j, (int)sum_blocks(j.rows, j.N), sum_rows(j.rows, j.N));
-    return hipGetLastError();
-}
-
 namespace {
 template <typename T>
 hipError_t gather(const void* x, long long R, int D, const int* labels, const float* weight, int ignore, long long cap, int* place, const CeRows& r, void* xp,
@@ -540,12 +560,12 @@ hipError_t launch_ce_finish(const CeChunk& c, hipStream_t stream) {
     k_ce_finish<<<dim3(blocks_of(c.rows, 4)), dim3(256), 0, stream>>>(c);
     return hipGetLastError();
 }
-hipError_t launch_ce_grad(const CeChunk& c, void* kept, long long pitch, float* part, hipStream_t stream) {
+hipError_t launch_ce_grad(const CeChunk& c, void* kept, long long pitch, long long rest, float* part, hipStream_t stream) {
     const int R = sum_rows(c.rows, c.V);
     const long long n = (long long)blocks_of(c.V, 256) * sum_blocks(c.rows, c.V);
     if (!grid_fits(n)) return hipErrorInvalidValue;
-    if (ce_grad_finishes(c.tiles_n)) k_ce_grad<true><<<dim3((unsigned)n), dim3(256), 0, stream>>>(c, kept, pitch, part, R);
-    else k_ce_grad<false><<<dim3((unsigned)n), dim3(256), 0, stream>>>(c, kept, pitch, part, R);
+    if (ce_grad_finishes(c.tiles_n)) k_ce_grad<true><<<dim3((unsigned)n), dim3(256), 0, stream>>>(c, kept, pitch, rest, part, R);
+    else k_ce_grad<false><<<dim3((unsigned)n), dim3(256), 0, stream>>>(c, kept, pitch, rest, part, R);
     return hipGetLastError();
 }
 hipError_t launch_ce_rows_f32(const CeRows& r, long long row0, long long rows, const float* scores, long long ld, int V, float* loss, void* grad,

@@ -72,6 +72,7 @@ struct LinearPlan {
     bool f32, few;                        // few: forward pass of at most FEW_ROWS rows, one launch on the arrays as they are
     int few_splits;
     bool copy_x, copy_w, own_dz;
+    bool rest;                            // backward: dz in two bf16 values, the rounded one and the rest
     long long Kp, Np, Mp;                 // multiples of 64
     size_t off_x, off_w, off_dz, off_xt, off_dyt, off_part, off_slots, off_slots_w, bytes;
     GemmPlan y;
@@ -103,8 +104,10 @@ LinearPlan plan_linear(const rnnt_linear_desc& d, bool backward) {
         p.own_dz = p.f32 || !plain || N % 64 != 0;
         p.copy_x = p.f32 || K % 8 != 0;
         p.copy_w = p.f32 || N % 64 != 0;
-        p.grads = plan_pair(M, K, (int)(p.Np / 64) * per, K, N, (int)(p.Mp / 64) * per, SLOT_CAP);
-        p.off_dz = c.take(p.own_dz ? (size_t)p.Mp * p.Np * e : 0);
+        p.rest = !p.f32 && M <= FEW_ROWS && d.activation != ACT_NONE && d.activation != ACT_RELU;
+        const int passes = p.rest ? 2 : per;
+        p.grads = plan_pair(M, K, (int)(p.Np / 64) * passes, K, N, (int)(p.Mp / 64) * passes, SLOT_CAP);
+        p.off_dz = c.take(p.own_dz ? (size_t)p.Mp * p.Np * e * (p.rest ? 2 : 1) : 0);
         p.off_x = c.take(p.copy_x ? (size_t)p.Mp * p.Kp * e : 0);
         p.off_w = c.take(p.copy_w ? (size_t)K * p.Np * e : 0);
         p.off_xt = c.take(!p.copy_x && M % 64 != 0 ? (size_t)64 * K * 2 : 0);
@@ -119,7 +122,15 @@ LinearPlan plan_linear(const rnnt_linear_desc& d, bool backward) {
 
 // An operand: the caller's array of pitch ld, or a copy of `rows` rows of pitch ld_copy
 GemmOperand operand(bool copied, bool f32, const void* own, long long ld, const void* copy, long long rows, long long ld_copy) {
-    return copied ? GemmOperand{copy, ld_copy, f32 ? rows * ld_copy : 0, nullptr, -1} : GemmOperand{own, ld, 0, nullptr, -1};
+    return copied ? GemmOperand{copy, ld_copy, f32 ? rows * ld_copy : 0, nullptr, -1, 0} : GemmOperand{own, ld, 0, nullptr, -1, 0};
+}
+
+// A bf16 product with an operand in two values: `once` by the rounded ones, then by the rest.
+// Rounding the gradient to bf16 adds as much to the products' error as their own rounding does, sqrt(2) times it where many values average; the few of a few
+// rows do not (up to 3 times).  There, up to FEW_ROWS rows, the products wait for W and dW rather than for their operations.
+void take_twice(GemmOperand& once, GemmOperand& two, long long rest, int stages) {
+    once.wrap = two.wrap = stages;
+    two.part = rest;
 }
 
 rnnt_status linear_fwd(const rnnt_linear_desc& d, const LinearPlan& p, const void* x, const void* W, const Bias& b, const void* residual,
@@ -153,10 +164,13 @@ rnnt_status linear_bwd(const rnnt_linear_desc& d, const LinearPlan& p, const voi
     const long long M = d.M, K = d.K, N = d.N, whole = M / 64 * 64;
     const bool ragged = M % 64 != 0;
     float* part = (float*)(ws + p.off_part);
+    Dropout mask = drop;                  // (its factor: in the products' epilogues)
+    mask.scale = 1.0f;
+    const long long rest = p.rest ? p.Mp * p.Np : 0;
     if (M == 0) dx = nullptr;
     if (M > 0 && (db || (p.own_dz && (dx || dW)))) {
         const DzArgs a{dy, d.activation == ACT_NONE ? nullptr : saved, p.own_dz && (dx || dW) ? ws + p.off_dz : nullptr, db ? part : nullptr, M,
-                       p.own_dz ? p.Mp : M, d.N, p.Np, d.activation, drop};
+                       p.own_dz ? p.Mp : M, d.N, p.Np, d.activation, mask, rest};
         LAYER_HIP(launch_dz(!p.f32, a, stream));
     }
     const int kind = p.f32 ? PAD_PARTS : PAD_16;
@@ -167,7 +181,7 @@ rnnt_status linear_bwd(const rnnt_linear_desc& d, const LinearPlan& p, const voi
     if (dW && !p.own_dz && ragged) pads.add(PAD_16, dy, M, N, whole, ws + p.off_dyt, 64, N);
     LAYER_HIP(launch_pads(pads, stream));
     GradGemm gx{}, gw{};
-    gx.g.per_block = gw.g.per_block = p.f32 ? PAIRS : 1;
+    gx.g.per_block = gw.g.per_block = p.f32 ? PAIRS : p.rest ? 2 : 1;
     const GemmOperand dz = operand(p.own_dz, p.f32, dy, N, ws + p.off_dz, p.Mp, p.Np);
     if (dx) {
         gx.g.A = dz;
@@ -178,7 +192,8 @@ rnnt_status linear_bwd(const rnnt_linear_desc& d, const LinearPlan& p, const voi
         gx.splits = p.grads.dx.splits;
         gx.per_split = p.grads.dx.per_split;
         gx.slots = (float*)(ws + p.off_slots);
-        gx.e = StoreEpilogue{dx, nullptr, nullptr, K, 0, Bias{}, M, d.K, !p.f32};
+        if (p.rest) take_twice(gx.g.B, gx.g.A, rest, (int)(p.Np / 64));
+        gx.e = StoreEpilogue{dx, nullptr, drop.scale, nullptr, nullptr, K, 0, Bias{}, M, d.K, !p.f32};
     }
     if (dW) {
         gw.g.A = operand(p.copy_x, p.f32, x, K, ws + p.off_x, p.Mp, p.Kp);
@@ -194,9 +209,11 @@ rnnt_status linear_bwd(const rnnt_linear_desc& d, const LinearPlan& p, const voi
         gw.splits = p.grads.dw.splits;
         gw.per_split = p.grads.dw.per_split;
         gw.slots = (float*)(ws + p.off_slots_w);
-        gw.e = StoreEpilogue{dW, d.accumulate_params ? (const float*)dW : nullptr, nullptr, N, 0, Bias{}, K, d.N, (d.param_grads_bf16 & 1) != 0};
+        if (p.rest) take_twice(gw.g.A, gw.g.B, rest, (int)(p.Mp / 64));
+        gw.e = StoreEpilogue{dW, d.accumulate_params ? (const float*)dW : nullptr, drop.scale, nullptr, nullptr, N, 0, Bias{}, K, d.N, (d.param_grads_bf16 & 1) != 0};
     }
-    const SumJob sum{db ? part : nullptr, M, p.Np, d.N, nullptr, 0, d.accumulate_params ? (const float*)db : nullptr, db, (d.param_grads_bf16 & 2) != 0};
+    const SumJob sum{db ? part : nullptr, M, p.Np, d.N, nullptr, 0, d.accumulate_params ? (const float*)db : nullptr, db, (d.param_grads_bf16 & 2) != 0, drop.scale,
+                     nullptr};
     LAYER_HIP(launch_grad_gemms(p.f32, p.grads.tile, gx, gw, sum, stream));
     return RNNT_OK;
 }
@@ -218,6 +235,7 @@ struct CePlan {
     bool f32, grads, copy_w;
     bool few;                             // at most FEW_ROWS rows (fp32: without gradients): scores by one launch on W as it is
     bool identity;                        // ... and without gradients on x as it is
+    long long rest;                       // elements from a chunk's score gradients to their rests (few; 0: none)
     long long cap, chunk, Dp, Vp, pitch;  // rows (a multiple of 256) in all and per chunk; widths up to 64; elements of a chunk row
     int chunks, tile, tile_log2, tiles_n;
     size_t off_count, off_index, off_label, off_weight, off_place, off_x, off_w, off_chunk, off_grad, off_score, off_stats, off_scale, off_part, off_slots,
@@ -241,8 +259,8 @@ CePlan plan_ce_chunk(const rnnt_ce_desc& d, bool grads, long long chunk) {
     p.copy_w = !p.identity && (p.f32 || p.Dp != D || p.Vp != V);
     p.tile = p.few ? FEW_TILE : plan_gemm(p.chunk, V, (int)(p.Dp / 64) * per, 0).tile;
     p.tile_log2 = p.few ? 5 : p.tile == 256 ? 8 : 7;
-    // (few: the columns of zeros up to Vp have parts of their own)
-    p.tiles_n = (int)(((p.few ? p.Vp : V) + p.tile - 1) / p.tile);
+    // (few, on a copy of W: the columns of zeros up to Vp have parts of their own)
+    p.tiles_n = (int)(((p.few && !p.identity ? p.Vp : V) + p.tile - 1) / p.tile);
     Carver c;
     if (p.identity) {
         p.off_score = c.take((size_t)FEW_ROWS * 4);
@@ -266,12 +284,15 @@ CePlan plan_ce_chunk(const rnnt_ce_desc& d, bool grads, long long chunk) {
         p.pitch = up(V, 256) + 64;
         p.off_score = c.take((size_t)p.chunk * 4);
         p.off_stats = c.take((size_t)p.chunk * p.tiles_n * 8);
-        p.off_scale = c.take((size_t)p.chunk * 8);
-        p.off_chunk = p.off_grad = c.take(grads ? (size_t)p.chunk * p.pitch * 2 : 0);
+        p.off_scale = c.take((size_t)p.chunk * 16);
+        p.rest = grads && p.few ? p.chunk * p.pitch : 0;
+        p.off_chunk = p.off_grad = c.take(grads ? (size_t)(p.chunk * p.pitch + p.rest) * 2 : 0);
     }
     if (grads) {
         p.off_part = c.take((size_t)sum_capacity(p.chunk, V) * p.pitch * 4);
-        p.pair = plan_pair(p.chunk, D, (int)(p.Vp / 64) * per, D, V, (int)(p.chunk / 64) * per, SLOT_CAP);
+        // (few: 64 rows, twice)
+        p.pair = p.rest ? plan_pair(FEW_ROWS, D, (int)(p.Vp / 64) * 2, D, V, 2, SLOT_CAP)
+                        : plan_pair(p.chunk, D, (int)(p.Vp / 64) * per, D, V, (int)(p.chunk / 64) * per, SLOT_CAP);
         p.off_slots = c.take(gemm_slot_bytes(p.pair.dx, p.chunk, D));
         p.off_slots_w = c.take(gemm_slot_bytes(p.pair.dw, D, V));
         // the weight gradient's sum over the chunks, where its output is bfloat16
@@ -328,10 +349,10 @@ rnnt_status run_ce(const rnnt_ce_desc& d, const CePlan& p, const void* x, const 
     unsigned char *chunk = ws + p.off_chunk, *grad = ws + p.off_grad;
     float* part = (float*)(ws + p.off_part);
     for (int k = 0; k < p.chunks; ++k) {
-        const long long row0 = (long long)k * p.chunk, n = std::min(p.chunk, p.cap - row0);
+        const long long row0 = (long long)k * p.chunk, n = p.rest ? FEW_ROWS : std::min(p.chunk, p.cap - row0);
         const bool first = k == 0, last = k == p.chunks - 1;
         GemmJob g{};
-        g.A = GemmOperand{ws + p.off_x + (size_t)row0 * p.Dp * 2, p.Dp, p.f32 ? p.cap * p.Dp : 0, nullptr, -1};
+        g.A = GemmOperand{ws + p.off_x + (size_t)row0 * p.Dp * 2, p.Dp, p.f32 ? p.cap * p.Dp : 0, nullptr, -1, 0};
         g.B = w;
         g.M = g.a_rows = n;
         g.N = V;
@@ -343,32 +364,35 @@ rnnt_status run_ce(const rnnt_ce_desc& d, const CePlan& p, const void* x, const 
         g.row0 = row0;
         if (d.R == 0) {
         } else if (p.f32) {
-            const StoreEpilogue e{chunk, nullptr, nullptr, p.pitch, 0, b, n, d.V, false};
+            const StoreEpilogue e{chunk, nullptr, 1.0f, nullptr, nullptr, p.pitch, 0, b, n, d.V, false};
             LAYER_HIP(launch_scores_f32(g, p.tile, e, stream));
             LAYER_HIP(launch_ce_rows_f32(rows, row0, n, (const float*)chunk, p.pitch, d.V, loss, p.grads ? grad : nullptr, stream));
             if (p.grads && db) LAYER_HIP(launch_col_sums_f32(grad, n, p.pitch, d.V, rows.count, row0, part, stream));
         } else {
             const CeEpilogue e{b, d.V, rows.label + row0, (float*)(ws + p.off_score), (float2*)(ws + p.off_stats), p.tiles_n,
                                p.grads ? chunk : nullptr, p.pitch};
-            const CeChunk c{rows, row0, n, e.label_score, e.stats, p.tiles_n, p.tile_log2, d.V, (float2*)(ws + p.off_scale), loss, false, 0};
+            const CeChunk c{rows, row0, n, e.label_score, e.stats, p.tiles_n, p.tile_log2, d.V, (float4*)(ws + p.off_scale), loss, false, 0};
             if (p.few) LAYER_HIP(launch_few_ce(FewJob{g.A.p, w.p, (int)d.R, (int)p.Dp, (int)p.Vp, false}, e, stream));
             else LAYER_HIP(launch_ce_gemm(g, p.tile, e, stream));
             if (!p.grads || !ce_grad_finishes(p.tiles_n)) LAYER_HIP(launch_ce_finish(c, stream));
-            if (p.grads) LAYER_HIP(launch_ce_grad(c, chunk, p.pitch, db ? part : nullptr, stream));
+            if (p.grads) LAYER_HIP(launch_ce_grad(c, chunk, p.pitch, p.rest, db ? part : nullptr, stream));
         }
         if (!p.grads) continue;
-        const GemmOperand dh{grad, p.pitch, p.f32 ? n * p.pitch : 0, nullptr, -1};
+        const GemmOperand dh{grad, p.pitch, p.f32 ? n * p.pitch : 0, nullptr, -1, 0};
+        const float* unit = p.f32 ? nullptr : ce_unit(rows);
         GradGemm gx{}, gw{};
-        gx.g.per_block = gw.g.per_block = g.per_block;
+        const int per = p.rest ? 2 : g.per_block;
         if (d.R > 0) {
             gx.g = g;
             gx.g.A = dh;
             gx.g.N = gx.g.b_rows = D;
-            gx.g.stages = (int)(p.Vp / 64) * g.per_block;
+            gx.g.per_block = per;
+            gx.g.stages = (int)(p.Vp / 64) * per;
+            if (p.rest) take_twice(gx.g.B, gx.g.A, p.rest, (int)(p.Vp / 64));
             gx.splits = p.pair.dx.splits;
             gx.per_split = p.pair.dx.per_split;
             gx.slots = (float*)(ws + p.off_slots);
-            gx.e = StoreEpilogue{dx, nullptr, rows.index + row0, D, 0, Bias{}, n, d.D, !p.f32};
+            gx.e = StoreEpilogue{dx, nullptr, 1.0f, unit, rows.index + row0, D, 0, Bias{}, n, d.D, !p.f32};
         }
         gw.g.A = g.A;
         gw.g.B = dh;
@@ -376,7 +400,9 @@ rnnt_status run_ce(const rnnt_ce_desc& d, const CePlan& p, const void* x, const 
         gw.g.a_rows = p.Dp;
         gw.g.N = V;
         gw.g.b_rows = p.Vp;
-        gw.g.stages = (int)(n / 64) * g.per_block;
+        gw.g.per_block = per;
+        gw.g.stages = (int)(n / 64) * per;
+        if (p.rest) take_twice(gw.g.A, gw.g.B, p.rest, 1);
         gw.g.limit = GEMM_ROWS_K;
         gw.g.count = rows.count;
         gw.g.row0 = row0;
@@ -385,10 +411,10 @@ rnnt_status run_ce(const rnnt_ce_desc& d, const CePlan& p, const void* x, const 
         gw.slots = (float*)(ws + p.off_slots_w);
         const bool w16 = (d.param_grads_bf16 & 1) != 0, b16 = (d.param_grads_bf16 & 2) != 0;
         float* acc = w16 ? (float*)(ws + p.off_acc) : (float*)dW;
-        gw.e = StoreEpilogue{last ? dW : acc, !first || d.accumulate_params ? acc : nullptr, nullptr, V, 0, Bias{}, D, d.V, last && w16};
+        gw.e = StoreEpilogue{last ? dW : acc, !first || d.accumulate_params ? acc : nullptr, 1.0f, unit, nullptr, V, 0, Bias{}, D, d.V, last && w16};
         float* dba = (float*)(ws + p.off_dbacc);
         const SumJob sum{db ? part : nullptr, n, p.pitch, d.V, rows.count, row0, first ? (d.accumulate_params ? (const float*)db : nullptr) : dba,
-                         last ? db : (void*)dba, last && b16};
+                         last ? db : (void*)dba, last && b16, 1.0f, unit};
         LAYER_HIP(launch_grad_gemms(p.f32, p.pair.tile, gx, gw, sum, stream));
     }
     return RNNT_OK;

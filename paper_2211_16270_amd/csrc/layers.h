@@ -40,6 +40,7 @@ struct GemmOperand {
     long long part;
     const void* tail;                    // k-slow operands whose K is no multiple of 64: the last stage's 64 rows, zeros from K on; else null
     int tail_stage;
+    int wrap;                            // bf16: stages from here on are those from 0 on again, `part` elements further; 0: none
 };
 // C[m, n] = sum_k A(m, k) B(k, n); a k-slow operand's extent along the other index is a multiple of 8, a k-contiguous one's K a multiple of 64.
 // limit: a count of rows that only the device knows, n = max(0, min(*count - row0, extent)): it bounds M (GEMM_ROWS_M) or K (GEMM_ROWS_K, the operands
@@ -78,10 +79,12 @@ struct LinearEpilogue {
     long long M;
     int N;
 };
-// out = prev + v as bf16 or float; row r goes to row_map[r] (those < 0 nowhere)
+// out = prev + scale *unit v as bf16 or float; row r goes to row_map[r] (those < 0 nowhere)
 struct StoreEpilogue {
     void* out;
     const float* prev;                   // same pitch, or null
+    float scale;
+    const float* unit;                   // or null: 1
     const int* row_map;                  // or null
     long long ld;
     long long split_stride;              // elements between the results of two splits
@@ -145,6 +148,8 @@ struct SumJob {
     const float* prev;
     void* out;
     bool bf16;
+    float scale;                         // out = prev + scale *unit times the sum
+    const float* unit;                   // or null: 1
 };
 // parts: fp32 products
 hipError_t launch_grad_gemms(bool parts, int tile, const GradGemm& dx, const GradGemm& dw, const SumJob& db, hipStream_t stream);
@@ -182,8 +187,10 @@ inline long long sum_capacity(long long rows, long long cols) {
     const long long few = 2048 / ((cols + 255) / 256) + 2, many = (rows + 127) / 128, most = (rows + 15) / 16;
     return few > many ? (few < most ? few : most) : many;
 }
-// dz = dy act'(z) mask / (1 - p) into dz [rows_to, ld] (zeros beyond [M, N]; null: not stored), column sums of blocks of sum_rows(M, N) rows into part
-// [sum_blocks(M, N), ld] (null: none).  bf16: saved fp16, dz bf16; else dy and saved float, dz as parts.
+// dz = dy act'(z) mask into dz [rows_to, ld] (zeros beyond [M, N]; null: not stored), column sums of blocks of sum_rows(M, N) rows into part
+// [sum_blocks(M, N), ld] (null: none).  bf16: saved fp16, dz bf16; else dy and saved float, dz as parts.  Dropout's 1 / (1 - p) is left to the products'
+// epilogue: without it dz of no activation or of relu is dy or 0, and its rounding to bf16 costs nothing.
+// rest (bf16, elements): what the rounding left goes there behind dz, as bf16 too; 0: nowhere.
 struct DzArgs {
     const void* dy;
     const void* saved;
@@ -194,18 +201,21 @@ struct DzArgs {
     long long ld;
     int act;
     Dropout drop;
+    long long rest;
 };
 hipError_t launch_dz(bool bf16, const DzArgs& a, hipStream_t stream);
-// out[n] = prev[n] + sum of the partial sums
-hipError_t launch_sum_parts(const SumJob& j, hipStream_t stream);
 // ---- cross entropy ---------------------------------------------------------------------------------------------------
 // Rows whose label is not `ignore`, in order: their number, places, labels, weights.  Arrays of `cap` entries (a multiple of 256).
 struct CeRows {
-    int* count;                          // [1]
+    int* count;                          // [1]; behind it the unit of the score gradients (ce_unit), a float
     int* index;                          // -1 behind the last
     int* label;
     float* weight;
 };
+#ifdef __HIPCC__
+__host__ __device__
+#endif
+inline const float* ce_unit(const CeRows& r) { return reinterpret_cast<const float*>(r.count + 1); }
 // x's rows in that order into xp [.., ld] (zeros beyond D and in the rows behind the last up to a multiple of 256; f32: as parts of cap rows); loss and dx
 // (null: no gradients) of the other rows = 0.  place: scratch of R ints for more than GATHER_SCAN rows.
 constexpr long long GATHER_SCAN = 16384;
@@ -218,16 +228,17 @@ struct CeChunk {
     const float* label_score;
     const float2* stats;
     int tiles_n, tile_log2, V;
-    float2* scale;                       // [rows] {maximum, weight / sum}: what turns a kept exponential into weight * probability
+    float4* scale;                       // [rows] {maximum, weight / sum, the label's gradient}: what turns kept exponentials into score gradients
     float* loss;
     bool identity;                       // r.label are the caller's labels, every row is its own place and the ones with `ignore` have loss 0
     int ignore;
 };
 // loss, scale
 hipError_t launch_ce_finish(const CeChunk& c, hipStream_t stream);
-// kept -> score gradients bf16, in place; their column sums (part: null: none).  Does launch_ce_finish's work too where ce_grad_finishes says so.
+// kept -> score gradients over the unit, bf16, in place; their column sums (part: null: none).  Does launch_ce_finish's work too where ce_grad_finishes says so.
 inline bool ce_grad_finishes(int tiles_n) { return tiles_n <= 16; }
-hipError_t launch_ce_grad(const CeChunk& c, void* kept, long long pitch, float* part, hipStream_t stream);
+// rest: as in DzArgs
+hipError_t launch_ce_grad(const CeChunk& c, void* kept, long long pitch, long long rest, float* part, hipStream_t stream);
 // fp32: scores [rows, V] (pitch ld) of a chunk -> loss and, where grad is not null, the score gradients as parts (`rows` rows of pitch ld; zeros behind the
 // last up to a multiple of 64)
 hipError_t launch_ce_rows_f32(const CeRows& r, long long row0, long long rows, const float* scores, long long ld, int V, float* loss, void* grad,

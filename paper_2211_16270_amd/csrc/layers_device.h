@@ -108,6 +108,19 @@ __device__ __forceinline__ void put_parts8(bf16_t* p, long long part, const floa
     *reinterpret_cast<bf16x8*>(p + 3 * part) = l;
 }
 
+// Eight values rounded to bf16 and, where rest is not 0, what that left: bf16 too, at p + rest.  (Nothing is left of an infinity.)
+__device__ __forceinline__ void put_rounded8(bf16_t* p, long long rest, const float (&v)[8]) {
+    bf16x8 h;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) h[j] = (bf16_t)v[j];
+    *reinterpret_cast<bf16x8*>(p) = h;
+    if (rest == 0) return;
+    bf16x8 l;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) l[j] = fabsf((float)h[j]) < -RNNT_NEG_INF ? (bf16_t)(v[j] - (float)h[j]) : (bf16_t)0.0f;
+    *reinterpret_cast<bf16x8*>(p + rest) = l;
+}
+
 // Philox4x32-10 (Salmon, Moraes, Dror, Shaw: Parallel random numbers, as easy as 1, 2, 3; 2011) with key {seed} on the counter {column / 8, row, offset}:
 // the 128 bits of eight columns, 16 for each.
 struct RandomBits8 {
@@ -128,7 +141,7 @@ __device__ __forceinline__ RandomBits8 random_bits8(unsigned long long seed, uns
     }
     return RandomBits8{{c0, c1, c2, c3}};
 }
-// v[j] *= mask / (1 - p), columns n .. n + 7 of row m (n a multiple of 8).  A dropped entry is 0 whatever it was.
+// v[j] *= mask d.scale, columns n .. n + 7 of row m (n a multiple of 8).  A dropped entry is 0 whatever it was.
 __device__ __forceinline__ void drop8(const Dropout& d, long long m, int n, float (&v)[8]) {
     if (d.cut == 0) return;
     const RandomBits8 r = random_bits8(d.state[0], d.state[1], (unsigned)m, (unsigned)n >> 3);
@@ -251,7 +264,8 @@ __device__ __forceinline__ void pass_rng(const LinearEpilogue& e) {
     if (e.rng_used != nullptr && threadIdx.x < 2) e.rng_used[threadIdx.x] = e.drop.state[threadIdx.x];
 }
 __device__ __forceinline__ void pass_rng(const StoreEpilogue&) {}
-// v: columns n .. n + 7 of row m of the product, with the bias.  fetch: what of memory the epilogue needs (sent ahead of the work on v).
+// v: columns n .. n + 7 of row m of the product, with the bias.  fetch: what of memory the epilogue needs (sent ahead of the work on v); factor: what is the
+// same for all of a product.
 struct LinearStore {
     typedef bf16x8 Extra;
     __device__ static __forceinline__ Extra fetch(const LinearEpilogue& e, long long m, int n) {
@@ -259,7 +273,8 @@ struct LinearStore {
         if (e.residual != nullptr && m < e.M && n < e.N) r = take8((const bf16_t*)e.residual + (size_t)m * e.N + n, e.N - n);
         return r;
     }
-    __device__ static __forceinline__ void store(const LinearEpilogue& e, long long m, int n, float (&v)[8], const Extra& r, int = 0) {
+    __device__ static __forceinline__ float factor(const LinearEpilogue&) { return 1.0f; }
+    __device__ static __forceinline__ void store(const LinearEpilogue& e, long long m, int n, float (&v)[8], const Extra& r, float = 1.0f, int = 0) {
         if (m >= e.M || n >= e.N) return;
         const size_t at = (size_t)m * e.N + n;
         if (e.saved != nullptr) put8((_Float16*)e.saved + at, e.N - n, saved8(e.act, v));
@@ -279,7 +294,8 @@ struct LinearStore32 {
         if (e.residual != nullptr && m < e.M && n < e.N) load8((const float*)e.residual + (size_t)m * e.N + n, e.N - n, r);
         return f32x8{r[0], r[1], r[2], r[3], r[4], r[5], r[6], r[7]};
     }
-    __device__ static __forceinline__ void store(const LinearEpilogue& e, long long m, int n, float (&v)[8], const Extra& r, int = 0) {
+    __device__ static __forceinline__ float factor(const LinearEpilogue&) { return 1.0f; }
+    __device__ static __forceinline__ void store(const LinearEpilogue& e, long long m, int n, float (&v)[8], const Extra& r, float = 1.0f, int = 0) {
         if (m >= e.M || n >= e.N) return;
         const size_t at = (size_t)m * e.N + n;
         if (e.saved != nullptr) store8((float*)e.saved + at, e.N - n, v);
@@ -296,10 +312,13 @@ struct PlainStore {
     __device__ static __forceinline__ Extra fetch(const StoreEpilogue& e, long long m, int n) {
         return m >= e.M || n >= e.N ? -1 : e.row_map != nullptr ? (long long)e.row_map[m] : m;
     }
-    __device__ static __forceinline__ void store(const StoreEpilogue& e, long long, int n, float (&v)[8], const Extra& x, int split = 0) {
+    __device__ static __forceinline__ float factor(const StoreEpilogue& e) { return e.unit != nullptr ? e.scale * *e.unit : e.scale; }
+    __device__ static __forceinline__ void store(const StoreEpilogue& e, long long, int n, float (&v)[8], const Extra& x, float factor, int split = 0) {
         if (x < 0) return;
         const size_t at = (size_t)split * e.split_stride + (size_t)x * e.ld + n;
         const int live = e.N - n;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= factor;
         if (e.prev != nullptr) {
             float p[8];
             load8(e.prev + at, live, p);
@@ -338,9 +357,11 @@ __device__ __forceinline__ void sum_parts(const SumJob& j, int blocks, int R, in
     red[row][c] = s;
     __syncthreads();
     if (row == 0 && n < j.N) {
-        float t = j.prev != nullptr ? j.prev[n] : 0.0f;
+        float t = 0.0f;
 #pragma unroll
         for (int r = 0; r < 8; ++r) t += red[r][c];
+        t *= j.unit != nullptr ? j.scale * *j.unit : j.scale;
+        if (j.prev != nullptr) t += j.prev[n];
         if (j.bf16) ((bf16_t*)j.out)[n] = (bf16_t)t;
         else ((float*)j.out)[n] = t;
     }
