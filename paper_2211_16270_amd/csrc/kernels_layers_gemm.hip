@@ -48,24 +48,29 @@ __device__ __forceinline__ void gemm_workgroup(const GemmJob& g, const E& e, int
     static_assert(TS::NT == 2 && TS::WAVES * TURN32_BYTES <= TS::SMEM, "a wave's 64 columns");
     typedef typename EpilogueOf<E>::type Store;
     const float factor = Store::factor(e);
-#pragma unroll
-    for (int i = 0; i < TS::MT; ++i) {
-        typename Store::Extra x[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] = Store::fetch(e, m0 + (wm * TS::MT + i) * 32 + 8 * k + (lane >> 3), n);
-        turn32_put(area, 0, acc[i][0], lane);
-        turn32_put(area, 1, acc[i][1], lane);
-        turn_fence();
+    // One loop over the pieces of eight rows; what four of them need of memory is sent for at once (one at a time, three ahead: a residual took 20 us of 16000 x
+    // 1024 x 4096, now 10: a wait for such a load is one for the stores in front of it too).
+    const long long first = m0 + wm * TS::MT * 32 + (lane >> 3);
+    typename Store::Extra mem[4];
 #pragma unroll 1
-        for (int k = 0; k < 4; ++k) {
-            const long long m = m0 + (wm * TS::MT + i) * 32 + 8 * k + (lane >> 3);
-            float v[8];
-            turn32_take(area, k, lane, v);
-            // (a register array indexed by the loop's counter would lie in memory)
-            const typename Store::Extra r = k & 2 ? (k & 1 ? x[3] : x[2]) : (k & 1 ? x[1] : x[0]);
-            Store::store(e, m, n, v, r, factor, t.split);
+    for (int k = 0; k < 4 * TS::MT; ++k) {
+        if (k % 4 == 0) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) mem[q] = Store::fetch(e, first + 8 * (k + q), n);
+            turn_fence();
+            static_for<0, TS::MT>([&](auto i) {
+                if (k / 4 == decltype(i)::value) {
+                    turn32_put(area, 0, acc[decltype(i)::value][0], lane);
+                    turn32_put(area, 1, acc[decltype(i)::value][1], lane);
+                }
+            });
+            turn_fence();
         }
-        turn_fence();
+        float v[8];
+        turn32_take(area, k % 4, lane, v);
+        // (a register array indexed by the loop's counter would lie in memory)
+        const typename Store::Extra r = k & 2 ? (k & 1 ? mem[3] : mem[2]) : (k & 1 ? mem[1] : mem[0]);
+        Store::store(e, first + 8 * k, n, v, r, factor, t.split);
     }
 }
 

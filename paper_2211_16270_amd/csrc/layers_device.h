@@ -25,6 +25,12 @@ struct Vec8<_Float16> {
     typedef f16x8 type;
     typedef f16x8_any any;
 };
+// Eight floats rounded to 16 bits each, nearest and even (as a vector: two to an instruction)
+template <typename T>
+__device__ __forceinline__ typename Vec8<T>::type round8(const float (&v)[8]) {
+    const f32x8 x = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
+    return __builtin_convertvector(x, typename Vec8<T>::type);
+}
 // The first `live` of eight consecutive values, zeros for the others
 template <typename T>
 __device__ __forceinline__ void load8(const T* p, int live, float (&v)[8]) {
@@ -50,10 +56,7 @@ template <typename T>
 __device__ __forceinline__ void store8(T* p, int live, const float (&v)[8]) {
     if (live >= 8) {
         if constexpr (sizeof(T) == 2) {
-            typename Vec8<T>::type x;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = (T)v[j];
-            *reinterpret_cast<typename Vec8<T>::any*>(p) = x;
+            *reinterpret_cast<typename Vec8<T>::any*>(p) = round8<T>(v);
         } else {
             *reinterpret_cast<f32x4_at4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
             *reinterpret_cast<f32x4_at4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
@@ -110,22 +113,21 @@ __device__ __forceinline__ void put_parts8(bf16_t* p, long long part, const floa
 
 // Eight values rounded to bf16 and, where rest is not 0, what that left: bf16 too, at p + rest.  (Nothing is left of an infinity.)
 __device__ __forceinline__ void put_rounded8(bf16_t* p, long long rest, const float (&v)[8]) {
-    bf16x8 h;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) h[j] = (bf16_t)v[j];
+    const bf16x8 h = round8<bf16_t>(v);
     *reinterpret_cast<bf16x8*>(p) = h;
     if (rest == 0) return;
-    bf16x8 l;
+    float l[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) l[j] = fabsf((float)h[j]) < -RNNT_NEG_INF ? (bf16_t)(v[j] - (float)h[j]) : (bf16_t)0.0f;
-    *reinterpret_cast<bf16x8*>(p + rest) = l;
+    for (int j = 0; j < 8; ++j) l[j] = fabsf((float)h[j]) < -RNNT_NEG_INF ? v[j] - (float)h[j] : 0.0f;
+    *reinterpret_cast<bf16x8*>(p + rest) = round8<bf16_t>(l);
 }
 
 // Philox4x32-10 (Salmon, Moraes, Dror, Shaw: Parallel random numbers, as easy as 1, 2, 3; 2011) with key {seed} on the counter {column / 8, row, offset}:
 // the 128 bits of eight columns, 16 for each.
 struct RandomBits8 {
     unsigned w[4];
-    __device__ __forceinline__ unsigned of(int j) const { return (j & 1) ? w[j >> 1] >> 16 : w[j >> 1] & 0xffffu; }
+    // entry j's bits in the upper half
+    __device__ __forceinline__ unsigned of(int j) const { return (j & 1) ? w[j >> 1] : w[j >> 1] << 16; }
 };
 __device__ __forceinline__ RandomBits8 random_bits8(unsigned long long seed, unsigned long long offset, unsigned row, unsigned group) {
     unsigned c0 = group, c1 = row, c2 = (unsigned)offset, c3 = (unsigned)(offset >> 32), k0 = (unsigned)seed, k1 = (unsigned)(seed >> 32);
@@ -146,7 +148,7 @@ __device__ __forceinline__ void drop8(const Dropout& d, long long m, int n, floa
     if (d.cut == 0) return;
     const RandomBits8 r = random_bits8(d.state[0], d.state[1], (unsigned)m, (unsigned)n >> 3);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = r.of(j) >= d.cut ? v[j] * d.scale : 0.0f;
+    for (int j = 0; j < 8; ++j) v[j] = r.of(j) >= d.cut << 16 ? v[j] * d.scale : 0.0f;
 }
 
 // FAST: by the exponential and reciprocal instructions (relative error about 1e-6, results that are rounded to bf16); else the math library's functions.
@@ -203,7 +205,9 @@ __device__ __forceinline__ void act8(int act, float (&v)[8]) {
         default: break;
     }
 }
-// g[j] *= act'(z[j]); z finite or NaN
+// A z of +-65504 at most: act' there is its limit, and it times 0 is 0.
+__device__ __forceinline__ float bounded(float z) { return __builtin_amdgcn_fmed3f(z, -65504.0f, 65504.0f); }
+// g[j] *= act'(z[j]).  NaN where z is (by the functions of z that are not bounded).
 template <bool FAST>
 __device__ __forceinline__ void act_grad8(int act, const float (&z)[8], float (&g)[8]) {
     switch (act) {
@@ -215,7 +219,7 @@ __device__ __forceinline__ void act_grad8(int act, const float (&z)[8], float (&
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float p = sigmoid<FAST>(z[j]), q = sigmoid<FAST>(-z[j]);     // (1 - p would lose it where p is near 1)
-                g[j] *= p * fmaf(z[j], q, 1.0f);
+                g[j] *= p * fmaf(bounded(z[j]), q, 1.0f);
             }
             break;
         case ACT_GELU:
@@ -223,7 +227,7 @@ __device__ __forceinline__ void act_grad8(int act, const float (&z)[8], float (&
             for (int j = 0; j < 8; ++j) {
                 float bell;
                 const float q = normal_tail<FAST>(z[j], bell);
-                g[j] *= fmaf(z[j] * 0.3989422804014327f, bell, z[j] > 0.0f ? 1.0f - q : q);
+                g[j] *= fmaf(bounded(z[j]) * 0.3989422804014327f, bell, z[j] > 0.0f ? 1.0f - q : q);
             }
             break;
         case ACT_TANH:
@@ -237,21 +241,14 @@ __device__ __forceinline__ void act_grad8(int act, const float (&z)[8], float (&
     }
 }
 
-// A saved pre-activation: fp16 (11 bits, where bf16's eight would add as much to the gradient's error as its own rounding does), beyond the largest
-// one that largest one (there act' has its limit).  relu's derivative is its sign: a nonzero one stays nonzero.
+// A saved pre-activation: fp16 (11 bits, where bf16's eight would add as much to the gradient's error as its own rounding does), beyond its range infinity.
+// relu's derivative is its sign: z times 2^127, of which even the smallest nonzero one stays nonzero.
 __device__ __forceinline__ f16x8 saved8(int act, const float (&z)[8]) {
-    f16x8 s;
+    const float up = act == ACT_RELU ? 0x1p127f : 1.0f;
+    float s[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float c = __builtin_amdgcn_fmed3f(z[j], -65504.0f, 65504.0f);
-        s[j] = (_Float16)(z[j] == z[j] ? c : z[j]);
-    }
-    if (act == ACT_RELU) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (s[j] == (_Float16)0.0f && z[j] != 0.0f) s[j] = z[j] > 0.0f ? (_Float16)5.9604644775390625e-8f : (_Float16)-5.9604644775390625e-8f;
-    }
-    return s;
+    for (int j = 0; j < 8; ++j) s[j] = z[j] * up;
+    return round8<_Float16>(s);
 }
 
 // ---- what becomes of columns n .. n + 7 (n a multiple of 8) of row m of a product --------------------------------------
@@ -280,10 +277,9 @@ struct LinearStore {
         if (e.saved != nullptr) put8((_Float16*)e.saved + at, e.N - n, saved8(e.act, v));
         act8<true>(e.act, v);
         drop8(e.drop, m, n, v);
-        bf16x8 y;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = (bf16_t)(v[j] + (float)r[j]);
-        put8((bf16_t*)e.y + at, e.N - n, y);
+        for (int j = 0; j < 8; ++j) v[j] += (float)r[j];
+        put8((bf16_t*)e.y + at, e.N - n, round8<bf16_t>(v));
     }
     __device__ static __forceinline__ void bias(const LinearEpilogue& e, int n, float (&b)[8]) { load_bias8(e.bias, n < e.N ? n : e.N - 1, e.N, b); }
 };
