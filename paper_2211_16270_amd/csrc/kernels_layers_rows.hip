@@ -11,13 +11,26 @@ namespace {
 inline unsigned blocks_of(long long n, long long per) { return (unsigned)((n + per - 1) / per); }
 inline bool grid_fits(long long n) { return n <= 0x7fffffffLL; }
 
-// One thread per eight values
-__global__ __launch_bounds__(256) void k_layer_pads(PadJobs jobs, unsigned first1, unsigned first2) {
-    const int k = blockIdx.x >= first2 ? 2 : blockIdx.x >= first1 ? 1 : 0;
-    const PadJob& j = jobs.job[k];
-    const unsigned first = k == 2 ? first2 : k == 1 ? first1 : 0, wgs = (k == 0 ? first1 : k == 1 ? first2 : gridDim.x) - first;
+// Padded copies, one thread per eight values: the workgroups of job k are [end[k - 1], end[k]) of those a launch has for them.
+struct PadLaunch {
+    PadJobs jobs;
+    unsigned end[3];
+};
+PadLaunch pad_launch(const PadJobs& j) {
+    PadLaunch p{j, {}};
+    unsigned n = 0;
+    for (int k = 0; k < 3; ++k) {
+        if (k < j.n) n += (unsigned)std::min<long long>((j.job[k].rows_to * (j.job[k].ld_to / 8) + 255) / 256, 8192);
+        p.end[k] = n;
+    }
+    return p;
+}
+__device__ __forceinline__ void pad_workgroup(const PadLaunch& p, unsigned block) {
+    const int k = block >= p.end[1] ? 2 : block >= p.end[0] ? 1 : 0;
+    const PadJob& j = p.jobs.job[k];
+    const unsigned first = k == 2 ? p.end[1] : k == 1 ? p.end[0] : 0, wgs = p.end[k] - first;
     const long long groups = j.ld_to / 8, total = j.rows_to * groups;
-    for (long long i = (long long)(blockIdx.x - first) * 256 + threadIdx.x; i < total; i += (long long)wgs * 256) {
+    for (long long i = (long long)(block - first) * 256 + threadIdx.x; i < total; i += (long long)wgs * 256) {
         const long long r = i / groups, c = (i - r * groups) * 8;
         const long long left = j.r0 + r < j.rows ? j.cols - c : 0;
         const int live = left < 0 ? 0 : left < 8 ? (int)left : 8;
@@ -32,6 +45,7 @@ __global__ __launch_bounds__(256) void k_layer_pads(PadJobs jobs, unsigned first
         }
     }
 }
+__global__ __launch_bounds__(256) void k_layer_pads(PadLaunch p) { pad_workgroup(p, blockIdx.x); }
 
 // The sums of 32 column granules over the eight thread rows of a workgroup -> part[n]
 __device__ __forceinline__ void fold_columns(float (&sum)[8], float (*red)[256], float* __restrict__ part, int n, int N, int tid) {
@@ -45,11 +59,13 @@ __device__ __forceinline__ void fold_columns(float (&sum)[8], float (*red)[256],
     if (n + tid < N) part[n + tid] = t;
 }
 
-// dz = dy act'(z) mask: a workgroup takes R rows x 256 columns, 8 thread rows x 32 granules of 8 columns.
+// dz = dy act'(z) mask: a workgroup takes R rows x 256 columns, 8 thread rows x 32 granules of 8 columns.  The workgroups from dz_wgs on make the products'
+// padded copies (a launch less: 1531 x 443 x 777, 4 us of 47).
 template <typename T, typename S>
-__global__ __launch_bounds__(256) void k_layer_dz(DzArgs a, int R) {
+__global__ __launch_bounds__(256) void k_layer_dz(DzArgs a, int R, int dz_wgs, PadLaunch pads) {
     constexpr bool FAST = sizeof(T) == 2;
     __shared__ __align__(16) float red[8][256];
+    if ((int)blockIdx.x >= dz_wgs) return pad_workgroup(pads, blockIdx.x - dz_wgs);
     const int nb = (int)((a.ld + 255) / 256), rb = blockIdx.x / nb;
     const int tid = threadIdx.x, n0 = (blockIdx.x - rb * nb) * 256, n = n0 + (tid & 31) * 8;
     const long long r0 = (long long)rb * R;
@@ -165,15 +181,18 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_ce_rows(const int* __restrict_
     }
 }
 
-// A workgroup takes 16 rows of x, a wavefront four: their copies, or loss = 0 and dx = 0.  The workgroups behind those fill what lies behind the last row.
+// A workgroup takes 16 rows of x, a wavefront four: their copies, or loss = 0 and dx = 0.  The FILL_WGS behind those fill what lies behind the last row; those
+// behind them make W's padded copy.
 // SCAN: a workgroup counts the real rows before its own itself (the labels come from the L2), which saves a launch; else k_ce_rows has left `place`.
-constexpr int GATHER_ROWS = 16;
+constexpr int GATHER_ROWS = 16, FILL_WGS = 16;
 typedef int i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 // T: bf16, or float, whose rows go to xp as parts of cap rows.
 template <typename T, bool SCAN>
 __global__ __launch_bounds__(256) void k_ce_gather(const T* __restrict__ x, long long R, int D, const int* __restrict__ labels,
                                                    const float* __restrict__ weight, int ignore, long long cap, const int* __restrict__ place, CeRows r,
-                                                   bf16_t* __restrict__ xp, long long ld, float* __restrict__ loss, T* __restrict__ dx, int row_wgs) {
+                                                   bf16_t* __restrict__ xp, long long ld, float* __restrict__ loss, T* __restrict__ dx, int row_wgs,
+                                                   PadLaunch pads) {
+    if ((int)blockIdx.x >= row_wgs + FILL_WGS) return pad_workgroup(pads, blockIdx.x - row_wgs - FILL_WGS);
     __shared__ int wave_count[4], at_row[GATHER_ROWS];
     __shared__ float wave_most[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -236,7 +255,8 @@ __global__ __launch_bounds__(256) void k_ce_gather(const T* __restrict__ x, long
         return;
     }
     // zeros behind the last row up to the next multiple of 256
-    const int wg = blockIdx.x - row_wgs, wgs = gridDim.x - row_wgs;
+    constexpr int wgs = FILL_WGS;
+    const int wg = blockIdx.x - row_wgs;
     const long long end = (n + 255) / 256 * 256;
     for (long long at = n + wg * 4 + wave; at < end; at += wgs * 4)
         for (int c = lane * 8; c < ld; c += 512)
@@ -514,47 +534,47 @@ hipError_t launch_scale(const float* factor, void* const (&p)[3], const long lon
 }
 
 hipError_t launch_pads(const PadJobs& j, hipStream_t stream) {
-    unsigned wgs[3] = {};
-    for (int k = 0; k < j.n; ++k) wgs[k] = (unsigned)std::min<long long>((j.job[k].rows_to * (j.job[k].ld_to / 8) + 255) / 256, 8192);
-    const unsigned total = wgs[0] + wgs[1] + wgs[2];
-    if (total == 0) return hipSuccess;
-    k_layer_pads<<<dim3(total), dim3(256), 0, stream>>>(j, wgs[0], wgs[0] + wgs[1]);
+    const PadLaunch p = pad_launch(j);
+    if (p.end[2] == 0) return hipSuccess;
+    k_layer_pads<<<dim3(p.end[2]), dim3(256), 0, stream>>>(p);
     return hipGetLastError();
 }
 
-hipError_t launch_dz(bool bf16, const DzArgs& a, hipStream_t stream) {
+hipError_t launch_dz(bool bf16, const DzArgs& a, const PadJobs& pads, hipStream_t stream) {
     const int R = sum_rows(a.M, a.N);
+    const PadLaunch p = pad_launch(pads);
     const long long n = (std::max(a.M, a.rows_to) + R - 1) / R * ((a.ld + 255) / 256);
-    if (!grid_fits(n)) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)n);
-    if (bf16) k_layer_dz<bf16_t, _Float16><<<grid, dim3(256), 0, stream>>>(a, R);
-    else k_layer_dz<float, float><<<grid, dim3(256), 0, stream>>>(a, R);
+    if (!grid_fits(n + p.end[2])) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)n + p.end[2]);
+    if (bf16) k_layer_dz<bf16_t, _Float16><<<grid, dim3(256), 0, stream>>>(a, R, (int)n, p);
+    else k_layer_dz<float, float><<<grid, dim3(256), 0, stream>>>(a, R, (int)n, p);
     return hipGetLastError();
 }
 
 namespace {
 template <typename T>
 hipError_t gather(const void* x, long long R, int D, const int* labels, const float* weight, int ignore, long long cap, int* place, const CeRows& r, void* xp,
-                  long long ld, float* loss, void* dx, hipStream_t stream) {
+                  long long ld, float* loss, void* dx, const PadJobs& pads, hipStream_t stream) {
     const unsigned row_wgs = blocks_of(R, GATHER_ROWS);
-    const dim3 grid(row_wgs + 16);
+    const PadLaunch p = pad_launch(pads);
+    const dim3 grid(row_wgs + FILL_WGS + p.end[2]);
     if (R <= GATHER_SCAN) {
         k_ce_gather<T, true><<<grid, dim3(256), 0, stream>>>((const T*)x, R, D, labels, weight, ignore, cap, nullptr, r, (bf16_t*)xp, ld, loss, (T*)dx,
-                                                             (int)row_wgs);
+                                                             (int)row_wgs, p);
     } else {
         k_ce_rows<<<dim3(blocks_of(R, SCAN_ROWS)), dim3(SCAN_THREADS), 0, stream>>>(labels, weight, R, ignore, cap, place, r);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         k_ce_gather<T, false><<<grid, dim3(256), 0, stream>>>((const T*)x, R, D, labels, weight, ignore, cap, place, r, (bf16_t*)xp, ld, loss, (T*)dx,
-                                                              (int)row_wgs);
+                                                              (int)row_wgs, p);
     }
     return hipGetLastError();
 }
 }  // namespace
 hipError_t launch_ce_gather(const void* x, bool f32, long long R, int D, const int* labels, const float* weight, int ignore, long long cap, int* place,
-                            const CeRows& r, void* xp, long long ld, float* loss, void* dx, hipStream_t stream) {
-    return f32 ? gather<float>(x, R, D, labels, weight, ignore, cap, place, r, xp, ld, loss, dx, stream)
-               : gather<bf16_t>(x, R, D, labels, weight, ignore, cap, place, r, xp, ld, loss, dx, stream);
+                            const CeRows& r, void* xp, long long ld, float* loss, void* dx, const PadJobs& pads, hipStream_t stream) {
+    return f32 ? gather<float>(x, R, D, labels, weight, ignore, cap, place, r, xp, ld, loss, dx, pads, stream)
+               : gather<bf16_t>(x, R, D, labels, weight, ignore, cap, place, r, xp, ld, loss, dx, pads, stream);
 }
 hipError_t launch_ce_finish(const CeChunk& c, hipStream_t stream) {
     k_ce_finish<<<dim3(blocks_of(c.rows, 4)), dim3(256), 0, stream>>>(c);

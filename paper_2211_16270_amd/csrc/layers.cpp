@@ -168,18 +168,17 @@ rnnt_status linear_bwd(const rnnt_linear_desc& d, const LinearPlan& p, const voi
     mask.scale = 1.0f;
     const long long rest = p.rest ? p.Mp * p.Np : 0;
     if (M == 0) dx = nullptr;
-    if (M > 0 && (db || (p.own_dz && (dx || dW)))) {
-        const DzArgs a{dy, d.activation == ACT_NONE ? nullptr : saved, p.own_dz && (dx || dW) ? ws + p.off_dz : nullptr, db ? part : nullptr, M,
-                       p.own_dz ? p.Mp : M, d.N, p.Np, d.activation, mask, rest};
-        LAYER_HIP(launch_dz(!p.f32, a, stream));
-    }
     const int kind = p.f32 ? PAD_PARTS : PAD_16;
     PadJobs pads{};
     if (dx && p.copy_w) pads.add(kind, W, K, N, 0, ws + p.off_w, K, p.Np);
     if (dW && p.copy_x) pads.add(kind, x, M, K, 0, ws + p.off_x, p.Mp, p.Kp);
     else if (dW && ragged) pads.add(PAD_16, x, M, K, whole, ws + p.off_xt, 64, K);
     if (dW && !p.own_dz && ragged) pads.add(PAD_16, dy, M, N, whole, ws + p.off_dyt, 64, N);
-    LAYER_HIP(launch_pads(pads, stream));
+    if (M > 0 && (db || (p.own_dz && (dx || dW)))) {
+        const DzArgs a{dy, d.activation == ACT_NONE ? nullptr : saved, p.own_dz && (dx || dW) ? ws + p.off_dz : nullptr, db ? part : nullptr, M,
+                       p.own_dz ? p.Mp : M, d.N, p.Np, d.activation, mask, rest};
+        LAYER_HIP(launch_dz(!p.f32, a, pads, stream));
+    } else LAYER_HIP(launch_pads(pads, stream));
     GradGemm gx{}, gw{};
     gx.g.per_block = gw.g.per_block = p.f32 ? PAIRS : p.rest ? 2 : 1;
     const GemmOperand dz = operand(p.own_dz, p.f32, dy, N, ws + p.off_dz, p.Mp, p.Np);
@@ -339,12 +338,12 @@ rnnt_status run_ce(const rnnt_ce_desc& d, const CePlan& p, const void* x, const 
     const CeRows rows{(int*)(ws + p.off_count), (int*)(ws + p.off_index), (int*)(ws + p.off_label), (float*)(ws + p.off_weight)};
     const int kind = p.f32 ? PAD_PARTS : PAD_16;
     PadJobs pads{};
+    if (d.R == 0) pads.add(PAD_32, nullptr, 0, 0, 0, rows.count, 1, 8);       // (the gradients of an empty sum; the part behind is 256 bytes away)
+    if (p.copy_w) pads.add(kind, W, D, V, 0, ws + p.off_w, p.Dp, p.Vp);
     if (d.R > 0)
         LAYER_HIP(launch_ce_gather(x, p.f32, d.R, d.D, label, row_weight, d.ignore_label, p.cap, (int*)(ws + p.off_place), rows, ws + p.off_x, p.Dp, loss,
-                                   p.grads ? dx : nullptr, stream));
-    else pads.add(PAD_32, nullptr, 0, 0, 0, rows.count, 1, 8);       // (no rows: the gradients of an empty sum; the part behind is 256 bytes away)
-    if (p.copy_w) pads.add(kind, W, D, V, 0, ws + p.off_w, p.Dp, p.Vp);
-    LAYER_HIP(launch_pads(pads, stream));
+                                   p.grads ? dx : nullptr, pads, stream));
+    else LAYER_HIP(launch_pads(pads, stream));
     const GemmOperand w = operand(p.copy_w, p.f32, W, V, ws + p.off_w, p.Dp, p.Vp);
     unsigned char *chunk = ws + p.off_chunk, *grad = ws + p.off_grad;
     float* part = (float*)(ws + p.off_part);

@@ -156,7 +156,7 @@ hipError_t launch_grad_gemms(bool parts, int tile, const GradGemm& dx, const Gra
 
 // ---- passes over memory --------------------------------------------------------------------------------------------
 // dst[rows_to, ld_to] = src[rows, cols] (dense) from row r0 on, zeros elsewhere, ld_to a multiple of 8: a copy of 16-bit values, of 32-bit ones, or of floats as
-// parts.  Up to three in one launch.
+// parts.  Up to three in a launch of their own or behind another kernel's work (`pads` there).
 enum PadKind { PAD_NONE = 0, PAD_16, PAD_32, PAD_PARTS };
 struct PadJob {
     int kind;
@@ -203,7 +203,7 @@ struct DzArgs {
     Dropout drop;
     long long rest;
 };
-hipError_t launch_dz(bool bf16, const DzArgs& a, hipStream_t stream);
+hipError_t launch_dz(bool bf16, const DzArgs& a, const PadJobs& pads, hipStream_t stream);
 // ---- cross entropy ---------------------------------------------------------------------------------------------------
 // Rows whose label is not `ignore`, in order: their number, places, labels, weights.  Arrays of `cap` entries (a multiple of 256).
 struct CeRows {
@@ -220,7 +220,7 @@ inline const float* ce_unit(const CeRows& r) { return reinterpret_cast<const flo
 // (null: no gradients) of the other rows = 0.  place: scratch of R ints for more than GATHER_SCAN rows.
 constexpr long long GATHER_SCAN = 16384;
 hipError_t launch_ce_gather(const void* x, bool f32, long long R, int D, const int* labels, const float* weight, int ignore, long long cap, int* place,
-                            const CeRows& r, void* xp, long long ld, float* loss, void* dx, hipStream_t stream);
+                            const CeRows& r, void* xp, long long ld, float* loss, void* dx, const PadJobs& pads, hipStream_t stream);
 // Rows [row0, row0 + rows) of that order and the statistics of their scores, tiles_n parts of 2^tile_log2 columns each (arrays: of the chunk)
 struct CeChunk {
     CeRows r;
