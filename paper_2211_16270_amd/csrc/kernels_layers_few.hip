@@ -70,7 +70,7 @@ struct FewCe {
 // The eight waves' sums -> the epilogue, or this split's slot
 template <int MT, class E>
 __device__ __forceinline__ void few_finish(const FewJob& j, const E& e, const f32x4 (&acc)[MT][2], unsigned char* smem, float* __restrict__ slots, int block,
-                                           int n0) {
+                                           int m0, int n0) {
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     __syncthreads();
     // register r of lane l: column 4 (l / 16) + r of its 16, row l % 16
@@ -82,11 +82,11 @@ __device__ __forceinline__ void few_finish(const FewJob& j, const E& e, const f3
             *reinterpret_cast<f32x4*>(part + ((wave * MT + i) * 16 + (lane & 15)) * FC + c * 16 + 4 * (lane >> 4)) = acc[i][c];
     __syncthreads();
     if (tid < MT * 64) {
-        const int m = tid >> 2, g = tid & 3;
+        const int in = tid >> 2, m = m0 + in, g = tid & 3;
         f32x4 p = f32x4{0}, q = f32x4{0};
 #pragma unroll
         for (int k = 0; k < FW; ++k) {
-            const float* s = part + ((size_t)k * MT * 16 + m) * FC + g * 8;
+            const float* s = part + ((size_t)k * MT * 16 + in) * FC + g * 8;
             p += *reinterpret_cast<const f32x4*>(s);
             q += *reinterpret_cast<const f32x4*>(s + 4);
         }
@@ -105,15 +105,15 @@ __device__ __forceinline__ void few_finish(const FewJob& j, const E& e, const f3
 // lines of W: they go to one XCD.  What bounds it: latency (one token, K = 640, N = 2560: the launch, two trips to memory, the reduction).
 // WHOLE: K and N are multiples of 32, no piece has an end in it (the code for ends, eight loads under eight conditions for each load, takes longer to fetch
 // than to run).
-// A long sum is split over workgroups too (gridDim.y > 1), whose results go to slots [split][M][N up to 8]: 64 rows, K = 2560, N = 640 19.8 us in 20
-// workgroups, half of it x, which each of them reads whole.
+// Rows in several workgroups: gridDim.z.  A long sum is split over workgroups too (gridDim.y > 1), whose results go to slots [split][M][N up to 8].
 template <int MT, bool WHOLE, class E>
 __global__ __launch_bounds__(64 * FW) void k_few_rows(FewJob j, E e, int blocks, float* __restrict__ slots, int per_split) {
     __shared__ __align__(16) unsigned char smem[FW * MT * 16 * FC * 4];
     static_assert(MT * 16 * FC * 4 >= 2048, "a step of W per wave");
     const int per = (blocks + 7) >> 3, block = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
     if ((int)(blockIdx.x >> 3) >= per || block >= blocks) return;
-    if (block == 0 && slots == nullptr) e.first();
+    const int m0 = blockIdx.z * MT * 16;
+    if (block == 0 && m0 == 0 && slots == nullptr) e.first();
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n0 = block * FC;
     const int K = j.K, N = j.N;
     unsigned char* area = smem + wave * 2048;
@@ -123,7 +123,7 @@ __global__ __launch_bounds__(64 * FW) void k_few_rows(FewJob j, E e, int blocks,
     bool row_ok[MT];
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-        const int row = 16 * i + (lane & 15);
+        const int row = m0 + 16 * i + (lane & 15);
         row_ok[i] = row < j.M;
         x[i] = (const bf16_t*)j.x + (size_t)(row_ok[i] ? row : 0) * K;
     }
@@ -185,7 +185,7 @@ __global__ __launch_bounds__(64 * FW) void k_few_rows(FewJob j, E e, int blocks,
                 if (t + FW * (q + FD) < steps) fetch(s, 32 * (t + FW * (q + FD)));
             }
         });
-    few_finish<MT>(j, e, acc, smem, slots, block, n0);
+    few_finish<MT>(j, e, acc, smem, slots, block, m0, n0);
 }
 
 // The same in fp32 on the fp32 matrix instruction (16 x 16 x 4), which takes its operands as they lie: a wave's step of 32 along k is eight of them, the
@@ -195,7 +195,8 @@ __global__ __launch_bounds__(64 * FW) void k_few_rows_f32(FewJob j, E e, int blo
     __shared__ __align__(16) unsigned char smem[FW * MT * 16 * FC * 4];
     const int per = (blocks + 7) >> 3, block = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
     if ((int)(blockIdx.x >> 3) >= per || block >= blocks) return;
-    if (block == 0 && slots == nullptr) e.first();
+    const int m0 = blockIdx.z * MT * 16;
+    if (block == 0 && m0 == 0 && slots == nullptr) e.first();
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n0 = block * FC, g = lane >> 4, l16 = lane & 15;
     const int K = j.K, N = j.N;
     const float* W = (const float*)j.W;
@@ -203,7 +204,7 @@ __global__ __launch_bounds__(64 * FW) void k_few_rows_f32(FewJob j, E e, int blo
     bool row_ok[MT];
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-        const int row = 16 * i + l16;
+        const int row = m0 + 16 * i + l16;
         row_ok[i] = row < j.M;
         x[i] = (const float*)j.x + (size_t)(row_ok[i] ? row : 0) * K;
     }
@@ -251,14 +252,23 @@ __global__ __launch_bounds__(64 * FW) void k_few_rows_f32(FewJob j, E e, int blo
                 if (t + FW * (q + D) < steps) fetch(s, 32 * (t + FW * (q + D)));
             }
         });
-    few_finish<MT>(j, e, acc, smem, slots, block, n0);
+    few_finish<MT>(j, e, acc, smem, slots, block, m0, n0);
 }
 
+// Blocks of 16 rows per workgroup: as few as leave a workgroup per compute unit at most.  A wave's loads of x are what takes long, and W comes from the L2 for
+// all but the first (64 rows, K = 640, N = 2560: 5.4 us, 7.3 with all rows in one workgroup; K = 2560, N = 640 7.0 and 10.3).
+int few_blocks(int M, int N) {
+    const int columns = (N + FC - 1) / FC, all = (M + 15) / 16;
+    int mt = 1;
+    while (mt < 4 && mt < all && columns * ((all + mt - 1) / mt) > 256) mt *= 2;
+    return mt;
+}
 template <bool F32, class E>
 hipError_t launch_few(const FewJob& j, const E& e, int splits, float* slots, hipStream_t stream) {
     if (j.M <= 0 || j.M > FEW_ROWS) return j.M <= 0 ? hipSuccess : hipErrorInvalidValue;
     const int blocks = (j.N + FC - 1) / FC, per = ((j.K + 31) / 32 + splits - 1) / splits;
-    const dim3 grid((unsigned)((blocks + 7) / 8 * 8), (unsigned)splits);
+    const int mt = few_blocks(j.M, j.N);
+    const dim3 grid((unsigned)((blocks + 7) / 8 * 8), (unsigned)splits, (unsigned)((j.M + 16 * mt - 1) / (16 * mt)));
     const bool whole = j.K % 32 == 0 && j.N % FC == 0;
     auto go = [&](auto mt) {
         constexpr int MT = decltype(mt)::value;
@@ -269,15 +279,18 @@ hipError_t launch_few(const FewJob& j, const E& e, int splits, float* slots, hip
         else k_few_rows<MT, false, E><<<grid, dim3(64 * FW), 0, stream>>>(j, e, blocks, slots, per);
         return hipGetLastError();
     };
-    return j.M <= 16 ? go(std::integral_constant<int, 1>{}) : j.M <= 32 ? go(std::integral_constant<int, 2>{}) : go(std::integral_constant<int, 4>{});
+    return mt == 1 ? go(std::integral_constant<int, 1>{}) : mt == 2 ? go(std::integral_constant<int, 2>{}) : go(std::integral_constant<int, 4>{});
 }
 
 }  // namespace
 
-// More than four steps per wave are shared by as many workgroups as fill the chip, each with a step per wave at least.
-int few_splits(long long M, int K, int N) {
-    const int steps = (K + 31) / 32, blocks = (N + FC - 1) / FC;
-    if (M > FEW_ROWS || steps <= 4 * FW) return 1;
+// Long sums are shared by as many workgroups as fill the chip, each with a step per wave at least: in fp32, whose steps take sixteen loads of W each, from five
+// steps per wave on (1 row, K = 2560, N = 640: 7.2 us, 14.4 in one workgroup per 32 columns), in bf16 from seventeen (with ten 6.6 us, 5.7 so: the second
+// launch takes what the split saves).
+int few_splits(bool f32, long long M, int K, int N) {
+    if (M < 1 || M > FEW_ROWS) return 1;
+    const int steps = (K + 31) / 32, mt = few_blocks((int)M, N), blocks = (N + FC - 1) / FC * (((int)M + 16 * mt - 1) / (16 * mt));
+    if (steps <= (f32 ? 4 : 16) * FW) return 1;
     const int most = std::min(steps / FW, std::max(1, 256 / blocks)), per = (steps + most - 1) / most;
     return (steps + per - 1) / per;
 }

@@ -91,7 +91,7 @@ LinearPlan plan_linear(const rnnt_linear_desc& d, bool backward) {
     p.Mp = up(M, 64);
     if (!backward && M <= FEW_ROWS) {
         p.few = true;
-        p.few_splits = few_splits(M, d.K, d.N);
+        p.few_splits = few_splits(p.f32, M, d.K, d.N);
         p.off_slots = c.take(p.few_splits > 1 ? (size_t)p.few_splits * M * up(N, 8) * 4 : 0);
     } else if (!backward) {
         p.copy_x = p.f32 || K % 64 != 0;

@@ -121,7 +121,7 @@ struct FewJob {
     int M, K, N;
     bool f32;                            // (results of the fp32 matrix instruction)
 };
-int few_splits(long long M, int K, int N);
+int few_splits(bool f32, long long M, int K, int N);
 hipError_t launch_few_linear(const FewJob& j, int splits, float* slots, const LinearEpilogue& e, hipStream_t stream);
 // the epilogue on the sum of slots [splits][M][N up to 8]
 hipError_t launch_linear_reduce(bool f32, long long M, int N, int splits, const float* slots, const LinearEpilogue& e, hipStream_t stream);
