@@ -55,9 +55,10 @@ typedef struct {
  * rng      dev [2]      {seed, offset}, read by the kernels when they run (a replayed graph takes what is there then); NULL allowed with p = 0
  * rng_used dev [2]      out, or NULL: the seed and offset this call took (for its backward pass, where the caller advances rng meanwhile)
  * y        dev [M, N]   desc->dtype, out
- * saved    dev [M, N]   out, or NULL: z for the backward pass, two bytes per entry with RNNT_BF16 (fp16), four with RNNT_F32.  The backward
- *                       pass of RNNT_ACT_NONE does without.
- * RNNT_BF16: the product runs on bf16 MFMA with fp32 accumulation, everything behind it in fp32, one rounding at the end.
+ * saved    dev [M, N]   out, or NULL: what the backward pass needs of z, two bytes per entry with RNNT_BF16 (z in fp16; RNNT_ACT_RELU: its sign), four with
+ *                       RNNT_F32.  The backward pass of RNNT_ACT_NONE does without.
+ * RNNT_BF16: the product runs on bf16 MFMA with fp32 accumulation, everything behind it in fp32, one rounding at the end.  RNNT_F32: every value as three
+ * bf16 parts, six products of them (as exact as fp32 ones); up to 64 rows on the fp32 MFMA.
  * workspace_bytes >= rnnt_linear_workspace_bytes(desc, 0); with 0 bytes workspace may be NULL.
  */
 size_t rnnt_linear_workspace_bytes(const rnnt_linear_desc* desc, int32_t backward);
@@ -67,7 +68,7 @@ rnnt_status rnnt_linear_fwd(const rnnt_linear_desc* desc, const void* x, const v
 /*
  * Gradients for an incoming dy = d/dy: with dz = dy act'(z) m / (1 - p)
  *   dx = dz W^T,  dW = x^T dz,  db = column sums of dz   (and dy itself is the residual's)
- * RNNT_BF16: dz is rounded to bfloat16 as the operand of both products (db: before that rounding).
+ * RNNT_BF16: dy act'(z) m is rounded to bfloat16 as the operand of both products, in two values of it up to 64 rows (db: before that rounding).
  *
  * x, W, rng as in the forward call, with the same values; saved: what it left (NULL allowed with RNNT_ACT_NONE)
  * dy dev [M, N] desc->dtype;  dx dev [M, K] desc->dtype, out;  dW dev [K, N], db dev [N], out.  Each of dx, dW, db may be NULL: not wanted.
@@ -104,7 +105,8 @@ typedef struct {
  *                        of the vocabulary is possible (all scores -inf: its gradient is that of the label alone)
  * dx         dev [R, D]  desc->dtype, out; zeros in padding rows
  * dW dev [D, V], db dev [V] (NULL: not wanted), out
- * RNNT_BF16: the three products run on bf16 MFMA with fp32 accumulation, the softmax in fp32; dh is rounded to bfloat16 as their operand.
+ * RNNT_BF16: the three products run on bf16 MFMA with fp32 accumulation, the softmax in fp32; dh is rounded to bfloat16 as their operand,
+ * relative to the mantissa of the largest weight, in two values of it up to 64 rows.  The label's entry comes from the loss: exact also where p is near 1.
  *
  * workspace bytes: grads = 0 for rnnt_ce_loss_fwd, 1 for rnnt_ce_loss_fwd_bwd.  budget_bytes = 0: the library's default (chunk buffers of at most
  * 1 GiB); otherwise chunks as large as fit the budget, and if even the smallest (256 rows) exceed it, their size.  A workspace larger than that of the

@@ -1,5 +1,5 @@
 """torch.autograd front end of the C-ABI library (argument marshalling only: every number comes out of
-rnnt_joint_loss_fwd_bwd_weighted).
+the library's calls).
 
     loss = rnnt_joint_loss(enc, pred, W_out, b_out, labels, T_len, U_len, blank=0)     # [B], -ln P(y_b|x_b)
     loss.sum().backward()        # or loss.mean(), (loss * mask).sum(), ...
@@ -12,6 +12,12 @@ weights, and otherwise calls the library once more with the incoming gradient as
 `sample_weight` (e.g. 1/B for a mean) to make the first call the only one.  The weights of the library are
 non-negative, so the gradient that reaches the loss vector must be >= 0 for every sample (backward raises
 otherwise).  The forward call's outputs and workspace stay alive until backward has run.
+
+    y = rnnt_linear(x, W, b, activation="silu", residual=None, dropout=0.1, rng_state=state)      # the encoders' layers
+    loss = rnnt_ce_loss(x, W_out, b_out, labels, row_weight=w)                                    # cross entropy of the same output layer
+
+Steps of these can be captured into a graph (torch.cuda.graph) as whole forward and backward passes.  Torch's own condition holds: no eager graph of the same
+leaves may be alive then (delete the warm-up's outputs and losses before the capture), as its gradient accumulators belong to another stream.
 """
 from __future__ import annotations
 
@@ -124,7 +130,7 @@ class _RnntCeSum(torch.autograd.Function):
         if any(ctx.needs_input_grad[:3]):
             out = _ce_grads(x, W, b, labels, row_weight, ignore_label, budget_bytes)
             ctx.save_for_backward(x, W, b, labels, row_weight)
-            ctx.grads, ctx.opts = out, (ignore_label, budget_bytes)
+            ctx.grads, ctx.opts, ctx.captured = out, (ignore_label, budget_bytes), torch.cuda.is_current_stream_capturing()
         else:
             out = Bd.run_ce_fwd(x, W, b, labels, ignore_label, budget_bytes=budget_bytes)
         return Bd.run_ce_total(out["loss"], row_weight)
@@ -134,8 +140,9 @@ class _RnntCeSum(torch.autograd.Function):
     def backward(ctx, g):
         x, W, b, labels, row_weight = ctx.saved_tensors
         g = g.float().contiguous()
-        if ctx.grads is not None:
-            # the forward call's gradients are handed out, times g in place; a second backward pass of the same graph computes them again
+        if ctx.grads is not None and ctx.captured == torch.cuda.is_current_stream_capturing():
+            # the forward call's gradients are handed out, times g in place; a second backward pass of the same graph computes them again, and so does one
+            # that is captured without its forward call, as each replay would scale them once more
             out, ctx.grads = ctx.grads, None
             Bd.run_ce_scale(g, out["dx"], out["dW"], out["db"])
         else:

@@ -107,16 +107,47 @@ __global__ __launch_bounds__(256) void k_layer_dz(DzArgs a, int R, int dz_wgs, P
 __device__ __forceinline__ float unit_of(float largest) {
     return largest > 0.0f && largest < -RNNT_NEG_INF ? __uint_as_float((__float_as_uint(largest) & 0x007fffffu) | 0x3f800000u) : 1.0f;
 }
-// Each workgroup counts the real rows before its own SCAN_ROWS (the labels come from the L2) and numbers its own.
-constexpr int SCAN_THREADS = 1024, SCAN_PER = 4, SCAN_ROWS = SCAN_THREADS * SCAN_PER;
+// A workgroup numbers the real rows of its SCAN_ROWS behind those of the workgroups before it, which k_ce_count has counted (with their largest weight).
+constexpr int SCAN_THREADS = 1024, SCAN_PER = CE_SCAN_ROWS / SCAN_THREADS;
+__global__ __launch_bounds__(SCAN_THREADS) void k_ce_count(const int* __restrict__ labels, const float* __restrict__ weight, long long R, int ignore,
+                                                           int2* __restrict__ counts) {
+    __shared__ int wave_sum[SCAN_THREADS / 64];
+    __shared__ float wave_most[SCAN_THREADS / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const long long first = (long long)blockIdx.x * CE_SCAN_ROWS;
+    int n = 0;
+    float most = 0.0f;
+#pragma unroll
+    for (int k = 0; k < SCAN_PER; ++k) {
+        const long long i = first + k * SCAN_THREADS + tid;
+        if (i >= R || labels[i] == ignore) continue;
+        ++n;
+        most = fmaxf(most, weight != nullptr ? fabsf(weight[i]) : 1.0f);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+    most = wave_max(most);
+    if (lane == 0) {
+        wave_sum[wave] = n;
+        wave_most[wave] = most;
+    }
+    __syncthreads();
+    if (tid == 0) {
+        for (int w = 1; w < SCAN_THREADS / 64; ++w) {
+            n += wave_sum[w];
+            most = fmaxf(most, wave_most[w]);
+        }
+        counts[blockIdx.x] = make_int2(n, __float_as_int(most));
+    }
+}
 __global__ __launch_bounds__(SCAN_THREADS) void k_ce_rows(const int* __restrict__ labels, const float* __restrict__ weight, long long R, int ignore,
-                                                          long long cap, int* __restrict__ place, CeRows r) {
+                                                          long long cap, const int2* __restrict__ counts, int* __restrict__ place, CeRows r) {
     __shared__ int wave_sum[SCAN_THREADS / 64], wave_before[SCAN_THREADS / 64];
     __shared__ float wave_most[SCAN_THREADS / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const long long first = (long long)blockIdx.x * SCAN_ROWS;
+    const long long first = (long long)blockIdx.x * CE_SCAN_ROWS;
     int before = 0;
-    for (long long i = tid; i < first; i += SCAN_THREADS) before += labels[i] != ignore;
+    for (unsigned i = tid; i < blockIdx.x; i += SCAN_THREADS) before += counts[i].x;
     int y[SCAN_PER], mine = 0;
 #pragma unroll
     for (int k = 0; k < SCAN_PER; ++k) {
@@ -157,13 +188,8 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_ce_rows(const int* __restrict_
         }
     }
     if (blockIdx.x == gridDim.x - 1) {
-        float most = weight != nullptr ? 0.0f : 1.0f;
-        if (weight != nullptr)
-#pragma unroll 8
-            for (long long i = tid; i < R; i += SCAN_THREADS) {
-                const float w = weight[i];
-                most = labels[i] != ignore ? fmaxf(most, fabsf(w)) : most;
-            }
+        float most = 0.0f;
+        for (unsigned i = tid; i < gridDim.x; i += SCAN_THREADS) most = fmaxf(most, __int_as_float(counts[i].y));
         most = wave_max(most);
         if (lane == 0) wave_most[wave] = most;
         __syncthreads();
@@ -183,7 +209,7 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_ce_rows(const int* __restrict_
 
 // A workgroup takes 16 rows of x, a wavefront four: their copies, or loss = 0 and dx = 0.  The FILL_WGS behind those fill what lies behind the last row; those
 // behind them make W's padded copy.
-// SCAN: a workgroup counts the real rows before its own itself (the labels come from the L2), which saves a launch; else k_ce_rows has left `place`.
+// SCAN: a workgroup counts the real rows before its own itself (the labels come from the L2), which saves two launches; else k_ce_rows has left `place`.
 constexpr int GATHER_ROWS = 16, FILL_WGS = 16;
 typedef int i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 // T: bf16, or float, whose rows go to xp as parts of cap rows.
@@ -491,6 +517,7 @@ __global__ __launch_bounds__(1024) void k_ce_total(const float* __restrict__ los
     }
 }
 
+// (bf16 gradients are rounded once more, where the factor is no power of two: the alternative is computing them again)
 struct ScaleArgs {
     void* p[3];
     long long n[3];
@@ -562,8 +589,12 @@ hipError_t gather(const void* x, long long R, int D, const int* labels, const fl
         k_ce_gather<T, true><<<grid, dim3(256), 0, stream>>>((const T*)x, R, D, labels, weight, ignore, cap, nullptr, r, (bf16_t*)xp, ld, loss, (T*)dx,
                                                              (int)row_wgs, p);
     } else {
-        k_ce_rows<<<dim3(blocks_of(R, SCAN_ROWS)), dim3(SCAN_THREADS), 0, stream>>>(labels, weight, R, ignore, cap, place, r);
-        const hipError_t e = hipGetLastError();
+        int2* counts = reinterpret_cast<int2*>(place + cap);
+        k_ce_count<<<dim3(blocks_of(R, CE_SCAN_ROWS)), dim3(SCAN_THREADS), 0, stream>>>(labels, weight, R, ignore, counts);
+        hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        k_ce_rows<<<dim3(blocks_of(R, CE_SCAN_ROWS)), dim3(SCAN_THREADS), 0, stream>>>(labels, weight, R, ignore, cap, counts, place, r);
+        e = hipGetLastError();
         if (e != hipSuccess) return e;
         k_ce_gather<T, false><<<grid, dim3(256), 0, stream>>>((const T*)x, R, D, labels, weight, ignore, cap, place, r, (bf16_t*)xp, ld, loss, (T*)dx,
                                                               (int)row_wgs, p);

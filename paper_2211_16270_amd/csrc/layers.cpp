@@ -127,7 +127,8 @@ GemmOperand operand(bool copied, bool f32, const void* own, long long ld, const 
 
 // A bf16 product with an operand in two values: `once` by the rounded ones, then by the rest.
 // Rounding the gradient to bf16 adds as much to the products' error as their own rounding does, sqrt(2) times it where many values average; the few of a few
-// rows do not (up to 3 times).  There, up to FEW_ROWS rows, the products wait for W and dW rather than for their operations.
+// rows do not (up to 3 times).  There, up to FEW_ROWS rows, the products wait for W and dW rather than for their operations (backward pass of 64 x 512 x 2048
+// 14.3 us with dz in one value, 16.8 in two; 64 x 1024 x 4096 21.7 and 25.4).
 void take_twice(GemmOperand& once, GemmOperand& two, long long rest, int stages) {
     once.wrap = two.wrap = stages;
     two.part = rest;
@@ -271,7 +272,7 @@ CePlan plan_ce_chunk(const rnnt_ce_desc& d, bool grads, long long chunk) {
     p.off_index = c.take((size_t)p.cap * 4);
     p.off_label = c.take((size_t)p.cap * 4);
     p.off_weight = c.take((size_t)p.cap * 4);
-    p.off_place = c.take(R > GATHER_SCAN ? (size_t)p.cap * 4 : 0);
+    p.off_place = c.take(R > GATHER_SCAN ? (size_t)ce_place_ints(p.cap) * 4 : 0);
     p.off_x = c.take((size_t)p.cap * p.Dp * e);
     p.off_w = c.take(p.copy_w ? (size_t)p.Dp * p.Vp * e : 0);
     if (p.f32) {

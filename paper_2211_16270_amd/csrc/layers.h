@@ -217,8 +217,9 @@ __host__ __device__
 #endif
 inline const float* ce_unit(const CeRows& r) { return reinterpret_cast<const float*>(r.count + 1); }
 // x's rows in that order into xp [.., ld] (zeros beyond D and in the rows behind the last up to a multiple of 256; f32: as parts of cap rows); loss and dx
-// (null: no gradients) of the other rows = 0.  place: scratch of R ints for more than GATHER_SCAN rows.
-constexpr long long GATHER_SCAN = 16384;
+// (null: no gradients) of the other rows = 0.  place: scratch of ce_place_ints(cap) ints for more than GATHER_SCAN rows.
+constexpr long long GATHER_SCAN = 16384, CE_SCAN_ROWS = 4096;
+inline long long ce_place_ints(long long cap) { return cap + 2 * ((cap + CE_SCAN_ROWS - 1) / CE_SCAN_ROWS); }
 hipError_t launch_ce_gather(const void* x, bool f32, long long R, int D, const int* labels, const float* weight, int ignore, long long cap, int* place,
                             const CeRows& r, void* xp, long long ld, float* loss, void* dx, const PadJobs& pads, hipStream_t stream);
 // Rows [row0, row0 + rows) of that order and the statistics of their scores, tiles_n parts of 2^tile_log2 columns each (arrays: of the chunk)

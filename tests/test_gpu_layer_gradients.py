@@ -150,7 +150,7 @@ def test_a_linear_layer_reads_nothing_of_its_workspace_that_it_did_not_write(M, 
 
 
 @pytest.mark.parametrize("R,D,V,pad", [(1, 64, 710, 0), (11, 64, 710, 1), (64, 63, 65, 9), (33, 128, 96, 33), (90, 70, 130, 50), (300, 64, 4100, 280),
-                                       (17000, 8, 40, 16990)])
+                                       (17000, 8, 40, 16990), (70001, 8, 24, 30000)])
 @pytest.mark.parametrize("bf16", [True, False])
 def test_the_cross_entropy_reads_nothing_of_its_workspace_that_it_did_not_write(R, D, V, pad, bf16):
     torch = _torch()
@@ -169,3 +169,30 @@ def test_the_cross_entropy_reads_nothing_of_its_workspace_that_it_did_not_write(
             assert torch.equal(u, v), kind
     ref = O.cross_entropy(i["x"], i["W"], i["b"], i["labels"], i["weight"])
     assert np.all(np.abs(_np(results["nan"][0]) - ref["loss"]) <= 2e-5 * (1 + np.abs(ref["loss"])))
+
+
+def test_a_captured_backward_pass_of_an_eager_forward_call_scales_once():
+    torch = _torch()
+    from paper_2211_16270_amd import autograd as A
+    i = _ce_inputs(90, 64, 128, True, 9, seed=8)
+    lab = _dev(i["labels"], torch.int32)
+    g = torch.full((), 0.25, device="cuda:0")
+
+    def leaves():
+        return [_dev(i[k], torch.bfloat16).requires_grad_() for k in ("x", "W")]
+
+    x, W = leaves()
+    ref = torch.autograd.grad(A.rnnt_ce_loss(x, W, None, lab), (x, W), g)
+    x, W = leaves()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        loss = A.rnnt_ce_loss(x, W, None, lab)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            got = torch.autograd.grad(loss, (x, W), g)
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        for u, v in zip(got, ref):
+            assert torch.equal(u, v)
