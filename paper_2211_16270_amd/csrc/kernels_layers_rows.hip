@@ -360,7 +360,7 @@ __global__ __launch_bounds__(256) void k_ce_finish(CeChunk c) {
     }
 }
 
-// A workgroup takes R rows x 256 columns.  FINISH: it also forms its rows' sums (those of the first columns write the losses).
+// A workgroup takes R rows x 256 columns.  FINISH: it also forms its rows' sums, 256 / R threads for each (those of the first columns write the losses).
 template <bool FINISH>
 __global__ __launch_bounds__(256) void k_ce_grad(CeChunk c, void* __restrict__ kept, long long pitch, long long rest, float* __restrict__ part, int R) {
     __shared__ __align__(16) float red[8][256];
@@ -373,20 +373,25 @@ __global__ __launch_bounds__(256) void k_ce_grad(CeChunk c, void* __restrict__ k
     // rows up to the next multiple of 64 are read by the weight gradient's product: zeros there
     const long long real_rows = (long long)*r.count - row0, live = (real_rows + 63) / 64 * 64;
     if (r0 >= live || real_rows <= 0) return;
-    if (tid < R) {
-        float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (r0 + tid < real_rows) {
-            if constexpr (FINISH) {
-                const float2* st = c.stats + (size_t)(r0 + tid) * c.tiles_n;
-                float M = RNNT_NEG_INF, S = 0.0f;
-                for (int t = 0; t < c.tiles_n; ++t) M = fmaxf(M, st[t].x);
-                const float z = M == RNNT_NEG_INF ? 0.0f : M;
-                for (int t = 0; t < c.tiles_n; ++t) S += st[t].y * __builtin_amdgcn_exp2f((st[t].x - z) * LOG2E_F);
-                f = ce_finish_row(c, r0 + tid, n0 == 0 ? r.index[row0 + r0 + tid] : -1, M, S);
-            } else f = c.scale[r0 + tid];
-        }
-        scale[tid] = f;
-    }
+    if constexpr (FINISH) {
+        const int per = 256 / R, in = tid / per, sub = tid & (per - 1);           // (R: a power of two from 16 to 128)
+        const bool real = r0 + in < real_rows;
+        const float2* st = c.stats + (size_t)(real ? r0 + in : 0) * c.tiles_n;
+        // FINISH_LOADS of them at most, kept for the second pass
+        float2 s[FINISH_LOADS];
+        float M = RNNT_NEG_INF, S = 0.0f;
+#pragma unroll
+        for (int k = 0; k < FINISH_LOADS; ++k) s[k] = sub + k * per < c.tiles_n ? st[sub + k * per] : make_float2(RNNT_NEG_INF, 0.0f);
+#pragma unroll
+        for (int k = 0; k < FINISH_LOADS; ++k) M = fmaxf(M, s[k].x);
+        for (int o = per >> 1; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
+        const float z = M == RNNT_NEG_INF ? 0.0f : M;
+#pragma unroll
+        for (int k = 0; k < FINISH_LOADS; ++k) S += s[k].y * __builtin_amdgcn_exp2f((s[k].x - z) * LOG2E_F);
+        for (int o = per >> 1; o > 0; o >>= 1) S += __shfl_xor(S, o, 64);
+        if (sub == 0)
+            scale[in] = real ? ce_finish_row(c, r0 + in, n0 == 0 ? r.index[row0 + r0 + in] : -1, M, S) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    } else if (tid < R) scale[tid] = r0 + tid < real_rows ? c.scale[r0 + tid] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     __syncthreads();
     float sum[8] = {};
     const int t = n >> c.tile_log2;
@@ -501,10 +506,19 @@ __global__ __launch_bounds__(256) void k_layer_col_sums_f32(const bf16_t* __rest
 __global__ __launch_bounds__(1024) void k_ce_total(const float* __restrict__ loss, const float* __restrict__ weight, long long R, float* __restrict__ total) {
     __shared__ double part[16];
     double s = 0.0;
-#pragma unroll 8
-    for (long long i = threadIdx.x; i < R; i += 1024) {
+    // (both loads whatever the weight is: behind a branch they would follow each other)
+    long long i = threadIdx.x * 4;
+#pragma unroll 4
+    for (; i + 4 <= R; i += 4096) {
+        const f32x4_at4 l = *reinterpret_cast<const f32x4_at4*>(loss + i);
+        f32x4 w = f32x4{1.0f, 1.0f, 1.0f, 1.0f};
+        if (weight != nullptr) w = *reinterpret_cast<const f32x4_at4*>(weight + i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s += w[j] != 0.0f ? (double)w[j] * (double)l[j] : 0.0;
+    }
+    for (; i < R; ++i) {                                           // (one thread's last three at most)
         const float w = weight != nullptr ? weight[i] : 1.0f;
-        if (w != 0.0f) s += (double)w * (double)loss[i];
+        s += w != 0.0f ? (double)w * (double)loss[i] : 0.0;
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
@@ -615,7 +629,7 @@ hipError_t launch_ce_grad(const CeChunk& c, void* kept, long long pitch, long lo
     const int R = sum_rows(c.rows, c.V);
     const long long n = (long long)blocks_of(c.V, 256) * sum_blocks(c.rows, c.V);
     if (!grid_fits(n)) return hipErrorInvalidValue;
-    if (ce_grad_finishes(c.tiles_n)) k_ce_grad<true><<<dim3((unsigned)n), dim3(256), 0, stream>>>(c, kept, pitch, rest, part, R);
+    if (ce_grad_finishes(c.rows, c.V, c.tiles_n)) k_ce_grad<true><<<dim3((unsigned)n), dim3(256), 0, stream>>>(c, kept, pitch, rest, part, R);
     else k_ce_grad<false><<<dim3((unsigned)n), dim3(256), 0, stream>>>(c, kept, pitch, rest, part, R);
     return hipGetLastError();
 }

@@ -374,7 +374,7 @@ rnnt_status run_ce(const rnnt_ce_desc& d, const CePlan& p, const void* x, const 
             const CeChunk c{rows, row0, n, e.label_score, e.stats, p.tiles_n, p.tile_log2, d.V, (float4*)(ws + p.off_scale), loss, false, 0};
             if (p.few) LAYER_HIP(launch_few_ce(FewJob{g.A.p, w.p, (int)d.R, (int)p.Dp, (int)p.Vp, false}, e, stream));
             else LAYER_HIP(launch_ce_gemm(g, p.tile, e, stream));
-            if (!p.grads || !ce_grad_finishes(p.tiles_n)) LAYER_HIP(launch_ce_finish(c, stream));
+            if (!p.grads || !ce_grad_finishes(n, V, p.tiles_n)) LAYER_HIP(launch_ce_finish(c, stream));
             if (p.grads) LAYER_HIP(launch_ce_grad(c, chunk, p.pitch, p.rest, db ? part : nullptr, stream));
         }
         if (!p.grads) continue;

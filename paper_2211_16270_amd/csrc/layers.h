@@ -237,7 +237,10 @@ struct CeChunk {
 // loss, scale
 hipError_t launch_ce_finish(const CeChunk& c, hipStream_t stream);
 // kept -> score gradients over the unit, bf16, in place; their column sums (part: null: none).  Does launch_ce_finish's work too where ce_grad_finishes says so.
-inline bool ce_grad_finishes(int tiles_n) { return tiles_n <= 16; }
+// FINISH_LOADS parts for each of the 256 / R threads of a row at most: every column block does it again (777 x 443 x 5001, 40 parts: a launch of 4 us less; 128 parts with
+// R = 128 would be 64 loads a thread in 128 column blocks).
+constexpr int FINISH_LOADS = 8;
+inline bool ce_grad_finishes(long long rows, long long V, int tiles_n) { return (long long)tiles_n * sum_rows(rows, V) <= FINISH_LOADS * 256; }
 // rest: as in DzArgs
 hipError_t launch_ce_grad(const CeChunk& c, void* kept, long long pitch, long long rest, float* part, hipStream_t stream);
 // fp32: scores [rows, V] (pitch ld) of a chunk -> loss and, where grad is not null, the score gradients as parts (`rows` rows of pitch ld; zeros behind the
