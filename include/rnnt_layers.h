@@ -3,7 +3,7 @@
  * and dtypes): what the encoders in front of the joint network are made of, and the other loss of its output layer.
  *
  *   rnnt_linear_*    y = residual + dropout(act(x W + b)) and its gradients.  The dropout mask is a function of a seed, an offset and an entry's
- *                    place and is never stored.
+ *                    place, not an array of its own.
  *   rnnt_ce_loss_*   cross entropy of softmax(x W + b) with one label per row, and its gradients, without the [R, V] scores.
  *
  * Conventions beyond those of rnnt_joint_loss.h: every array is dense; device pointers are 16-byte aligned (RNNT_ERR_UNSUPPORTED otherwise),
@@ -56,7 +56,7 @@ typedef struct {
  * rng_used dev [2]      out, or NULL: the seed and offset this call took (for its backward pass, where the caller advances rng meanwhile)
  * y        dev [M, N]   desc->dtype, out
  * saved    dev [M, N]   out, or NULL: what the backward pass needs of z, two bytes per entry with RNNT_BF16 (z in fp16; RNNT_ACT_RELU: its sign), four with
- *                       RNNT_F32.  The backward pass of RNNT_ACT_NONE does without.
+ *                       RNNT_F32; -infinity in dropped entries.  The backward pass of RNNT_ACT_NONE does without.
  * RNNT_BF16: the product runs on bf16 MFMA with fp32 accumulation, everything behind it in fp32, one rounding at the end.  RNNT_F32: every value as three
  * bf16 parts, six products of them (as exact as fp32 ones); up to 64 rows on the fp32 MFMA.
  * workspace_bytes >= rnnt_linear_workspace_bytes(desc, 0); with 0 bytes workspace may be NULL.

@@ -83,8 +83,15 @@ __global__ __launch_bounds__(256) void k_layer_dz(DzArgs a, int R, int dz_wgs, P
                 float z[8];
                 load8((const S*)a.saved + at, live, z);
                 act_grad8<FAST>(a.act, z, v);
+                // (a dropped entry, see saved8; one that was -infinity by itself has act' = 0)
+                if (a.drop.cut != 0)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] = z[j] == RNNT_NEG_INF ? 0.0f : v[j];
+            } else if (a.drop.cut != 0) {
+                bool keep[8];
+                keep8(a.drop, m, n, keep);
+                drop8(a.drop, keep, v);
             }
-            drop8(a.drop, m, n, v);
             if (live < 8)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = j < live ? v[j] : 0.0f;

@@ -143,12 +143,16 @@ __device__ __forceinline__ RandomBits8 random_bits8(unsigned long long seed, uns
     }
     return RandomBits8{{c0, c1, c2, c3}};
 }
-// v[j] *= mask d.scale, columns n .. n + 7 of row m (n a multiple of 8).  A dropped entry is 0 whatever it was.
-__device__ __forceinline__ void drop8(const Dropout& d, long long m, int n, float (&v)[8]) {
-    if (d.cut == 0) return;
+// Which of columns n .. n + 7 of row m (n a multiple of 8) are kept (d.cut not 0)
+__device__ __forceinline__ void keep8(const Dropout& d, long long m, int n, bool (&keep)[8]) {
     const RandomBits8 r = random_bits8(d.state[0], d.state[1], (unsigned)m, (unsigned)n >> 3);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = r.of(j) >= d.cut << 16 ? v[j] * d.scale : 0.0f;
+    for (int j = 0; j < 8; ++j) keep[j] = r.of(j) >= d.cut << 16;
+}
+// v[j] *= mask d.scale.  A dropped entry is 0 whatever it was.
+__device__ __forceinline__ void drop8(const Dropout& d, const bool (&keep)[8], float (&v)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = keep[j] ? v[j] * d.scale : 0.0f;
 }
 
 // FAST: by the exponential and reciprocal instructions (relative error about 1e-6, results that are rounded to bf16); else the math library's functions.
@@ -156,6 +160,14 @@ template <bool FAST>
 __device__ __forceinline__ float sigmoid(float x) {
     if constexpr (FAST) return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-LOG2E_F * x));
     else return 1.0f / (1.0f + expf(-x));
+}
+// p, q = sigmoid(+-x), both to their own precision, by one exponential and one reciprocal
+template <bool FAST>
+__device__ __forceinline__ void sigmoids(float x, float& p, float& q) {
+    const float e = FAST ? __builtin_amdgcn_exp2f(-LOG2E_F * fabsf(x)) : expf(-fabsf(x));
+    const float most = FAST ? __builtin_amdgcn_rcpf(1.0f + e) : 1.0f / (1.0f + e), least = e * most;
+    p = x > 0.0f ? most : least;
+    q = x > 0.0f ? least : most;
 }
 // Phi(-|x|), the normal distribution's tail, and e^{-x^2/2}.  FAST: erfc(z) = t Q(t) e^{-z^2} with t = 1 / (1 + 0.375 z) and a polynomial Q of degree 6
 // fitted to it for the smallest relative error over z < 9.3 (6.5e-7; in fp32 2e-6 for |x| < 5, 9e-6 where the tail leaves fp32's range): one reciprocal,
@@ -218,7 +230,8 @@ __device__ __forceinline__ void act_grad8(int act, const float (&z)[8], float (&
         case ACT_SILU:
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float p = sigmoid<FAST>(z[j]), q = sigmoid<FAST>(-z[j]);     // (1 - p would lose it where p is near 1)
+                float p, q;
+                sigmoids<FAST>(z[j], p, q);
                 g[j] *= p * fmaf(bounded(z[j]), q, 1.0f);
             }
             break;
@@ -233,8 +246,9 @@ __device__ __forceinline__ void act_grad8(int act, const float (&z)[8], float (&
         case ACT_TANH:
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                // 1 - tanh^2 = 4 p q with p, q = sigmoid(+-2z)
-                g[j] *= 4.0f * sigmoid<FAST>(2.0f * z[j]) * sigmoid<FAST>(-2.0f * z[j]);
+                float p, q;
+                sigmoids<FAST>(2.0f * z[j], p, q);                 // 1 - tanh^2 = 4 p q
+                g[j] *= 4.0f * p * q;
             }
             break;
         default: break;
@@ -242,12 +256,16 @@ __device__ __forceinline__ void act_grad8(int act, const float (&z)[8], float (&
 }
 
 // A saved pre-activation: fp16 (11 bits, where bf16's eight would add as much to the gradient's error as its own rounding does), beyond its range infinity.
-// relu's derivative is its sign: z times 2^127, of which even the smallest nonzero one stays nonzero.
-__device__ __forceinline__ f16x8 saved8(int act, const float (&z)[8]) {
+// relu's derivative is its sign: z times 2^127, of which even the smallest nonzero one stays nonzero.  A dropped entry is -infinity: the backward pass need not draw its
+// random bits again (16000 x 4096 with gelu': they were half of dz's arithmetic).
+__device__ __forceinline__ f16x8 saved8(int act, const float (&z)[8], const Dropout& d, const bool (&keep)[8]) {
     const float up = act == ACT_RELU ? 0x1p127f : 1.0f;
     float s[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) s[j] = z[j] * up;
+    if (d.cut != 0)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] = keep[j] ? s[j] : RNNT_NEG_INF;
     return round8<_Float16>(s);
 }
 
@@ -274,9 +292,11 @@ struct LinearStore {
     __device__ static __forceinline__ void store(const LinearEpilogue& e, long long m, int n, float (&v)[8], const Extra& r, float = 1.0f, int = 0) {
         if (m >= e.M || n >= e.N) return;
         const size_t at = (size_t)m * e.N + n;
-        if (e.saved != nullptr) put8((_Float16*)e.saved + at, e.N - n, saved8(e.act, v));
+        bool keep[8] = {};
+        if (e.drop.cut != 0) keep8(e.drop, m, n, keep);
+        if (e.saved != nullptr) put8((_Float16*)e.saved + at, e.N - n, saved8(e.act, v, e.drop, keep));
         act8<true>(e.act, v);
-        drop8(e.drop, m, n, v);
+        if (e.drop.cut != 0) drop8(e.drop, keep, v);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] += (float)r[j];
         put8((bf16_t*)e.y + at, e.N - n, round8<bf16_t>(v));
@@ -294,9 +314,16 @@ struct LinearStore32 {
     __device__ static __forceinline__ void store(const LinearEpilogue& e, long long m, int n, float (&v)[8], const Extra& r, float = 1.0f, int = 0) {
         if (m >= e.M || n >= e.N) return;
         const size_t at = (size_t)m * e.N + n;
-        if (e.saved != nullptr) store8((float*)e.saved + at, e.N - n, v);
+        bool keep[8] = {};
+        if (e.drop.cut != 0) keep8(e.drop, m, n, keep);
+        if (e.saved != nullptr) {
+            float s[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[j] = e.drop.cut == 0 || keep[j] ? v[j] : RNNT_NEG_INF;
+            store8((float*)e.saved + at, e.N - n, s);
+        }
         act8<false>(e.act, v);
-        drop8(e.drop, m, n, v);
+        if (e.drop.cut != 0) drop8(e.drop, keep, v);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] += r[j];
         store8((float*)e.y + at, e.N - n, v);

@@ -196,3 +196,30 @@ def test_a_captured_backward_pass_of_an_eager_forward_call_scales_once():
         torch.cuda.synchronize()
         for u, v in zip(got, ref):
             assert torch.equal(u, v)
+
+
+@pytest.mark.parametrize("name", Bd.ACTIVATIONS)
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("M", [40, 150])
+def test_dropped_entries_take_nothing_from_an_infinite_gradient(name, bf16, M):
+    torch = _torch()
+    K, N = 64, 72
+    i = _linear_inputs(M, K, N, bf16, res=False, seed=9)
+    dt = torch.bfloat16 if bf16 else torch.float32
+    x, W, b, dy = _dev(i["x"], dt), _dev(i["W"], dt), _dev(i["b"], torch.float32), _dev(i["dy"], dt)
+    rng = torch.tensor(STATE, dtype=torch.int64, device="cuda:0")
+    dropped = torch.from_numpy(O.keep_scale(M, N, *STATE, 0.3) == 0).cuda()
+    f = Bd.run_linear_fwd(x, W, b, name, None, 0.3, rng, save=True)
+    zero, wild = dy.masked_fill(dropped, 0.0), dy.masked_fill(dropped, float("inf"))
+    wild[0][dropped[0]] = float("nan")
+    g, h = (Bd.run_linear_bwd(x, W, d, name, f["saved"], 0.3, rng) for d in (zero, wild))
+    for k in ("dx", "dW", "db"):
+        assert torch.equal(g[k], h[k]), k
+    # and an infinite z that is dropped, or kept where act' is 0 or 1 there
+    big = torch.full((N,), 1e30, device="cuda:0")
+    for sign in (1.0, -1.0):
+        f = Bd.run_linear_fwd(x, W, sign * big, name, None, 0.3, rng, save=True)
+        g = Bd.run_linear_bwd(x, W, dy, name, f["saved"], 0.3, rng)
+        slope = {"none": 1.0, "tanh": 0.0}.get(name, 1.0 if sign > 0 else 0.0)
+        ref = (dy.double() * (~dropped) * (65536.0 / (65536 - round(0.3 * 65536))) * slope).sum(0)
+        assert torch.allclose(g["db"].double(), ref, rtol=1e-5, atol=1e-4), (sign, name)
