@@ -1,4 +1,5 @@
-// A few rows (at most 64) through a layer: single tokens, beams.  The product is bound by reading W, the call by latency, so one launch does it all.
+// A few rows (at most 64) through a layer: single tokens, beams.  The product is bound by reading W, the call by latency, so one launch does it all
+// (1 row, K = 640, N = 2560: 4.1 us on the GPU, W's 3.3 MB at a copy's rate 0.7).
 #include <algorithm>
 
 #include "layers_device.h"
@@ -102,7 +103,7 @@ __device__ __forceinline__ void few_finish(const FewJob& j, const E& e, const f3
 
 // rows x 32 columns of x W per workgroup, MT blocks of 16 rows.  A wave brings its steps (32 of k) of W through registers into LDS of its own, where the
 // transposing read makes MFMA fragments of them; x comes as fragments from memory.  The eight waves' sums meet in LDS.  Neighbouring column blocks share
-// lines of W: they go to one XCD.  What bounds it: latency (one token, K = 640, N = 2560: the launch, two trips to memory, the reduction).
+// lines of W: they go to one XCD.  What bounds it: latency (the launch, two trips to memory, the reduction).
 // WHOLE: K and N are multiples of 32, no piece has an end in it (the code for ends, eight loads under eight conditions for each load, takes longer to fetch
 // than to run).
 // Rows in several workgroups: gridDim.z.  A long sum is split over workgroups too (gridDim.y > 1), whose results go to slots [split][M][N up to 8].
@@ -189,7 +190,7 @@ __global__ __launch_bounds__(64 * FW) void k_few_rows(FewJob j, E e, int blocks,
 }
 
 // The same in fp32 on the fp32 matrix instruction (16 x 16 x 4), which takes its operands as they lie: a wave's step of 32 along k is eight of them, the
-// i-th with k = 8 g + i in the lanes of group g = l / 16, so that a lane's eight values of x are one piece.
+// i-th with k = 8 g + i in the lanes of group g = l / 16, so that a lane's eight values of x are one piece.  1 x 640 x 2560 6.0 us, 64 x 640 x 2560 9.7.
 template <int MT, bool WHOLE, class E>
 __global__ __launch_bounds__(64 * FW) void k_few_rows_f32(FewJob j, E e, int blocks, float* __restrict__ slots, int per_split) {
     __shared__ __align__(16) unsigned char smem[FW * MT * 16 * FC * 4];

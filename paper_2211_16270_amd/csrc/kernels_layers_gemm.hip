@@ -82,13 +82,16 @@ struct TileJob {
     int mt, nt, splits, per_split;
     __host__ __device__ long long workgroups() const { return ((long long)mt * nt * splits + 7) / 8 * 8; }
 };
+// y, or a split of it.  Bound by the matrix units' power in long sums, by each tile's start and epilogue in short ones: 16000 x 1024 x 4096 137 us (980 TFLOP/s)
+// plain, 175 with gelu, dropout and the saved z (their vector work, nothing hides it); 8000 x 512 x 2048 27 and 35.
 template <class TS, bool AKS, bool BKS, Passes HOW, class E>
 __global__ __launch_bounds__(TS::THREADS, 2) void k_layer_gemm(TileJob<E> j) {
     extern __shared__ __align__(16) unsigned char smem[];
     if (blockIdx.x == 0) pass_rng(j.e);
     gemm_workgroup<TS, AKS, BKS, HOW, E>(j.g, j.e, blockIdx.x, j.mt, j.nt, j.splits, j.per_split, smem);
 }
-// dx and dW; the product whose workgroups take longer goes first (16000 x 1024 x 4096: 239 us, behind the other 308).
+// dx and dW; the product whose workgroups take longer goes first (16000 x 1024 x 4096: 225 to 240 us, behind the other 308).  Bound like k_layer_gemm: CE, 9288 x
+// 1024 x 32768, 1190 us (1050 TFLOP/s; workgroups of 145 and 512 stages leave a tenth of the compute units' time unused).
 template <class TS, Passes HOW>
 __global__ __launch_bounds__(TS::THREADS, 2) void k_layer_grads(TileJob<StoreEpilogue> x, TileJob<StoreEpilogue> w, int wgs_x, int wgs_w) {
     extern __shared__ __align__(16) unsigned char smem[];
@@ -98,7 +101,7 @@ __global__ __launch_bounds__(TS::THREADS, 2) void k_layer_grads(TileJob<StoreEpi
     else gemm_workgroup<TS, true, true, HOW, StoreEpilogue>(w.g, w.e, x_first ? L - wgs_x : L, w.mt, w.nt, w.splits, w.per_split, smem);
 }
 
-// The sum of the splits' results, in order, and the epilogue.  One thread per eight columns.
+// The sum of the splits' results, in order, and the epilogue.  One thread per eight columns.  Bound by its bytes and, at 4 to 12 us, by the launch.
 template <class E>
 struct ReduceJob {
     GemmJob g;
@@ -146,7 +149,8 @@ __global__ __launch_bounds__(256) void k_layer_reduce_grads(ReduceJob<StoreEpilo
 
 // Scores of a tile and what the softmax needs of them: each row's maximum over the tile's columns, the sum of the exponentials relative to it and, where
 // the gradients follow, those exponentials.  They are kept as fp16 scaled by 2^15: 11 bits from 2^-29 of the tile's maximum up, an absolute error of
-// 2^-40 of it below, so a probability is off by at most 2^-12 of itself or 2^-40; one exponential per entry serves the statistics and the gradient.
+// 2^-40 of it below, so a probability is off by at most 2^-12 of itself or 2^-40; one exponential per entry serves the statistics and the gradient.  Bound by the
+// products and, behind each tile's, by its exponentials: 9288 x 1024 x 32768 700 to 735 us (870 TFLOP/s, 16 stages a tile).
 template <class TS, bool KEEP>
 __global__ __launch_bounds__(TS::THREADS, 2) void k_ce_scores(GemmJob g, CeEpilogue e, int mt, int nt) {
     extern __shared__ __align__(16) unsigned char smem[];
