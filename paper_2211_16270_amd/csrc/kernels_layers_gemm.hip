@@ -1,6 +1,7 @@
 // bf16 matrix products of the linear layer (y, dx, dW) and of the output layer's cross entropy (scores with their statistics; dx, dW).
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 
 #include "gemm_bf16_tile.h"
 #include "layers_device.h"
@@ -300,16 +301,19 @@ hipError_t grad_gemms(const GradGemm& dx, const GradGemm& dw, hipStream_t stream
 }  // namespace
 
 // Rounds of the chip (256 compute units; one large tile each, or two small ones) times a round's time, in units of a large tile's stage (about 1.5 us;
-// a small one, with its neighbour beside it, 0.7), with five stages' time for a round's start and end; the slots' way to memory and back.
+// a small one, with its neighbour beside it, 0.7), with some stages' time for a round's start and end: in a product by itself nine, of which a small tile's neighbour
+// hides a part; where two products share a launch, less.  Small tiles follow each other as places get free, so they go by parts of rounds (0.3 for the last):
+// 12000 x 512 x 1536, 2.2 rounds of small tiles 39.7 us and with silu, dropout and the saved z 51.8, two of large ones 44.2 and 65.6; 10000 x 640 x 2560, 3.1 and 2:
+// 58.2 and 75.5, 52.1 and 74.7.  Then the slots' way to memory and back.
 namespace {
-constexpr double STAGE_TIME[2] = {1.0, 0.7}, ENDS_TIME[2] = {5.0, 4.0}, AT_ONCE[2] = {256.0, 512.0}, BYTES_PER_UNIT = 6e6, LAUNCH_TIME = 3.0;
+constexpr double STAGE_TIME[2] = {1.0, 0.7}, ENDS_TIME[2] = {5.0, 4.0}, ALONE_ENDS[2] = {9.0, 5.5}, AT_ONCE[2] = {256.0, 512.0}, BYTES_PER_UNIT = 6e6, LAUNCH_TIME = 3.0;
 constexpr int SPLITS[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 32, 48, 64}, N_SPLITS = sizeof(SPLITS) / sizeof(int);
 struct Choice {
     GemmPlan p;
     double workgroups, time, extra;      // number, each one's time, the slots' time
 };
 // The splits of a product with tiles of shape k that are possible
-int choices(int k, long long M, long long N, int stages, size_t slot_cap, Choice (&c)[N_SPLITS]) {
+int choices(int k, long long M, long long N, int stages, size_t slot_cap, double ends, Choice (&c)[N_SPLITS]) {
     const int tile = k == 0 ? 256 : 128;
     const double tiles = (double)((M + tile - 1) / tile) * (double)((N + tile - 1) / tile);
     int n = 0;
@@ -317,7 +321,7 @@ int choices(int k, long long M, long long N, int stages, size_t slot_cap, Choice
         const GemmPlan p{tile, splits, (stages + splits - 1) / splits};
         const size_t bytes = gemm_slot_bytes(p, M, N);
         if (splits > 1 && (splits > stages / 2 || (splits - 1) * p.per_split >= stages || bytes > slot_cap)) continue;
-        c[n++] = Choice{p, tiles * splits, p.per_split * STAGE_TIME[k] + ENDS_TIME[k], (double)bytes * 2.0 / BYTES_PER_UNIT};
+        c[n++] = Choice{p, tiles * splits, p.per_split * STAGE_TIME[k] + ends, (double)bytes * 2.0 / BYTES_PER_UNIT};
     }
     return n;
 }
@@ -327,9 +331,9 @@ GemmPlan plan_gemm(long long M, long long N, int stages, size_t slot_cap) {
     double least = 1e300;
     for (int k = 0; k < 2; ++k) {
         Choice c[N_SPLITS];
-        const int n = choices(k, M, N, stages, slot_cap, c);
+        const int n = choices(k, M, N, stages, slot_cap, ALONE_ENDS[k], c);
         for (int i = 0; i < n; ++i) {
-            const double rounds = std::max(1.0, (double)(long long)((c[i].workgroups + AT_ONCE[k] - 1) / AT_ONCE[k]));
+            const double part = c[i].workgroups / AT_ONCE[k], rounds = std::max(1.0, k == 0 ? std::ceil(part) : part + 0.3);
             const double t = rounds * c[i].time + (c[i].p.splits > 1 ? LAUNCH_TIME + c[i].extra : 0.0);
             if (t < least) {
                 least = t;
@@ -345,7 +349,7 @@ PairPlan plan_pair(long long Mx, long long Nx, int stages_x, long long Mw, long 
     double least = 1e300;
     for (int k = 0; k < 2; ++k) {
         Choice x[N_SPLITS], w[N_SPLITS];
-        const int nx = choices(k, Mx, Nx, stages_x, slot_cap, x), nw = choices(k, Mw, Nw, stages_w, slot_cap, w);
+        const int nx = choices(k, Mx, Nx, stages_x, slot_cap, ENDS_TIME[k], x), nw = choices(k, Mw, Nw, stages_w, slot_cap, ENDS_TIME[k], w);
         for (int i = 0; i < nx; ++i)
             for (int j = 0; j < nw; ++j) {
                 // at least one workgroup's time; the last round is on average half empty
