@@ -399,7 +399,7 @@ hipError_t launch_grad_gemms(bool parts, int tile, const GradGemm& dx, const Gra
     ReduceJob<StoreEpilogue> x{}, w{};
     if (dx.g.M > 0) x = reduce_job(dx.g, dx.e, dx.slots, dx.splits);
     if (dw.g.M > 0) w = reduce_job(dw.g, dw.e, dw.slots, dw.splits);
-    const long long n = (long long)x.workgroups() + w.workgroups() + (db.part != nullptr ? (db.N + 31) / 32 : 0);
+    const long long n = (long long)x.workgroups() + w.workgroups() + (db.out != nullptr ? (db.N + 31) / 32 : 0);
     if (n == 0) return hipSuccess;
     if (n > 0x7fffffffLL) return hipErrorInvalidValue;
     k_layer_reduce_grads<<<dim3((unsigned)n), dim3(256), 0, stream>>>(x, w, db, (int)sum_blocks(db.rows, db.N), sum_rows(db.rows, db.N));

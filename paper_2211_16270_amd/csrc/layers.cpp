@@ -212,8 +212,8 @@ rnnt_status linear_bwd(const rnnt_linear_desc& d, const LinearPlan& p, const voi
         if (p.rest) take_twice(gw.g.A, gw.g.B, rest, (int)(p.Mp / 64));
         gw.e = StoreEpilogue{dW, d.accumulate_params ? (const float*)dW : nullptr, drop.scale, nullptr, nullptr, N, 0, Bias{}, K, d.N, (d.param_grads_bf16 & 1) != 0};
     }
-    const SumJob sum{db ? part : nullptr, M, p.Np, d.N, nullptr, 0, d.accumulate_params ? (const float*)db : nullptr, db, (d.param_grads_bf16 & 2) != 0, drop.scale,
-                     nullptr};
+    // (whether it is wanted is told by db: without rows the workspace, and with it `part`, may be null)
+    const SumJob sum{part, M, p.Np, d.N, nullptr, 0, d.accumulate_params ? (const float*)db : nullptr, db, (d.param_grads_bf16 & 2) != 0, drop.scale, nullptr};
     LAYER_HIP(launch_grad_gemms(p.f32, p.grads.tile, gx, gw, sum, stream));
     return RNNT_OK;
 }
@@ -413,8 +413,8 @@ rnnt_status run_ce(const rnnt_ce_desc& d, const CePlan& p, const void* x, const 
         float* acc = w16 ? (float*)(ws + p.off_acc) : (float*)dW;
         gw.e = StoreEpilogue{last ? dW : acc, !first || d.accumulate_params ? acc : nullptr, 1.0f, unit, nullptr, V, 0, Bias{}, D, d.V, last && w16};
         float* dba = (float*)(ws + p.off_dbacc);
-        const SumJob sum{db ? part : nullptr, n, p.pitch, d.V, rows.count, row0, first ? (d.accumulate_params ? (const float*)db : nullptr) : dba,
-                         last ? db : (void*)dba, last && b16, 1.0f, unit};
+        const SumJob sum{part, n, p.pitch, d.V, rows.count, row0, first ? (d.accumulate_params ? (const float*)db : nullptr) : dba,
+                         last || !db ? db : (void*)dba, last && b16, 1.0f, unit};
         LAYER_HIP(launch_grad_gemms(p.f32, p.pair.tile, gx, gw, sum, stream));
     }
     return RNNT_OK;

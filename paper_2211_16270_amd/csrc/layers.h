@@ -140,13 +140,13 @@ struct PairPlan {
 };
 PairPlan plan_pair(long long Mx, long long Nx, int stages_x, long long Mw, long long Nw, int stages_w, size_t slot_cap);
 struct SumJob {
-    const float* part;                   // null: none
-    long long rows, ld;                  // the rows that left the column sums
+    const float* part;
+    long long rows, ld;                  // the rows that left the column sums (0: part is not read)
     int N;
     const int* count;                    // of them those below *count - row0, or null
     long long row0;
     const float* prev;
-    void* out;
+    void* out;                           // null: none
     bool bf16;
     float scale;                         // out = prev + scale *unit times the sum
     const float* unit;                   // or null: 1
