@@ -616,7 +616,8 @@ def _check_rng(rng_state, dropout, device):
 
 
 def _aligned(t):
-    # (a view that starts inside a 16-byte piece is copied: the kernels move such pieces)
+    # (a view that starts inside a 16-byte piece is copied: the kernels move such pieces.  Called where the call's stream is the current one: copy, use and the
+    # memory's next owner follow each other on it.)
     return t if t is None or t.data_ptr() % 16 == 0 else t.clone()
 
 
@@ -669,8 +670,8 @@ def run_linear_fwd(x, W, b=None, activation="none", residual=None, dropout=0.0, 
     if residual is not None:
         _check_tensor("residual", residual, x.dtype, device, shape)
     desc, ref, nbytes = _linear_call(x.numel() // K, K, N, code, activation, dropout, 0, 0, bias_bf16, False)
-    x, W, b, residual = _aligned(x), _aligned(W), _aligned(b), _aligned(residual)
     with _CallOn(device, stream) as handle:
+        x, W, b, residual = _aligned(x), _aligned(W), _aligned(b), _aligned(residual)
         y = torch.empty(shape, dtype=x.dtype, device=device)
         saved = rng_used = None
         if save:
@@ -705,8 +706,8 @@ def run_linear_bwd(x, W, dy, activation="none", saved=None, dropout=0.0, rng_sta
         if saved is None:
             raise ValueError(f"the backward pass of {activation} needs what the forward call saved")
         _check_tensor("saved", saved, torch.float16 if code == RNNT_BF16 else torch.float32, device, shape)
-    x, W, dy, saved = _aligned(x), _aligned(W), _aligned(dy), _aligned(saved)
     with _CallOn(device, stream) as handle:
+        x, W, dy, saved = _aligned(x), _aligned(W), _aligned(dy), _aligned(saved)
         dx = torch.empty_like(x) if "dx" in want else None
         dW, db = _param_grads(accumulate_into, param_grads_bf16, want, (K, N), (N,), device)
         ws, ws_ptr, ws_bytes = _workspace(workspace, nbytes, device)
@@ -745,8 +746,8 @@ def run_ce_fwd(x, W, b, labels, ignore_label=-1, workspace: Optional[Workspace] 
     D, V, code, bias_bf16 = _check_ce(x, W, b, labels)
     device = x.device
     desc, ref, nbytes = _ce_call(labels.numel(), D, V, code, int(ignore_label), 0, 0, bias_bf16, False, int(budget_bytes))
-    x, W, b = _aligned(x), _aligned(W), _aligned(b)
     with _CallOn(device, stream) as handle:
+        x, W, b = _aligned(x), _aligned(W), _aligned(b)
         loss = torch.empty(labels.shape, dtype=torch.float32, device=device)
         ws, ws_ptr, ws_bytes = _workspace(workspace, nbytes, device)
         st = lib().rnnt_ce_loss_fwd(ref, x.data_ptr(), W.data_ptr(), _ptr(b), labels.data_ptr(), loss.data_ptr(), ws_ptr, ws_bytes, handle)
@@ -768,8 +769,8 @@ def run_ce_fwd_bwd(x, W, b, labels, row_weight=None, ignore_label=-1, accumulate
         raise ValueError("accumulate_into: dW is needed")
     desc, ref, nbytes = _ce_call(labels.numel(), D, V, code, int(ignore_label), int(accumulate_into is not None), int(param_grads_bf16), bias_bf16, True,
                                  int(budget_bytes))
-    x, W, b = _aligned(x), _aligned(W), _aligned(b)
     with _CallOn(device, stream) as handle:
+        x, W, b = _aligned(x), _aligned(W), _aligned(b)
         loss = torch.empty(labels.shape, dtype=torch.float32, device=device)
         dx = torch.empty_like(x)
         dW, db = _param_grads(accumulate_into, param_grads_bf16, ("dW", "db") if want_db else ("dW",), (D, V), (V,), device)

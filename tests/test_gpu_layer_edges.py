@@ -37,3 +37,39 @@ def test_an_empty_batch_has_gradients_of_zero(K, N, bf16, activation):
     del junk
     A.rnnt_linear(*leaves, activation=activation).sum().backward()
     assert leaves[0].grad.shape == (0, K) and bool((leaves[1].grad == 0).all()) and bool((leaves[2].grad == 0).all())
+
+
+def test_unaligned_views_on_a_stream_of_their_own():
+    """The caller's stream has waited for the current one, which is then kept busy: copies of views off a 16-byte boundary follow the call's stream alone."""
+    torch = _torch()
+    i = _linear_inputs(70, 63, 65, True, res=True)
+    c = _ce_inputs(70, 63, 65, True, 9)
+
+    def off(a, dtype=torch.bfloat16):
+        flat = torch.zeros(a.size + 1, dtype=dtype, device="cuda:0")
+        flat[1:] = _dev(a, dtype).reshape(-1)
+        return flat[1:].view(a.shape)
+
+    x, W, r, dy, b = (off(i[k]) for k in ("x", "W", "residual", "dy", "b"))
+    xc, Wc, lab, w = off(c["x"]), off(c["W"]), _dev(c["labels"], torch.int32), _dev(c["weight"], torch.float32)
+
+    def calls(stream=None):
+        f = Bd.run_linear_fwd(x, W, b, "silu", r, save=True, stream=stream)
+        g = Bd.run_linear_bwd(x, W, dy, "silu", f["saved"], stream=stream)
+        l = Bd.run_ce_fwd(xc, Wc, b, lab, stream=stream)
+        o = Bd.run_ce_fwd_bwd(xc, Wc, b, lab, w, stream=stream)
+        return [f["y"], f["saved"], *g.values(), l["loss"], *o.values()]
+
+    want = calls()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        side.wait_stream(torch.cuda.current_stream())
+        torch.cuda._sleep(20_000_000)
+        got = calls(side)
+        # (memory that the call's own copies took may be handed out again on this stream)
+        junk = [torch.full((n,), float("nan"), dtype=torch.bfloat16, device="cuda:0") for n in (70 * 63, 63 * 65, 70 * 65, 65)]
+        side.synchronize()
+        torch.cuda.synchronize()
+        del junk
+        for a, e in zip(got, want):
+            assert torch.equal(a, e)

@@ -1,0 +1,71 @@
+"""The Python front end of the layers beside the transducer loss, without a GPU: what it calls when, and what it refuses.  The library's calls are replaced by
+records of them, the tensors lie in host memory."""
+import pytest
+import torch
+
+from paper_2211_16270_amd import binding as Bd
+
+REAL = Bd.lib
+
+
+class _Library:
+    """The library with its calls that launch something recorded instead (all succeed)"""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        if name.endswith("_workspace_bytes"):
+            return getattr(REAL(), name)
+        return lambda *args: self.calls.append((name, args)) or 0
+
+
+class _Stream:
+    """Stands for the block in which the stream of a call is the current one"""
+    active = False
+
+    def __init__(self, device, stream):
+        pass
+
+    def __enter__(self):
+        _Stream.active = True
+
+    def __exit__(self, *exc):
+        _Stream.active = False
+
+
+@pytest.fixture
+def library(monkeypatch):
+    fake = _Library()
+    monkeypatch.setattr(Bd, "lib", lambda: fake)
+    monkeypatch.setattr(Bd, "_CallOn", _Stream)
+    monkeypatch.setattr(Bd, "_layer_dtype", lambda x, W, K: Bd.RNNT_BF16 if x.dtype == torch.bfloat16 else Bd.RNNT_F32)
+    return fake
+
+
+def _off(*shape, dtype=torch.bfloat16):
+    """A tensor that starts off a 16-byte boundary"""
+    n = 1
+    for s in shape:
+        n *= s
+    t = torch.zeros(n + 1, dtype=dtype)[1:].view(shape)
+    assert t.data_ptr() % 16 != 0
+    return t
+
+
+def test_copies_of_unaligned_tensors_are_made_on_the_calls_stream(library, monkeypatch):
+    clone, where = torch.Tensor.clone, []
+
+    def recorded(self, *args, **kw):
+        where.append(_Stream.active)
+        return clone(self, *args, **kw)
+
+    monkeypatch.setattr(torch.Tensor, "clone", recorded)
+    x, W, b, y, s = _off(5, 8), _off(8, 24), _off(24), _off(5, 24), _off(5, 24, dtype=torch.float16)
+    lab = torch.zeros(5, dtype=torch.int32)
+    for call, copies in ((lambda: Bd.run_linear_fwd(x, W, b, "silu", y), 4), (lambda: Bd.run_linear_bwd(x, W, y, "silu", s), 4),
+                         (lambda: Bd.run_ce_fwd(x, W, b, lab), 3), (lambda: Bd.run_ce_fwd_bwd(x, W, b, lab), 3)):
+        where.clear()
+        call()
+        assert where == [True] * copies
+    assert [name for name, _ in library.calls] == ["rnnt_linear_fwd", "rnnt_linear_bwd", "rnnt_ce_loss_fwd", "rnnt_ce_loss_fwd_bwd"]
