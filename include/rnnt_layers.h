@@ -109,8 +109,8 @@ typedef struct {
  * relative to the mantissa of the largest weight, in two values of it up to 64 rows.  The label's entry comes from the loss: exact also where p is near 1.
  *
  * workspace bytes: grads = 0 for rnnt_ce_loss_fwd, 1 for rnnt_ce_loss_fwd_bwd.  budget_bytes = 0: the library's default (chunk buffers of at most
- * 1 GiB); otherwise chunks as large as fit the budget, and if even the smallest (256 rows) exceed it, their size.  A workspace larger than that of the
- * default is used for larger chunks.
+ * 1 GiB); otherwise the size for as few chunks as the budget has room for, or, where it is too small for any number of them, the least size there is.  A
+ * call takes every workspace of at least such a size; one larger than the default's is used for larger chunks.
  */
 size_t rnnt_ce_loss_workspace_bytes(const rnnt_ce_desc* desc, int32_t grads, size_t budget_bytes);
 rnnt_status rnnt_ce_loss_fwd(const rnnt_ce_desc* desc, const void* x, const void* W, const void* b, const int32_t* label, float* loss,

@@ -302,26 +302,33 @@ CePlan plan_ce_chunk(const rnnt_ce_desc& d, bool grads, long long chunk) {
     p.bytes = c.bytes;
     return p;
 }
-// The largest chunks whose plan takes at most `budget` bytes (0: whose buffers take at most CE_CHUNK), at least 256 rows
+// Equal chunks, as few as a plan of at most `budget` bytes has (0: as chunk buffers of at most CE_CHUNK allow); the plan of fewest bytes where none does.
+// A plan's bytes do not grow with its chunks: a single one needs no sums over the chunks (D x V floats), and longer ones take fewer splits.  So every number of
+// chunks that can fit is looked at (1 us each).  The plan for a budget of its own bytes is itself.
 CePlan plan_ce(const rnnt_ce_desc& d, bool grads, size_t budget) {
+    const bool f32 = d.dtype == RNNT_F32;
     const long long all = std::max(256LL, up(d.R, 256));
-    const size_t row = d.dtype == RNNT_BF16 ? (size_t)(up(d.V, 256) + 64) * 2 : (size_t)up(d.V, 64) * (4 + (grads ? PARTS * 2 : 0));
-    if (budget == 0) {
-        // equal chunks
-        const long long most = std::max(256LL, (long long)(CE_CHUNK / row) / 256 * 256), n = (all + most - 1) / most;
-        return plan_ce_chunk(d, grads, up((all + n - 1) / n, 256));
+    const size_t row = f32 ? (size_t)up(d.V, 64) * (4 + (grads ? PARTS * 2 : 0)) : (size_t)(up(d.V, 256) + 64) * 2;
+    // the chunks where each takes at most `rows` rows, a multiple of 256
+    auto equal = [&](long long rows) {
+        const long long n = (all + rows - 1) / rows;
+        return up((all + n - 1) / n, 256);
+    };
+    if (budget == 0) return plan_ce_chunk(d, grads, equal(std::max(256LL, (long long)(CE_CHUNK / row) / 256 * 256)));
+    // (losses alone of RNNT_BF16 keep no exponentials)
+    const size_t most = f32 || grads ? budget / row : (size_t)all;
+    for (long long c = equal(std::max(256LL, (long long)std::min(most, (size_t)all) / 256 * 256));; c = equal(c - 256)) {
+        const CePlan p = plan_ce_chunk(d, grads, c);
+        if (p.bytes <= budget) return p;
+        if (c <= 256) break;
     }
-    long long lo = 1, hi = all / 256;                 // in units of 256 rows; lo always taken
-    CePlan best = plan_ce_chunk(d, grads, 256);
-    while (lo < hi) {
-        const long long mid = (lo + hi + 1) / 2;
-        const CePlan p = plan_ce_chunk(d, grads, mid * 256);
-        if (p.bytes <= budget) {
-            lo = mid;
-            best = p;
-        } else hi = mid - 1;
+    CePlan least = plan_ce_chunk(d, grads, all);
+    for (long long c = all; c > 256;) {
+        c = equal(c - 256);
+        const CePlan p = plan_ce_chunk(d, grads, c);
+        if (p.bytes < least.bytes) least = p;
     }
-    return best;
+    return least;
 }
 
 rnnt_status run_ce(const rnnt_ce_desc& d, const CePlan& p, const void* x, const void* W, const Bias& b, const int32_t* label, const float* row_weight,
@@ -472,10 +479,7 @@ static rnnt_status ce_loss(const rnnt_ce_desc* desc, bool grads, const void* x, 
     if (!aligned({x, W, b, dx, dW, db}) || (((uintptr_t)label | (uintptr_t)row_weight | (uintptr_t)loss) % 4) != 0) return RNNT_ERR_UNSUPPORTED;
     // the default plan where it fits, larger chunks in a larger workspace, smaller ones in a smaller
     CePlan p = plan_ce(*desc, grads, 0);
-    if (workspace_bytes != p.bytes && (p.chunks > 1 || workspace_bytes < p.bytes)) {
-        const CePlan q = plan_ce(*desc, grads, workspace_bytes == 0 ? 1 : workspace_bytes);
-        if (workspace_bytes < p.bytes || q.chunk > p.chunk) p = q;
-    }
+    if (workspace_bytes < p.bytes || (workspace_bytes > p.bytes && p.chunks > 1)) p = plan_ce(*desc, grads, workspace_bytes == 0 ? 1 : workspace_bytes);
     if (!workspace_ok(workspace, workspace_bytes, p.bytes)) return RNNT_ERR_WORKSPACE;
     return run_ce(*desc, p, x, W, Bias{b, desc->bias_bf16 != 0}, label, row_weight, loss, dx, dW, db, (unsigned char*)workspace, (hipStream_t)hip_stream);
 }

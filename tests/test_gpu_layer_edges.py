@@ -4,7 +4,7 @@ import pytest
 
 from paper_2211_16270_amd import binding as Bd
 from tests import layer_oracle as O
-from tests.test_gpu_layers import _ce_inputs, _check_ce, _check_linear, _dev, _linear_inputs, _np, _torch
+from tests.test_gpu_layers import _ce_inputs, _check_ce, _check_linear, _dev, _linear_inputs, _np, _run_ce, _torch
 
 pytestmark = pytest.mark.gpu
 
@@ -73,3 +73,12 @@ def test_unaligned_views_on_a_stream_of_their_own():
         del junk
         for a, e in zip(got, want):
             assert torch.equal(a, e)
+
+
+@pytest.mark.parametrize("R,D,V,bits,budget", [(1024, 64, 2048, 3, 4 << 20), (1856, 512, 1024, 3, 18881224), (1291, 685, 1343, 0, 27 << 20),
+                                               (1742, 646, 717, 3, 12 << 20), (1130, 559, 898, 0, 15100000)])
+def test_cross_entropy_within_budgets(R, D, V, bits, budget):
+    i = _ce_inputs(R, D, V, True, R // 5)
+    ref = O.cross_entropy(i["x"], i["W"], i["b"], i["labels"], i["weight"])
+    for b in (budget, Bd.rnnt_ce_loss_workspace_bytes(Bd.RnntCeDesc(R, D, V, Bd.RNNT_BF16, -1, 0, bits, 0), True, budget)):
+        _check_ce(_run_ce(i, True, budget=b, bits=bits), i, ref, True, bits)
