@@ -117,11 +117,16 @@ def rnnt_linear(x, W, b=None, activation="none", residual=None, dropout: float =
 
 
 def _ce_grads(x, W, b, labels, row_weight, ignore_label, budget_bytes):
-    out = Bd.run_ce_fwd_bwd(x, W, b, labels, row_weight, ignore_label, param_grads_bf16=_grads_bf16(W, b), want_db=b is not None,
-                            budget_bytes=budget_bytes)
-    if b is not None and out["db"].dtype != b.dtype:
-        out["db"] = out["db"].to(b.dtype)
-    return out
+    return Bd.run_ce_fwd_bwd(x, W, b, labels, row_weight, ignore_label, param_grads_bf16=_grads_bf16(W, b), want_db=b is not None,
+                             budget_bytes=budget_bytes)
+
+
+def _ce_leaf_grads(need, out, b):
+    """dx, dW, db as the leaves have them (the library's db is float32 beside a float32 W, whatever b's type)"""
+    db = out["db"]
+    if need[2] and db.dtype != b.dtype:
+        db = db.to(b.dtype)
+    return out["dx"] if need[0] else None, out["dW"] if need[1] else None, db if need[2] else None
 
 
 class _RnntCeSum(torch.autograd.Function):
@@ -148,8 +153,7 @@ class _RnntCeSum(torch.autograd.Function):
         else:
             w = g.expand(labels.shape).contiguous() if row_weight is None else row_weight * g
             out = _ce_grads(x, W, b, labels, w, *ctx.opts)
-        need = ctx.needs_input_grad
-        return (out["dx"] if need[0] else None, out["dW"] if need[1] else None, out["db"] if need[2] else None, None, None, None, None)
+        return (*_ce_leaf_grads(ctx.needs_input_grad, out, b), None, None, None, None)
 
 
 class _RnntCeRows(torch.autograd.Function):
@@ -163,10 +167,8 @@ class _RnntCeRows(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, g):
         x, W, b, labels = ctx.saved_tensors
-        need = ctx.needs_input_grad
         out = _ce_grads(x, W, b, labels, g.float().contiguous(), *ctx.opts)
-        return (out["dx"] if need[0] else None, out["dW"] if need[1] else None, out["db"] if need[2] else None,
-                None, None, None)
+        return (*_ce_leaf_grads(ctx.needs_input_grad, out, b), None, None, None)
 
 
 def rnnt_ce_loss(x, W, b, labels, row_weight=None, ignore_label: int = -1, reduction: str = "sum", budget_bytes: int = 0):

@@ -82,3 +82,31 @@ def test_cross_entropy_within_budgets(R, D, V, bits, budget):
     ref = O.cross_entropy(i["x"], i["W"], i["b"], i["labels"], i["weight"])
     for b in (budget, Bd.rnnt_ce_loss_workspace_bytes(Bd.RnntCeDesc(R, D, V, Bd.RNNT_BF16, -1, 0, bits, 0), True, budget)):
         _check_ce(_run_ce(i, True, budget=b, bits=bits), i, ref, True, bits)
+
+
+@pytest.mark.parametrize("x_bf16", [True, False])
+@pytest.mark.parametrize("b_bf16", [True, False])
+@pytest.mark.parametrize("reduction", ["sum", "none"])
+@pytest.mark.parametrize("R", [40, 150])
+def test_cross_entropy_takes_a_bias_of_either_type(x_bf16, b_bf16, reduction, R):
+    torch = _torch()
+    from paper_2211_16270_amd import autograd as A
+    i = _ce_inputs(R, 40, 130, x_bf16, 9)
+    dt = torch.bfloat16 if x_bf16 else torch.float32
+    b = _dev(i["b"], torch.bfloat16 if b_bf16 else torch.float32)
+    i["b"] = _np(b)
+    leaves = dict(dx=_dev(i["x"], dt), dW=_dev(i["W"], dt), db=b)
+    for t in leaves.values():
+        t.requires_grad_()
+    w, lab = _dev(i["weight"], torch.float32), _dev(i["labels"], torch.int32)
+    if reduction == "sum":
+        loss = A.rnnt_ce_loss(*leaves.values(), lab, row_weight=w)
+    else:
+        loss = (A.rnnt_ce_loss(*leaves.values(), lab, reduction="none") * w).sum()
+    (loss * 3.0).backward()
+    ref = O.cross_entropy(i["x"], i["W"], i["b"], i["labels"], 3.0 * i["weight"])
+    for k, t in leaves.items():
+        assert t.grad.dtype == t.dtype, k
+        # (1e-2: every bf16 gradient of the library; an fp32 one 1e-5, its bias' rounding to bf16 2^-8)
+        tol = 1e-2 if x_bf16 else 2.0 ** -8 if t.dtype == torch.bfloat16 else 1e-5
+        assert np.linalg.norm(_np(t.grad) - ref[k]) <= tol * np.linalg.norm(ref[k]), k

@@ -39,6 +39,8 @@ def library(monkeypatch):
     fake = _Library()
     monkeypatch.setattr(Bd, "lib", lambda: fake)
     monkeypatch.setattr(Bd, "_CallOn", _Stream)
+    monkeypatch.setattr(Bd, "_stream_handle", lambda stream: None)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
     monkeypatch.setattr(Bd, "_layer_dtype", lambda x, W, K: Bd.RNNT_BF16 if x.dtype == torch.bfloat16 else Bd.RNNT_F32)
     return fake
 
@@ -69,3 +71,19 @@ def test_copies_of_unaligned_tensors_are_made_on_the_calls_stream(library, monke
         call()
         assert where == [True] * copies
     assert [name for name, _ in library.calls] == ["rnnt_linear_fwd", "rnnt_linear_bwd", "rnnt_ce_loss_fwd", "rnnt_ce_loss_fwd_bwd"]
+
+
+@pytest.mark.parametrize("x_type,b_type,bits", [(torch.float32, torch.bfloat16, 0), (torch.float32, torch.float32, 0), (torch.bfloat16, torch.bfloat16, 3),
+                                                (torch.bfloat16, torch.float32, 1)])
+def test_summed_loss_scales_gradients_of_the_librarys_types(library, monkeypatch, x_type, b_type, bits):
+    """The descriptor of rnnt_ce_loss_scale is one the library takes, whatever the bias' type; the leaves get gradients of their own types."""
+    from paper_2211_16270_amd import autograd as A
+    seen = []
+    monkeypatch.setattr(Bd, "rnnt_ce_loss_scale", lambda desc, *a, **kw: seen.append(
+        (desc.dtype, desc.param_grads_bf16, REAL().rnnt_ce_loss_scale(desc, None, None, None, None, None))) or 0)
+    x, W, b = torch.zeros(5, 8, dtype=x_type), torch.zeros(8, 24, dtype=x_type), torch.zeros(24, dtype=b_type)
+    leaves = [t.requires_grad_() for t in (x, W, b)]
+    A.rnnt_ce_loss(*leaves, torch.zeros(5, dtype=torch.int32)).backward()
+    # (a factor of NULL is what the library complains of last)
+    assert seen == [(Bd.RNNT_BF16 if x_type == torch.bfloat16 else Bd.RNNT_F32, bits, Bd.STATUS_NAMES.index("RNNT_ERR_NULL"))]
+    assert all(t.grad.dtype == t.dtype and t.grad.shape == t.shape for t in leaves)
