@@ -16,8 +16,9 @@ otherwise).  The forward call's outputs and workspace stay alive until backward 
     y = rnnt_linear(x, W, b, activation="silu", residual=None, dropout=0.1, rng_state=state)      # the encoders' layers
     loss = rnnt_ce_loss(x, W_out, b_out, labels, row_weight=w)                                    # cross entropy of the same output layer
 
-Steps of these can be captured into a graph (torch.cuda.graph) as whole forward and backward passes.  Torch's own condition holds: no eager graph of the same
-leaves may be alive then (delete the warm-up's outputs and losses before the capture), as its gradient accumulators belong to another stream.
+Steps of these can be captured into a graph (torch.cuda.graph), forward and backward passes together or each in one of its own.  Torch's own condition holds: no
+eager graph of the same leaves may be alive then (delete the warm-up's outputs and losses before the capture), as its gradient accumulators belong to another
+stream.
 """
 from __future__ import annotations
 
@@ -135,7 +136,7 @@ class _RnntCeSum(torch.autograd.Function):
         if any(ctx.needs_input_grad[:3]):
             out = _ce_grads(x, W, b, labels, row_weight, ignore_label, budget_bytes)
             ctx.save_for_backward(x, W, b, labels, row_weight)
-            ctx.grads, ctx.opts, ctx.captured = out, (ignore_label, budget_bytes), torch.cuda.is_current_stream_capturing()
+            ctx.grads, ctx.opts, ctx.captured = out, (ignore_label, budget_bytes), Bd.capture_id()
         else:
             out = Bd.run_ce_fwd(x, W, b, labels, ignore_label, budget_bytes=budget_bytes)
         return Bd.run_ce_total(out["loss"], row_weight)
@@ -145,10 +146,15 @@ class _RnntCeSum(torch.autograd.Function):
     def backward(ctx, g):
         x, W, b, labels, row_weight = ctx.saved_tensors
         g = g.float().contiguous()
-        if ctx.grads is not None and ctx.captured == torch.cuda.is_current_stream_capturing():
+        capture = Bd.capture_id()
+        if ctx.grads is not None and ctx.captured == capture:
             # the forward call's gradients are handed out, times g in place; a second backward pass of the same graph computes them again, and so does one
-            # that is captured without its forward call, as each replay would scale them once more
+            # that is captured behind an eager forward call
             out, ctx.grads = ctx.grads, None
+            Bd.run_ce_scale(g, out["dx"], out["dW"], out["db"])
+        elif ctx.grads is not None and ctx.captured and capture:
+            # captured, and the forward call too, but elsewhere: in place, each replay of this graph alone would scale them once more
+            out = {k: None if ctx.grads[k] is None else ctx.grads[k].clone() for k in ("dx", "dW", "db")}
             Bd.run_ce_scale(g, out["dx"], out["dW"], out["db"])
         else:
             w = g.expand(labels.shape).contiguous() if row_weight is None else row_weight * g

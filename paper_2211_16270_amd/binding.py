@@ -556,6 +556,20 @@ def rnnt_ce_loss_scale(desc: RnntCeDesc, factor, dx, dW, db, stream=None) -> int
     return int(lib().rnnt_ce_loss_scale(ctypes.byref(desc), _ptr(factor), _ptr(dx), _ptr(dW), _ptr(db), _stream_handle(stream)))
 
 
+def capture_id() -> int:
+    """0 where torch's current stream is not being captured into a graph, else a number that only the capture under way has."""
+    import torch
+    if not torch.cuda.is_current_stream_capturing():
+        return 0
+    status, number = ctypes.c_int(), ctypes.c_ulonglong()
+    query = lib().hipStreamGetCaptureInfo              # (of the runtime that the library is linked with)
+    query.argtypes, query.restype = [ctypes.c_void_p, ctypes.POINTER(ctypes.c_int), ctypes.POINTER(ctypes.c_ulonglong)], ctypes.c_int
+    err = query(_stream_handle(None), ctypes.byref(status), ctypes.byref(number))
+    if err != 0:
+        raise RuntimeError(f"hipStreamGetCaptureInfo: error {err}")
+    return int(number.value) + 1
+
+
 # What a call of the functions below needs besides its tensors is a function of sizes and types: kept, so that a small call does not spend its time here.
 @functools.lru_cache(maxsize=4096)
 def _linear_call(M, K, N, code, activation, dropout, accumulate, param_grads_bf16, bias_bf16, backward):

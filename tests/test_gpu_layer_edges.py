@@ -110,3 +110,43 @@ def test_cross_entropy_takes_a_bias_of_either_type(x_bf16, b_bf16, reduction, R)
         # (1e-2: every bf16 gradient of the library; an fp32 one 1e-5, its bias' rounding to bf16 2^-8)
         tol = 1e-2 if x_bf16 else 2.0 ** -8 if t.dtype == torch.bfloat16 else 1e-5
         assert np.linalg.norm(_np(t.grad) - ref[k]) <= tol * np.linalg.norm(ref[k]), k
+
+
+@pytest.mark.parametrize("R", [40, 300])
+@pytest.mark.parametrize("together", [True, False])
+def test_captured_forward_and_backward_passes(R, together):
+    """In one graph, or a backward pass captured by itself: each of its replays gives the gradients of its forward pass' last one, however often it is replayed."""
+    torch = _torch()
+    from paper_2211_16270_amd import autograd as A
+    D, V = 64, 200
+    g = torch.Generator(device="cuda:0").manual_seed(R)
+    n = lambda *s, k=1.0: (torch.randn(*s, generator=g, device="cuda:0") * k).bfloat16()
+    x, W, b = n(R, D), n(D, V, k=D ** -0.5), n(V)
+    lab = torch.randint(-1, V, (R,), generator=g, device="cuda:0", dtype=torch.int32)
+    up = torch.tensor(4.0, device="cuda:0")                      # (a power of two: scaling rounds nothing)
+    leaves = [t.requires_grad_() for t in (x, W, b)]
+    # the code is loaded before the capture
+    A.rnnt_ce_loss(*leaves, lab).backward()
+    for t in leaves:
+        t.grad = None
+    torch.cuda.synchronize()
+    pool = torch.cuda.graph_pool_handle()
+    forward, backward = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(forward, pool=pool):
+        loss = A.rnnt_ce_loss(*leaves, lab)
+        if together:
+            grads = torch.autograd.grad(loss, leaves, up)
+    if not together:
+        with torch.cuda.graph(backward, pool=pool):
+            grads = torch.autograd.grad(loss, leaves, up)
+    for k in range(3):
+        with torch.no_grad():
+            x.copy_(n(R, D))
+        forward.replay()
+        want = Bd.run_ce_fwd_bwd(x.detach(), W.detach(), b.detach(), lab, param_grads_bf16=3)
+        for again in range(3):
+            (forward if together else backward).replay()
+            torch.cuda.synchronize()
+            for got, key in zip(grads, ("dx", "dW", "db")):
+                assert torch.equal(got, (want[key].float() * 4.0).bfloat16()), (k, again, key)
+            torch.zeros(1 << 16, device="cuda:0").sum().item()
