@@ -642,6 +642,8 @@ class _CallOn:
 
     def __init__(self, device, stream):
         import torch
+        if device.type != "cuda":
+            raise ValueError(f"expected CUDA tensors, got one on {device}")
         self.contexts, self.index = None, device.index
         if stream is not None:
             if stream.device != device:
@@ -811,12 +813,21 @@ def run_ce_total(loss, row_weight=None, stream=None):
 
 
 def run_ce_scale(factor, dx, dW, db=None, stream=None):
-    """The gradients of run_ce_fwd_bwd times the scalar float32 tensor `factor`, in place (nothing is moved where it is 1)."""
+    """The gradients of run_ce_fwd_bwd (dx [..., D], dW [D, V], db [V] or None) times the scalar float32 tensor `factor`, in place (nothing is moved where it is
+    1).  dW and db are float32, or bfloat16 beside a bfloat16 dx."""
     import torch
-    _check_tensor("factor", factor, torch.float32, dx.device)
+    code = _DTYPE_CODES.get(str(dx.dtype))
+    if code is None or factor.numel() != 1 or dW.dim() != 2 or dx.dim() < 1 or dx.shape[-1] != dW.shape[0] or dW.numel() == 0:
+        raise ValueError(f"factor, dx [..., D] and dW [D, V] do not fit: {tuple(factor.shape)}, {dx.dtype} {tuple(dx.shape)}, {tuple(dW.shape)}")
     D, V = dW.shape
-    code = RNNT_BF16 if dx.dtype == torch.bfloat16 else RNNT_F32
-    bits = int(dW.dtype == torch.bfloat16) | (2 if db is not None and db.dtype == torch.bfloat16 else 0)
+    _check_tensor("factor", factor, torch.float32, dx.device)
+    _check_tensor("dx", dx, dx.dtype, dx.device)
+    bits = 0
+    for bit, name, t, shape in ((1, "dW", dW, (D, V)), (2, "db", db, (V,))):
+        if t is not None:
+            bf16 = code == RNNT_BF16 and t.dtype == torch.bfloat16
+            _check_tensor(name, t, torch.bfloat16 if bf16 else torch.float32, dx.device, shape)
+            bits |= bit * bf16
     with _CallOn(dx.device, stream):
         st = rnnt_ce_loss_scale(RnntCeDesc(dx.numel() // D, D, V, code, -1, 0, bits, 0), factor, dx, dW, db)
     if st != 0:

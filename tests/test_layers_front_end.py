@@ -87,3 +87,31 @@ def test_summed_loss_scales_gradients_of_the_librarys_types(library, monkeypatch
     # (a factor of NULL is what the library complains of last)
     assert seen == [(Bd.RNNT_BF16 if x_type == torch.bfloat16 else Bd.RNNT_F32, bits, Bd.STATUS_NAMES.index("RNNT_ERR_NULL"))]
     assert all(t.grad.dtype == t.dtype and t.grad.shape == t.shape for t in leaves)
+
+
+def test_scaling_refuses_gradients_that_do_not_fit_together(library):
+    f = torch.ones(())
+    t = lambda *s, dtype=torch.float32: torch.zeros(s, dtype=dtype)
+    half = torch.float16
+    for dx, dW, db in ((t(5, 8, dtype=half), t(8, 24), None), (t(5, 8), t(8, 24, dtype=half), None), (t(5, 8), t(8, 24), t(24, dtype=half)),      # types
+                       (t(5, 8), t(8, 24), t(23)), (t(5, 7), t(8, 24), None), (t(5, 8), t(8 * 24), None), (t(5, 8), t(8, 24), t(24, 1)),            # shapes
+                       (t(8, 5).t(), t(8, 24), None), (t(5, 8), t(8, 48)[:, ::2], None), (t(5, 8), t(24, 8).t(), None), (t(5, 8), t(8, 24), t(48)[::2]),   # strides
+                       (t(5, 8), t(8, 24, dtype=torch.bfloat16), None), (t(5, 8), t(8, 24), t(24, dtype=torch.bfloat16)),        # of no descriptor
+                       (t(5, 8).to("meta"), t(8, 24), None), (t(5, 8), t(8, 24).to("meta"), None)):                             # devices
+        with pytest.raises(ValueError):
+            Bd.run_ce_scale(f, dx, dW, db)
+    for factor in (torch.ones(2), torch.ones(0), torch.ones((), dtype=torch.float64)):
+        with pytest.raises(ValueError):
+            Bd.run_ce_scale(factor, t(5, 8), t(8, 24))
+    assert library.calls == []
+    Bd.run_ce_scale(f, t(5, 8), t(8, 24), t(24))
+    Bd.run_ce_scale(torch.ones(1), t(2, 3, 8, dtype=torch.bfloat16), t(8, 24, dtype=torch.bfloat16), t(24))
+    Bd.run_ce_scale(f, t(0, 8), t(8, 24))
+    assert len(library.calls) == 3
+
+
+def test_tensors_in_host_memory_are_refused():
+    with pytest.raises(ValueError, match="CUDA"):
+        Bd.run_ce_total(torch.zeros(4))
+    with pytest.raises(ValueError, match="CUDA"):
+        Bd.run_ce_scale(torch.ones(()), torch.zeros(5, 8), torch.zeros(8, 24))
