@@ -666,6 +666,8 @@ class _CallOn:
 def _workspace(workspace, nbytes, device):
     """(the tensor to keep, its address, its bytes)"""
     import torch
+    if workspace is not None and workspace.buf.device != device:
+        raise ValueError(f"workspace on {workspace.buf.device}, tensors on {device}")
     buf = workspace.buf if workspace is not None else torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
     return (None, None, 0) if buf is None else (buf, buf.data_ptr(), buf.numel())
 

@@ -115,3 +115,17 @@ def test_tensors_in_host_memory_are_refused():
         Bd.run_ce_total(torch.zeros(4))
     with pytest.raises(ValueError, match="CUDA"):
         Bd.run_ce_scale(torch.ones(()), torch.zeros(5, 8), torch.zeros(8, 24))
+
+
+def test_a_workspace_of_another_device_is_refused(library):
+    x, W, y, lab = torch.zeros(5, 7), torch.zeros(7, 24), torch.zeros(5, 24), torch.zeros(5, dtype=torch.int32)
+    ws = Bd.Workspace.__new__(Bd.Workspace)
+    ws.buf = torch.empty(1 << 20, dtype=torch.uint8, device="meta")
+    for call in (lambda: Bd.run_linear_fwd(x, W, workspace=ws), lambda: Bd.run_linear_bwd(x, W, y, workspace=ws),
+                 lambda: Bd.run_ce_fwd(x, W, None, lab, workspace=ws), lambda: Bd.run_ce_fwd_bwd(x, W, None, lab, workspace=ws)):
+        with pytest.raises(ValueError, match="workspace"):
+            call()
+    assert library.calls == []
+    ws.buf = torch.empty(1 << 20, dtype=torch.uint8)
+    Bd.run_linear_fwd(x, W, workspace=ws)
+    assert len(library.calls) == 1
