@@ -77,6 +77,11 @@ def rnnt_joint_loss(enc, pred, W_out, b_out, labels, T_len, U_len, blank: int = 
                                 keep_scores)
 
 
+def _tracked(*tensors):
+    """Whether a gradient of one of them can be asked for.  (ctx.needs_input_grad does not tell: it is true under no_grad too.)"""
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
 def _grads_bf16(W, b):
     """param_grads_bf16 of leaves W, b: gradients of their types"""
     return 0 if W.dtype == torch.float32 else 3 if b is not None and b.dtype == torch.bfloat16 else 1
@@ -114,6 +119,8 @@ def rnnt_linear(x, W, b=None, activation="none", residual=None, dropout: float =
     x [..., K], W [K, N] (float32 or bfloat16, CUDA, contiguous), b [N] (float32 or bfloat16) or None, residual [..., N] or None; activation: none,
     relu, silu, gelu, tanh.  dropout in [0, 1) needs rng_state, an int64 tensor [2] on the device with {seed, offset}: the mask is a function of them
     and of an entry's place, so advance the offset between calls that shall have different masks (in place, also inside a captured graph)."""
+    if not _tracked(x, W, b, residual):
+        return Bd.run_linear_fwd(x, W, b, activation, residual, dropout, rng_state)["y"]
     return _RnntLinear.apply(x, W, b, activation, residual, float(dropout), rng_state)
 
 
@@ -133,12 +140,9 @@ def _ce_leaf_grads(need, out, b):
 class _RnntCeSum(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, W, b, labels, row_weight, ignore_label, budget_bytes):
-        if any(ctx.needs_input_grad[:3]):
-            out = _ce_grads(x, W, b, labels, row_weight, ignore_label, budget_bytes)
-            ctx.save_for_backward(x, W, b, labels, row_weight)
-            ctx.grads, ctx.opts, ctx.captured = out, (ignore_label, budget_bytes), Bd.capture_id()
-        else:
-            out = Bd.run_ce_fwd(x, W, b, labels, ignore_label, budget_bytes=budget_bytes)
+        out = _ce_grads(x, W, b, labels, row_weight, ignore_label, budget_bytes)
+        ctx.save_for_backward(x, W, b, labels, row_weight)
+        ctx.grads, ctx.opts, ctx.captured = out, (ignore_label, budget_bytes), Bd.capture_id()
         return Bd.run_ce_total(out["loss"], row_weight)
 
     @staticmethod
@@ -183,12 +187,15 @@ def rnnt_ce_loss(x, W, b, labels, row_weight=None, ignore_label: int = -1, reduc
     x [..., D], W [D, V] (float32 or bfloat16, CUDA, contiguous), b [V] (float32 or bfloat16) or None, labels [...] int32 (rows with ignore_label are
     padding: loss and gradients 0, x never used).
     reduction "sum": sum of row_weight * loss over the rows (row_weight [...] float32 on the device, None: ones; 1 / count for a mean), a scalar.  The
-    forward call computes the gradients too (three products per row); backward scales them.
+    forward call computes the gradients too (three products per row) where one can be asked for, not under no_grad; backward scales them.
     reduction "none": the loss of each row; the gradients are computed in backward, with the incoming gradient as the rows' weights (four products)."""
+    if reduction not in ("sum", "none"):
+        raise ValueError(f"reduction must be 'sum' or 'none', got {reduction!r}")
+    if reduction == "none" and row_weight is not None:
+        raise ValueError("row_weight goes with reduction='sum'; with 'none' weight the returned losses")
+    if not _tracked(x, W, b):
+        loss = Bd.run_ce_fwd(x, W, b, labels, ignore_label, budget_bytes=budget_bytes)["loss"]
+        return loss if reduction == "none" else Bd.run_ce_total(loss, row_weight)
     if reduction == "sum":
         return _RnntCeSum.apply(x, W, b, labels, row_weight, ignore_label, budget_bytes)
-    if reduction != "none":
-        raise ValueError(f"reduction must be 'sum' or 'none', got {reduction!r}")
-    if row_weight is not None:
-        raise ValueError("row_weight goes with reduction='sum'; with 'none' weight the returned losses")
     return _RnntCeRows.apply(x, W, b, labels, ignore_label, budget_bytes)

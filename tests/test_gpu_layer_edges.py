@@ -150,3 +150,35 @@ def test_captured_forward_and_backward_passes(R, together):
             for got, key in zip(grads, ("dx", "dW", "db")):
                 assert torch.equal(got, (want[key].float() * 4.0).bfloat16()), (k, again, key)
             torch.zeros(1 << 16, device="cuda:0").sum().item()
+
+
+@pytest.mark.parametrize("R", [40, 2000])
+def test_evaluation_computes_no_gradients(R):
+    torch = _torch()
+    from paper_2211_16270_amd import autograd as A
+    D, V, N = 512, 8192, 1024
+    i = _ce_inputs(R, D, V, True, R // 4)
+    x, W, b = (_dev(i[k], torch.bfloat16).requires_grad_() for k in ("x", "W", "b"))
+    w, lab = _dev(i["weight"], torch.float32), _dev(i["labels"], torch.int32)
+    Wl = torch.full((D, N), 0.01, dtype=torch.bfloat16, device="cuda:0", requires_grad=True)
+
+    def peak(f):
+        torch.cuda.synchronize()
+        torch.cuda.reset_peak_memory_stats()
+        before = torch.cuda.memory_allocated()
+        r = f()
+        torch.cuda.synchronize()
+        return r, torch.cuda.max_memory_allocated() - before
+
+    with torch.no_grad():
+        loss, most = peak(lambda: A.rnnt_ce_loss(x, W, b, lab, row_weight=w))
+        rows, _ = peak(lambda: A.rnnt_ce_loss(x, W, b, lab, reduction="none"))
+        only, least = peak(lambda: Bd.run_ce_total(Bd.run_ce_fwd(x, W, b, lab)["loss"], w))
+        y, kept = peak(lambda: A.rnnt_linear(x, Wl, None, "silu"))
+        plain, bare = peak(lambda: Bd.run_linear_fwd(x, Wl, None, "silu")["y"])
+    assert not loss.requires_grad and torch.equal(loss, only) and not y.requires_grad and torch.equal(y, plain)
+    assert torch.equal(rows, Bd.run_ce_fwd(x, W, b, lab)["loss"])
+    # neither dW nor the chunk of exponentials, nor the saved z
+    assert most <= least and kept <= bare, (most, least, kept, bare)
+    # with gradients the value is the same
+    assert abs(float(A.rnnt_ce_loss(x, W, b, lab, row_weight=w)) - float(loss)) <= 1e-5 * abs(float(loss))

@@ -129,3 +129,45 @@ def test_a_workspace_of_another_device_is_refused(library):
     ws.buf = torch.empty(1 << 20, dtype=torch.uint8)
     Bd.run_linear_fwd(x, W, workspace=ws)
     assert len(library.calls) == 1
+
+
+@pytest.mark.parametrize("off", [torch.no_grad, torch.inference_mode])
+def test_nothing_is_computed_for_gradients_where_there_are_none(library, off):
+    from paper_2211_16270_amd import autograd as A
+    x, W, b, Wl, lab = torch.zeros(5, 8), torch.zeros(8, 24), torch.zeros(24), torch.zeros(8, 16), torch.zeros(5, dtype=torch.int32)
+    r = torch.zeros(5, 16)
+    state = torch.zeros(2, dtype=torch.int64)
+
+    def names(f):
+        library.calls.clear()
+        out = f()
+        return out, [n for n, _ in library.calls]
+
+    def layer():
+        return A.rnnt_linear(x, Wl, None, "silu", r, 0.5, state)
+
+    def check(tracked):
+        for reduction, evaluated, trained in (("sum", ["rnnt_ce_loss_fwd", "rnnt_ce_loss_total"], ["rnnt_ce_loss_fwd_bwd", "rnnt_ce_loss_total"]),
+                                              ("none", ["rnnt_ce_loss_fwd"], ["rnnt_ce_loss_fwd"])):
+            loss, called = names(lambda: A.rnnt_ce_loss(x, W, b, lab, reduction=reduction))
+            assert called == (trained if tracked else evaluated) and loss.requires_grad == tracked
+            assert loss.shape == (() if reduction == "sum" else (5,))
+        y, called = names(layer)
+        assert called == ["rnnt_linear_fwd"] and y.requires_grad == tracked
+        used, saved = (library.calls[0][1][k] for k in (6, 8))                # (rng_used, saved)
+        assert (used is not None) == tracked and (saved is not None) == tracked
+
+    check(False)
+    for t in (x, W, b, Wl):
+        t.requires_grad_()
+    check(True)
+    with off():
+        check(False)
+    for t in (x, W, b, Wl):
+        t.requires_grad_(False)
+    # a residual's gradient is dy: nothing is kept for it
+    r.requires_grad_()
+    y, _ = names(layer)
+    assert y.requires_grad and library.calls[0][1][8] is None
+    y.sum().backward()
+    assert bool((r.grad == 1).all())
