@@ -155,7 +155,8 @@ __device__ __forceinline__ void drop8(const Dropout& d, const bool (&keep)[8], f
     for (int j = 0; j < 8; ++j) v[j] = keep[j] ? v[j] * d.scale : 0.0f;
 }
 
-// FAST: by the exponential and reciprocal instructions (relative error about 1e-6, results that are rounded to bf16); else the math library's functions.
+// FAST: by the exponential and reciprocal instructions (relative error about 1e-6, from |x| = 16 on |x| 6e-8, of tanh see there; results that are rounded to
+// bf16); else the math library's functions.
 template <bool FAST>
 __device__ __forceinline__ float sigmoid(float x) {
     if constexpr (FAST) return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-LOG2E_F * x));
@@ -190,6 +191,9 @@ __device__ __forceinline__ float normal_tail(float x, float& bell) {
         return 0.5f * erfcf(0.70710678118654752f * fabsf(x));
     }
 }
+// 1 - 2 / (1 + e^{2x}) has an absolute error of 2.4e-7, so near 0 tanh is x itself, which is off by x^2 / 3 of it: 3.1e-5 at most, where the two meet.  Two
+// instructions more (16000 x 1024 x 4096: 153.8 us without them, 156.5 with; a series up to x^9 in their place, good to 1e-6, took 10 %).
+__device__ __forceinline__ float near_tanh(float x) { return fabsf(x) < 0x1p-7f ? x : fast_tanh(x); }
 template <bool FAST>
 __device__ __forceinline__ void act8(int act, float (&v)[8]) {
     switch (act) {
@@ -212,7 +216,7 @@ __device__ __forceinline__ void act8(int act, float (&v)[8]) {
             break;
         case ACT_TANH:
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = FAST ? fast_tanh(v[j]) : tanhf(v[j]);
+            for (int j = 0; j < 8; ++j) v[j] = FAST ? near_tanh(v[j]) : tanhf(v[j]);
             break;
         default: break;
     }

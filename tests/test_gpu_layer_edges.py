@@ -182,3 +182,22 @@ def test_evaluation_computes_no_gradients(R):
     assert most <= least and kept <= bare, (most, least, kept, bare)
     # with gradients the value is the same
     assert abs(float(A.rnnt_ce_loss(x, W, b, lab, row_weight=w)) - float(loss)) <= 1e-5 * abs(float(loss))
+
+
+@pytest.mark.parametrize("M", [40, 400])
+def test_tanh_of_small_arguments(M):
+    """z = x W of one nonzero product each, exact in fp32; y is off by its rounding to bf16, 2^-8, and the function's 3.1e-5: below 2^-7 it is z, off by z^2 / 3
+    (2.0e-5 of it), above 1 - 2 / (1 + e^{2z}) in fp32: the reciprocal of about 2 to 2^-23, doubled, the sum to 2^-24 and the exponential to 2^-23, times its
+    slope of 1 / 2, are 2.4e-7 together."""
+    torch = _torch()
+    K, N = 64, 128
+    g = np.random.default_rng(M)
+    x, W = np.zeros((M, K)), np.zeros((K, N))
+    x[:, 0] = np.exp(g.uniform(np.log(1e-12), np.log(2.0), M)) * g.choice([-1.0, 1.0], M)
+    W[0] = np.exp(g.uniform(np.log(0.25), np.log(4.0), N)) * g.choice([-1.0, 1.0], N)
+    xt, Wt = _dev(x, torch.bfloat16), _dev(W, torch.bfloat16)
+    want = np.tanh(_np(xt) @ _np(Wt))
+    got = _np(Bd.run_linear_fwd(xt, Wt, None, "tanh")["y"])
+    over = np.abs(got - want) / np.abs(want)
+    assert over.max() <= 2.0 ** -8 + 3.1e-5, over.max()
+    assert bool((Bd.run_linear_fwd(torch.zeros_like(xt), Wt, None, "tanh")["y"] == 0).all())
