@@ -702,8 +702,6 @@ def run_linear_fwd(x, W, b=None, activation="none", residual=None, dropout=0.0, 
                                    _ptr(saved), ws_ptr, ws_bytes, handle)
     if st != 0:
         raise RnntError(st, "rnnt_linear_fwd")
-    if rng_used is not None and desc.M == 0:
-        rng_used.copy_(rng_state)
     return dict(y=y, saved=saved, rng_used=rng_used)
 
 

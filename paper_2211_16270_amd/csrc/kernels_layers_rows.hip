@@ -46,6 +46,9 @@ __device__ __forceinline__ void pad_workgroup(const PadLaunch& p, unsigned block
     }
 }
 __global__ __launch_bounds__(256) void k_layer_pads(PadLaunch p) { pad_workgroup(p, blockIdx.x); }
+__global__ __launch_bounds__(64) void k_layer_rng(const unsigned long long* __restrict__ state, unsigned long long* __restrict__ used) {
+    if (threadIdx.x < 2) used[threadIdx.x] = state[threadIdx.x];
+}
 
 // The sums of 32 column granules over the eight thread rows of a workgroup -> part[n]
 __device__ __forceinline__ void fold_columns(float (&sum)[8], float (*red)[256], float* __restrict__ part, int n, int N, int tid) {
@@ -588,6 +591,11 @@ hipError_t launch_pads(const PadJobs& j, hipStream_t stream) {
     const PadLaunch p = pad_launch(j);
     if (p.end[2] == 0) return hipSuccess;
     k_layer_pads<<<dim3(p.end[2]), dim3(256), 0, stream>>>(p);
+    return hipGetLastError();
+}
+
+hipError_t launch_pass_rng(const unsigned long long* state, unsigned long long* used, hipStream_t stream) {
+    k_layer_rng<<<dim3(1), dim3(64), 0, stream>>>(state, used);
     return hipGetLastError();
 }
 

@@ -445,7 +445,10 @@ extern "C" rnnt_status rnnt_linear_fwd(const rnnt_linear_desc* desc, const void*
     if (rng_used && !rng) return RNNT_ERR_NULL;
     const LinearPlan p = plan_linear(*desc, false);
     if (!workspace_ok(workspace, workspace_bytes, p.bytes)) return RNNT_ERR_WORKSPACE;
-    if (desc->M == 0) return RNNT_OK;
+    if (desc->M == 0) {
+        if (rng_used) LAYER_HIP(launch_pass_rng(drop.state, (unsigned long long*)rng_used, (hipStream_t)hip_stream));
+        return RNNT_OK;
+    }
     unsigned char* ws = (unsigned char*)workspace;
     const Bias bias{b, desc->bias_bf16 != 0};
     return linear_fwd(*desc, p, x, W, bias, residual, drop, rng_used, y, saved, ws, (hipStream_t)hip_stream);

@@ -173,6 +173,8 @@ struct PadJobs {
     }
 };
 hipError_t launch_pads(const PadJobs& j, hipStream_t stream);
+// {seed, offset} of a call that launches nothing else
+hipError_t launch_pass_rng(const unsigned long long* state, unsigned long long* used, hipStream_t stream);
 
 // Rows per workgroup of a pass over [rows, cols] that leaves column sums, and so per row of these partial sums: 128 where there are workgroups of
 // 128 x 256 enough, fewer for a small array (1632 x 640 in fp32, dz: 29.6 us with 128, 39 workgroups).

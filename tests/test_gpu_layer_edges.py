@@ -201,3 +201,18 @@ def test_tanh_of_small_arguments(M):
     over = np.abs(got - want) / np.abs(want)
     assert over.max() <= 2.0 ** -8 + 3.1e-5, over.max()
     assert bool((Bd.run_linear_fwd(torch.zeros_like(xt), Wt, None, "tanh")["y"] == 0).all())
+
+
+def test_a_call_without_rows_leaves_the_state_it_took():
+    torch = _torch()
+    state = torch.tensor([123, 456], dtype=torch.int64, device="cuda:0")
+    used, W = torch.zeros(2, dtype=torch.int64, device="cuda:0"), torch.zeros(8, 8, device="cuda:0")
+    d = Bd.RnntLinearDesc(0, 8, 8, Bd.RNNT_F32, 0, 0.5, 0, 0, 0)
+    assert Bd.rnnt_linear_fwd(d, None, W, None, None, state, used, None, None) == 0
+    torch.cuda.synchronize()
+    assert used.tolist() == [123, 456]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    out = Bd.run_linear_fwd(torch.zeros(0, 8, device="cuda:0"), W, None, dropout=0.5, rng_state=state, save=True, stream=side)
+    side.synchronize()
+    assert out["rng_used"].tolist() == [123, 456] and out["y"].shape == (0, 8)
