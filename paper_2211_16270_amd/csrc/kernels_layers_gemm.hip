@@ -344,10 +344,10 @@ GemmPlan plan_gemm(long long M, long long N, int stages, size_t slot_cap) {
     return best;
 }
 // The same for two products that share a launch: workgroups of both fill the chip one after the other.
-PairPlan plan_pair(long long Mx, long long Nx, int stages_x, long long Mw, long long Nw, int stages_w, size_t slot_cap) {
+PairPlan plan_pair(long long Mx, long long Nx, int stages_x, long long Mw, long long Nw, int stages_w, size_t slot_cap, bool small) {
     PairPlan best{256, {256, 1, stages_x}, {256, 1, stages_w}};
     double least = 1e300;
-    for (int k = 0; k < 2; ++k) {
+    for (int k = small ? 1 : 0; k < 2; ++k) {
         Choice x[N_SPLITS], w[N_SPLITS];
         const int nx = choices(k, Mx, Nx, stages_x, slot_cap, ENDS_TIME[k], x), nw = choices(k, Mw, Nw, stages_w, slot_cap, ENDS_TIME[k], w);
         for (int i = 0; i < nx; ++i)
@@ -391,6 +391,7 @@ hipError_t launch_grad_gemms(bool parts, int tile, const GradGemm& dx, const Gra
         typedef TileShape<256> L;
         typedef TileShape<128> S;
         const bool twice = dx.g.A.wrap > 0 || dw.g.B.wrap > 0;
+        if (twice && tile != 128) return hipErrorInvalidValue;          // (planned for another kernel)
         const hipError_t e = parts   ? (tile == 256 ? grad_gemms<L, IN_PARTS>(dx, dw, stream) : grad_gemms<S, IN_PARTS>(dx, dw, stream))
                              : twice ? grad_gemms<S, TWICE>(dx, dw, stream)
                                      : (tile == 256 ? grad_gemms<L, ONCE>(dx, dw, stream) : grad_gemms<S, ONCE>(dx, dw, stream));

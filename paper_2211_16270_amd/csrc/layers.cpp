@@ -106,7 +106,7 @@ LinearPlan plan_linear(const rnnt_linear_desc& d, bool backward) {
         p.copy_w = p.f32 || N % 64 != 0;
         p.rest = !p.f32 && M <= FEW_ROWS && d.activation != ACT_NONE && d.activation != ACT_RELU;
         const int passes = p.rest ? 2 : per;
-        p.grads = plan_pair(M, K, (int)(p.Np / 64) * passes, K, N, (int)(p.Mp / 64) * passes, SLOT_CAP);
+        p.grads = plan_pair(M, K, (int)(p.Np / 64) * passes, K, N, (int)(p.Mp / 64) * passes, SLOT_CAP, p.rest);
         p.off_dz = c.take(p.own_dz ? (size_t)p.Mp * p.Np * e * (p.rest ? 2 : 1) : 0);
         p.off_x = c.take(p.copy_x ? (size_t)p.Mp * p.Kp * e : 0);
         p.off_w = c.take(p.copy_w ? (size_t)K * p.Np * e : 0);
@@ -291,8 +291,8 @@ CePlan plan_ce_chunk(const rnnt_ce_desc& d, bool grads, long long chunk) {
     if (grads) {
         p.off_part = c.take((size_t)sum_capacity(p.chunk, V) * p.pitch * 4);
         // (few: 64 rows, twice)
-        p.pair = p.rest ? plan_pair(FEW_ROWS, D, (int)(p.Vp / 64) * 2, D, V, 2, SLOT_CAP)
-                        : plan_pair(p.chunk, D, (int)(p.Vp / 64) * per, D, V, (int)(p.chunk / 64) * per, SLOT_CAP);
+        p.pair = p.rest ? plan_pair(FEW_ROWS, D, (int)(p.Vp / 64) * 2, D, V, 2, SLOT_CAP, true)
+                        : plan_pair(p.chunk, D, (int)(p.Vp / 64) * per, D, V, (int)(p.chunk / 64) * per, SLOT_CAP, false);
         p.off_slots = c.take(gemm_slot_bytes(p.pair.dx, p.chunk, D));
         p.off_slots_w = c.take(gemm_slot_bytes(p.pair.dw, D, V));
         // the weight gradient's sum over the chunks, where its output is bfloat16

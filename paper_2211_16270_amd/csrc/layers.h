@@ -138,7 +138,8 @@ struct PairPlan {
     int tile;
     GemmPlan dx, dw;
 };
-PairPlan plan_pair(long long Mx, long long Nx, int stages_x, long long Mw, long long Nw, int stages_w, size_t slot_cap);
+// small: 128 x 128 tiles only (an operand in two values, GemmOperand::wrap)
+PairPlan plan_pair(long long Mx, long long Nx, int stages_x, long long Mw, long long Nw, int stages_w, size_t slot_cap, bool small);
 struct SumJob {
     const float* part;
     long long rows, ld;                  // the rows that left the column sums (0: part is not read)

@@ -4,7 +4,7 @@ import pytest
 
 from paper_2211_16270_amd import binding as Bd
 from tests import layer_oracle as O
-from tests.test_gpu_layers import _ce_inputs, _check_ce, _check_linear, _dev, _linear_inputs, _np, _run_ce, _torch
+from tests.test_gpu_layers import _ce_inputs, _check_ce, _check_linear, _dev, _linear_inputs, _np, _run_ce, _run_linear, _torch
 
 pytestmark = pytest.mark.gpu
 
@@ -216,3 +216,18 @@ def test_a_call_without_rows_leaves_the_state_it_took():
     out = Bd.run_linear_fwd(torch.zeros(0, 8, device="cuda:0"), W, None, dropout=0.5, rng_state=state, save=True, stream=side)
     side.synchronize()
     assert out["rng_used"].tolist() == [123, 456] and out["y"].shape == (0, 8)
+
+
+@pytest.mark.parametrize("R,D,V", [(20, 512, 26624), (64, 704, 10624)])
+def test_cross_entropy_of_few_rows_over_long_vocabularies(R, D, V):
+    """Widths for which large tiles would be planned; operands in two values have small ones, and a plan for others is refused."""
+    i = _ce_inputs(R, D, V, True, 3)
+    ref = O.cross_entropy(i["x"], i["W"], i["b"], i["labels"], i["weight"])
+    _check_ce(_run_ce(i, True, bits=3), i, ref, True, 3)
+
+
+@pytest.mark.parametrize("M,K,N", [(1, 1088, 4032), (64, 1600, 2304)])
+def test_linear_gradients_of_few_rows_and_wide_layers(M, K, N):
+    i = _linear_inputs(M, K, N, True, res=False)
+    ref = O.linear(i["x"], i["W"], i["b"], "silu", None, None, i["dy"])
+    _check_linear(_run_linear(i, "silu", 0.0, True), i, ref, "silu", 0.0, True)
