@@ -186,13 +186,16 @@ def rnnt_ce_loss(x, W, b, labels, row_weight=None, ignore_label: int = -1, reduc
 
     x [..., D], W [D, V] (float32 or bfloat16, CUDA, contiguous), b [V] (float32 or bfloat16) or None, labels [...] int32 (rows with ignore_label are
     padding: loss and gradients 0, x never used).
-    reduction "sum": sum of row_weight * loss over the rows (row_weight [...] float32 on the device, None: ones; 1 / count for a mean), a scalar.  The
+    reduction "sum": sum of row_weight * loss over the rows (row_weight [...] float32 on the device, without a gradient
+    of its own, None: ones; 1 / count for a mean), a scalar.  The
     forward call computes the gradients too (three products per row) where one can be asked for, not under no_grad; backward scales them.
     reduction "none": the loss of each row; the gradients are computed in backward, with the incoming gradient as the rows' weights (four products)."""
     if reduction not in ("sum", "none"):
         raise ValueError(f"reduction must be 'sum' or 'none', got {reduction!r}")
     if reduction == "none" and row_weight is not None:
         raise ValueError("row_weight goes with reduction='sum'; with 'none' weight the returned losses")
+    if _tracked(row_weight):
+        raise ValueError("row_weight gets no gradient here: pass it detached, or weight the losses of reduction='none'")
     if not _tracked(x, W, b):
         loss = Bd.run_ce_fwd(x, W, b, labels, ignore_label, budget_bytes=budget_bytes)["loss"]
         return loss if reduction == "none" else Bd.run_ce_total(loss, row_weight)

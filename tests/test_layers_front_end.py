@@ -171,3 +171,20 @@ def test_nothing_is_computed_for_gradients_where_there_are_none(library, off):
     assert y.requires_grad and library.calls[0][1][8] is None
     y.sum().backward()
     assert bool((r.grad == 1).all())
+
+
+def test_weights_that_want_a_gradient_are_refused(library):
+    from paper_2211_16270_amd import autograd as A
+    x, W, lab = torch.zeros(5, 8), torch.zeros(8, 24), torch.zeros(5, dtype=torch.int32)
+    w = torch.ones(5, requires_grad=True)
+    for leaf in (False, True):
+        x.requires_grad_(leaf)
+        with pytest.raises(ValueError, match="row_weight"):
+            A.rnnt_ce_loss(x, W, None, lab, row_weight=w)
+    assert library.calls == []
+    A.rnnt_ce_loss(x, W, None, lab, row_weight=w.detach())
+    with torch.no_grad():
+        A.rnnt_ce_loss(x, W, None, lab, row_weight=w)
+    # weights by the formula: their gradient is the rows' losses
+    (A.rnnt_ce_loss(x, W, None, lab, reduction="none") * w).sum().backward()
+    assert w.grad is not None and x.grad is not None
