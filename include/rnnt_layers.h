@@ -106,7 +106,8 @@ typedef struct {
  * dx         dev [R, D]  desc->dtype, out; zeros in padding rows
  * dW dev [D, V], db dev [V] (NULL: not wanted), out
  * RNNT_BF16: the three products run on bf16 MFMA with fp32 accumulation, the softmax in fp32; dh is rounded to bfloat16 as their operand,
- * relative to the mantissa of the largest weight, in two values of it up to 64 rows.  The label's entry comes from the loss: exact also where p is near 1.
+ * relative to the mantissa of the largest weight, in two values of it up to 64 rows.  The label's entry, row_weight (p - 1), comes from the loss and is as
+ * good as that one: about row_weight 2^-20 where p is near 1 (RNNT_F32 likewise).
  *
  * workspace bytes: grads = 0 for rnnt_ce_loss_fwd, 1 for rnnt_ce_loss_fwd_bwd.  budget_bytes = 0: the library's default (chunk buffers of at most
  * 1 GiB); otherwise the size for as few chunks as the budget has room for, or, where it is too small for any number of them, the least size there is.  A
@@ -124,7 +125,8 @@ rnnt_status rnnt_ce_loss_fwd_bwd(const rnnt_ce_desc* desc, const void* x, const 
  */
 rnnt_status rnnt_ce_loss_total(const rnnt_ce_desc* desc, const float* loss, const float* row_weight, float* total, void* hip_stream);
 /*
- * dx, dW, db (each may be NULL) of rnnt_ce_loss_fwd_bwd times *factor (dev, read by the kernel), in place; a factor of 1 moves no data.
+ * dx, dW, db (each may be NULL) of rnnt_ce_loss_fwd_bwd times *factor (dev, read by the kernel), in place; a factor of 1 moves no data.  Those in bfloat16 are
+ * rounded a second time, where the factor is no power of two: weights that hold it already spare them that.
  */
 rnnt_status rnnt_ce_loss_scale(const rnnt_ce_desc* desc, const float* factor, void* dx, void* dW, void* db, void* hip_stream);
 

@@ -186,9 +186,9 @@ def rnnt_ce_loss(x, W, b, labels, row_weight=None, ignore_label: int = -1, reduc
 
     x [..., D], W [D, V] (float32 or bfloat16, CUDA, contiguous), b [V] (float32 or bfloat16) or None, labels [...] int32 (rows with ignore_label are
     padding: loss and gradients 0, x never used).
-    reduction "sum": sum of row_weight * loss over the rows (row_weight [...] float32 on the device, without a gradient
-    of its own, None: ones; 1 / count for a mean), a scalar.  The
-    forward call computes the gradients too (three products per row) where one can be asked for, not under no_grad; backward scales them.
+    reduction "sum": sum of row_weight * loss over the rows (row_weight [...] float32 on the device, without a gradient of its own, None: ones; 1 / count for
+    a mean), a scalar.  The forward call computes the gradients too (three products per row) where one can be asked for, not under no_grad; backward scales them, which
+    rounds those of bfloat16 leaves a second time unless the incoming gradient is a power of two (1 with loss.backward(); put other factors into row_weight).
     reduction "none": the loss of each row; the gradients are computed in backward, with the incoming gradient as the rows' weights (four products)."""
     if reduction not in ("sum", "none"):
         raise ValueError(f"reduction must be 'sum' or 'none', got {reduction!r}")

@@ -195,7 +195,7 @@ struct ColumnBias {
 // Before the fourth every wave has read all it needs of the stage and the next one has landed: one barrier per stage.  The copies of A two stages ahead
 // go out in the first two steps (their buffer became free a stage ago), those of B in the fourth, into the buffer that has just become free.  (Two stages of
 // both, all copies in the fourth step: 8192^3 1250 to 1280 TFLOP/s, now 1346 to 1374; without any copies 1470 to 1510.  The rest of the loss is the prologue and
-// the epilogue, which nothing hides: K = 1024 980 TFLOP/s.)  A wave has priority while it sends MFMAs (K = 1024: 874 without).
+// the epilogue, which nothing hides: 16000 x 1024 x 4096 930 TFLOP/s.)  A wave has priority while it sends MFMAs (11 % of that less without).
 // init: what the sums of the columns start from.
 // IN_PARTS: the matrix instruction's accumulation rounds towards minus infinity, alike for all results: 5e-11 of a result's size per unit of
 // depth, which sums over many of them would show.  So every 1024 of depth the sum changes its sign, and B enters with the other one.

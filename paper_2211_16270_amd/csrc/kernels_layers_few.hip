@@ -1,5 +1,5 @@
 // A few rows (at most 64) through a layer: single tokens, beams.  The product is bound by reading W, the call by latency, so one launch does it all
-// (1 row, K = 640, N = 2560: 4.1 us on the GPU, W's 3.3 MB at a copy's rate 0.7).
+// (1 row, K = 640, N = 2560: 4.4 us, W's 3.3 MB at a copy's rate 0.7).  Times in this file: a call among others in a captured graph; the profiler shows 0.6 to 0.8 more.
 #include <algorithm>
 
 #include "layers_device.h"
@@ -190,7 +190,8 @@ __global__ __launch_bounds__(64 * FW) void k_few_rows(FewJob j, E e, int blocks,
 }
 
 // The same in fp32 on the fp32 matrix instruction (16 x 16 x 4), which takes its operands as they lie: a wave's step of 32 along k is eight of them, the
-// i-th with k = 8 g + i in the lanes of group g = l / 16, so that a lane's eight values of x are one piece.  1 x 640 x 2560 6.0 us, 64 x 640 x 2560 9.7.
+// i-th with k = 8 g + i in the lanes of group g = l / 16, so that a lane's eight values of x are one piece.  1 x 640 x 2560 6.3 us, 64 x 640 x 2560 9.8: sixteen loads of four bytes of W a
+// step, two steps of them in flight.
 template <int MT, bool WHOLE, class E>
 __global__ __launch_bounds__(64 * FW) void k_few_rows_f32(FewJob j, E e, int blocks, float* __restrict__ slots, int per_split) {
     __shared__ __align__(16) unsigned char smem[FW * MT * 16 * FC * 4];
@@ -257,7 +258,8 @@ __global__ __launch_bounds__(64 * FW) void k_few_rows_f32(FewJob j, E e, int blo
 }
 
 // Blocks of 16 rows per workgroup: as few as leave a workgroup per compute unit at most.  A wave's loads of x are what takes long, and W comes from the L2 for
-// all but the first (64 rows, K = 640, N = 2560: 5.4 us, 7.3 with all rows in one workgroup; K = 2560, N = 640 7.0 and 10.3).
+// all but the first (bf16, 64 rows, K = 640, N = 2560: 5.6 us, 7.6 with all rows in one workgroup; K = 2560, N = 640 7.2 and 14.9; fp32 9.8 and 16.2, but 15.5 and
+// 13.2, where the long sum is split too).
 int few_blocks(int M, int N) {
     const int columns = (N + FC - 1) / FC, all = (M + 15) / 16;
     int mt = 1;
@@ -286,8 +288,8 @@ hipError_t launch_few(const FewJob& j, const E& e, int splits, float* slots, hip
 }  // namespace
 
 // Long sums are shared by as many workgroups as fill the chip, each with a step per wave at least: in fp32, whose steps take sixteen loads of W each, from five
-// steps per wave on (1 row, K = 2560, N = 640: 7.2 us, 14.4 in one workgroup per 32 columns), in bf16 from seventeen (with ten 6.6 us, 5.7 so: the second
-// launch takes what the split saves).
+// steps per wave on (1 row, K = 2560, N = 640: 7.5 us, 14.7 in one workgroup per 32 columns; 64 rows 15.5 and 16.4), in bf16 from seventeen (with ten, split, 6.8 us
+// and 9.4 for 64 rows; 5.9 and 7.2 so: the second launch takes what the split saves).
 int few_splits(bool f32, long long M, int K, int N) {
     if (M < 1 || M > FEW_ROWS) return 1;
     const int steps = (K + 31) / 32, mt = few_blocks((int)M, N), blocks = (N + FC - 1) / FC * (((int)M + 16 * mt - 1) / (16 * mt));

@@ -83,8 +83,9 @@ struct TileJob {
     int mt, nt, splits, per_split;
     __host__ __device__ long long workgroups() const { return ((long long)mt * nt * splits + 7) / 8 * 8; }
 };
-// y, or a split of it.  Bound by the matrix units' power in long sums, by each tile's start and epilogue in short ones: 16000 x 1024 x 4096 137 us (980 TFLOP/s)
-// plain, 175 with gelu, dropout and the saved z (their vector work, nothing hides it); 8000 x 512 x 2048 27 and 35.
+// y, or a split of it.  Bound by the matrix units' power in long sums, by each tile's start and epilogue in short ones: 16000 x 1024 x 4096 143 to 147 us (930
+// TFLOP/s) plain, 160 with silu, 177 with gelu, 208 to 212 with gelu, dropout and the saved z (their vector work and its bytes, nothing hides them); 8000 x 512 x 2048
+// 28 plain, 39 with silu, dropout and the saved z.
 template <class TS, bool AKS, bool BKS, Passes HOW, class E>
 __global__ __launch_bounds__(TS::THREADS, 2) void k_layer_gemm(TileJob<E> j) {
     extern __shared__ __align__(16) unsigned char smem[];

@@ -330,7 +330,7 @@ __global__ __launch_bounds__(256) void k_ce_gather(const T* __restrict__ x, long
 }
 
 // Row i of a chunk: lse = M + ln(S / 2^15) out of the parts' statistics, loss = lse - score of the label (at < 0: not written); its scale.  The label's gradient
-// w (p - 1) = w expm1(-loss): the difference would leave little of it where p is near 1.
+// w (p - 1) = w expm1(-loss): as good as the loss, about w 2^-20, where the kept exponential's p would leave it w 2^-12.
 __device__ __forceinline__ float4 ce_finish_row(const CeChunk& c, long long i, int at, float M, float S) {
     const float m = M == RNNT_NEG_INF ? 0.0f : M;
     const int y = c.r.label[c.row0 + i];

@@ -128,7 +128,7 @@ GemmOperand operand(bool copied, bool f32, const void* own, long long ld, const 
 // A bf16 product with an operand in two values: `once` by the rounded ones, then by the rest.
 // Rounding the gradient to bf16 adds as much to the products' error as their own rounding does, sqrt(2) times it where many values average; the few of a few
 // rows do not (up to 3 times).  There, up to FEW_ROWS rows, the products wait for W and dW rather than for their operations (backward pass of 64 x 512 x 2048
-// 14.3 us with dz in one value, 16.8 in two; 64 x 1024 x 4096 21.7 and 25.4).
+// in a captured graph 14.5 us with dz in one value (relu), 17.2 in two (silu); 64 x 1024 x 4096 20.4 and 23.3).
 void take_twice(GemmOperand& once, GemmOperand& two, long long rest, int stages) {
     once.wrap = two.wrap = stages;
     two.part = rest;
